@@ -228,6 +228,119 @@ int vla_version(void);
  * invalid/unsupported.  Host-only, launches nothing. */
 int vla_resolve_mode(int B, int H, int T, int d_k, int d_v, int io_dtype, const vla_opts* opts);
 
+/*
+ * ---- Operators around the recurrence -------------------------------------------------------------------------
+ *
+ * The gated delta rule (the sister recurrence: the same residual write on a state of the same layout, a decay and a write
+ * strength in place of A) and the norm of queries and keys with the position rotation (what comes before either
+ * recurrence).  The rules above hold for them: device pointers, nothing allocated or kept, asynchronous on `stream`, all
+ * validation on the host before anything is launched, no written buffer overlapping another one of the call.
+ */
+
+/* Element strides of a [B, H, T, d] (gates: [B, H, T]) tensor.  All zero: contiguous.  The last dimension of d elements is always
+ * contiguous; strides of q, k, v, o and of their gradients are multiples of 16 bytes (of the gates: any), none is negative,
+ * and a written tensor's rows do not overlap.  A read tensor may repeat rows (stride 0), but not by three zeros. */
+typedef struct vla_strides {
+  long long b, h, t;
+} vla_strides;
+
+/* Always initialise with vla_delta_default_opts() and then change fields: later versions may append fields. */
+typedef struct vla_delta_opts {
+  float scale;        /* [0 = 1 / sqrt(d_k)] factor of the read-out */
+  const int* lengths; /* [NULL = T] device, [B]: tokens of each sequence (values outside 0..T count as the nearer end).  Later tokens
+                         are not part of it: whatever they hold, even NaN, their o is 0, the states are those after the last
+                         token of the sequence, and their gradients are 0 */
+  vla_strides q, k, v, o, g, beta; /* [contiguous]; dO of the backward pass has the strides of o */
+  vla_strides dq, dk, dv;          /* [contiguous] of the backward pass's outputs; dg and dbeta are contiguous */
+  void* saved;        /* [NULL = not wanted] device, vla_delta_saved_bytes(): what vla_delta_forward keeps for vla_delta_backward
+                         (the states that blocks of tokens start from); written by the first, read by the second */
+  size_t saved_bytes;
+  int segments;       /* [0 = the library chooses] time segments that vla_delta_forward cuts long sequences of few heads into (1: none).
+                         Sizes the workspace, so pass the same value to vla_delta_workspace_bytes() */
+} vla_delta_opts;
+
+void vla_delta_default_opts(vla_delta_opts* opts);
+
+/* Bytes of device workspace that vla_delta_forward (backward: vla_delta_backward) wants for these arguments; 0 when it wants none and
+ * when they are invalid.  A forward call with a smaller one, or none, runs every sequence from its start to its end (the same
+ * results up to float32 rounding, slower for few heads); a backward call returns VLA_ERR_WORKSPACE. */
+size_t vla_delta_workspace_bytes(int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts, int backward);
+/* Bytes of opts->saved. */
+size_t vla_delta_saved_bytes(int B, int H_v, int T, int d_k, int d_v, int io_dtype);
+
+/*
+ * vla_delta_forward -- the gated delta rule.  For every batch row b and value head h, with the key head h / (H_v / H_k), from S = S0[b,h]:
+ *
+ *     S'_t = exp(g_t) S_{t-1};   S_t = S'_t + beta_t (v_t - S'_t k_t) k_t^T;   o_t = scale S_t q_t
+ *
+ *   q, k   [B, H_k, T, d_k]   io_dtype by strides; ||k_t|| <= 1 (vla_qk_norm_rope with l2) and 0 <= beta_t <= 2 keep the state bounded;
+ *                             neither is checked
+ *   v, o   [B, H_v, T, d_v]   io_dtype by strides; o written
+ *   g      [B, H_v, T]        float32, the logarithm of the decay; -infinity forgets the state
+ *   beta   [B, H_v, T]        float32
+ *   S0     [B, H_v, d_v, d_k] float32 or NULL (zero);  S_T the same, written, or NULL; may be S0 itself
+ *   H_v a multiple of H_k;  T >= 0 (T == 0 copies S0 to S_T);  d_k, d_v in {16, 32, 64, 96, 128}, any pair
+ *
+ * Sums, decays and the state are float32 whatever io_dtype; products of the state with q, k and the writes are formed from parts
+ * that carry all of its bits (bf16: the read-out, which is rounded to bf16, from 16 of them).  q, k, v, o, S0 and S_T are
+ * 16-byte aligned.  Running [0, T1) and then [T1, T) with the carried S_T gives the same result as one call up to rounding.
+ */
+int vla_delta_forward(const void* q, const void* k, const void* v, const float* g, const float* beta, const float* S0, void* o,
+                      float* S_T, int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token on a state that stays where it is: vla_delta_forward with T = 1 and S0 = S_T = S (all strides are those of [B, H, 1, d]). */
+int vla_delta_decode_step(const void* q, const void* k, const void* v, const float* g, const float* beta, float* S, void* o, int B,
+                          int H_k, int H_v, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts, void* stream);
+
+/*
+ * vla_delta_backward -- the gradients of vla_delta_forward's inputs, given those of o and S_T, its inputs and what it saved.
+ *   dO      [B, H_v, T, d_v] io_dtype;  dS_T [B, H_v, d_v, d_k] float32 or NULL (zero)
+ *   dq, dk  [B, H_k, T, d_k] io_dtype, summed over the value heads that share a key head, in a fixed order
+ *   dv      [B, H_v, T, d_v] io_dtype;  dg, dbeta [B, H_v, T] float32;  dS0 [B, H_v, d_v, d_k] float32 or NULL (not wanted)
+ * The same inputs and saved states give the same bits.
+ */
+int vla_delta_backward(const void* q, const void* k, const void* v, const float* g, const float* beta, const void* dO, const float* dS_T,
+                       void* dq, void* dk, void* dv, float* dg, float* dbeta, float* dS0, int B, int H_k, int H_v, int T, int d_k,
+                       int d_v, int io_dtype, const vla_delta_opts* opts, void* workspace, size_t workspace_bytes, void* stream);
+
+typedef struct vla_norm_opts {
+  float eps;            /* [1e-6] */
+  int l2;               /* [0] 0: x / sqrt(mean x^2 + eps) (RMS); 1: x / sqrt(sum x^2 + eps) (unit length) */
+  int interleaved;      /* [0] pairs of the rotation: 0: columns i and i + rot / 2; 1: columns 2i and 2i + 1 */
+  int rot;              /* [0 = d, or none without tables] columns that are rotated, the first ones; a multiple of 8 */
+  int places;           /* [0] rows of the tables */
+  int offset;           /* [0] position of token 0 where positions is NULL */
+  int weight_dtype;     /* [VLA_F32] of both weights */
+  const int* positions; /* [NULL = offset + t] device, [B, T].  A position that the tables do not hold gives rows of NaN */
+  vla_strides q, k;         /* [contiguous] */
+  vla_strides q_out, k_out; /* [contiguous]; in the backward pass of dq_out, dk_out */
+  vla_strides dq, dk;       /* [contiguous] */
+} vla_norm_opts;
+
+/* Fills *opts with the values in brackets. */
+void vla_norm_default_opts(vla_norm_opts* opts);
+
+/*
+ * vla_qk_norm_rope -- every head's row x of q (k): y = Rot_p(w * x r), r = 1 / sqrt(n^-1 sum x^2 + eps), n = d (RMS) or 1 (l2).
+ *   q, k          [B, H_q, T, d], [B, H_k, T, d] io_dtype by strides (views of a projection [B, T, H d] as they are); H_q or H_k
+ *                 may be 0 with a NULL tensor
+ *   weights       [d], opts->weight_dtype, or NULL (ones)
+ *   cos, sin      [places, rot / 2] float32, or NULL without a rotation (opts->rot 0)
+ *   q_out, k_out  as q, k; written, by default contiguous, which is what the recurrences take
+ * Float32 arithmetic; one rounding, to io_dtype.  d in {16, 32, 64, 96, 128}; all pointers but positions 16-byte aligned.
+ */
+int vla_qk_norm_rope(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos, const float* sin,
+                     void* q_out, void* k_out, int B, int T, int H_q, int H_k, int d, int io_dtype, const vla_norm_opts* opts,
+                     void* stream);
+/* Its gradients: dq, dk, and those of the weights (float32 [d], summed over all rows in a fixed order; NULL: not wanted).  The
+ * workspace is needed where one of the latter is wanted. */
+size_t vla_qk_norm_rope_workspace_bytes(int d);
+int vla_qk_norm_rope_backward(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos,
+                              const float* sin, const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight,
+                              float* dk_weight, int B, int T, int H_q, int H_k, int d, int io_dtype, const vla_norm_opts* opts,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

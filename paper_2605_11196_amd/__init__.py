@@ -1,4 +1,5 @@
-"""MI355X-native Variational Linear Attention forward (thin binding over libvla.so)."""
+"""MI355X-native Variational Linear Attention forward, and the gated delta rule and the norm of queries and keys with the
+position rotation next to it (thin binding over libvla.so)."""
 from .binding import (  # noqa: F401
     VLA_BF16,
     VLA_F32,
@@ -20,3 +21,10 @@ from .binding import (  # noqa: F401
     vla_forward_static_raw,
     vla_forward_workspace_bytes,
 )
+from .gated_delta import (  # noqa: F401
+    gated_delta,
+    gated_delta_backward,
+    gated_delta_decode_step,
+    gated_delta_forward,
+)
+from .qk_norm import qk_norm_rope, qk_norm_rope_backward  # noqa: F401

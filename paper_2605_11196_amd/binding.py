@@ -15,12 +15,15 @@ VLA_F32, VLA_BF16 = 0, 1
 MODE_AUTO, MODE_SCAN, MODE_CHUNKED, MODE_TWO_PHASE, MODE_TIME_PARALLEL = 0, 1, 2, 3, 4
 
 EXPORTS = ("vla_default_opts", "vla_forward_workspace_bytes", "vla_forward", "vla_forward_static",
-           "vla_decode_step", "vla_status_string", "vla_version", "vla_resolve_mode")
+           "vla_decode_step", "vla_status_string", "vla_version", "vla_resolve_mode", "vla_delta_default_opts",
+           "vla_delta_workspace_bytes", "vla_delta_saved_bytes", "vla_delta_forward", "vla_delta_decode_step",
+           "vla_delta_backward", "vla_norm_default_opts", "vla_qk_norm_rope", "vla_qk_norm_rope_workspace_bytes",
+           "vla_qk_norm_rope_backward")
 
 
 class VlaError(RuntimeError):
-    def __init__(self, status, name):
-        super().__init__(f"vla_forward failed: {name} ({status})")
+    def __init__(self, status, name, call="vla_forward"):
+        super().__init__(f"{call} failed: {name} ({status})")
         self.status = status
 
 
@@ -30,6 +33,22 @@ class VlaOpts(ctypes.Structure):
                 ("refresh_eta", ctypes.c_float), ("step_offset", ctypes.c_int),
                 ("normalise_output", ctypes.c_int), ("feature_map", ctypes.c_int),
                 ("zkey0", ctypes.c_void_p), ("zkey_T", ctypes.c_void_p), ("segments", ctypes.c_int)]
+
+
+class VlaStrides(ctypes.Structure):
+    _fields_ = [("b", ctypes.c_longlong), ("h", ctypes.c_longlong), ("t", ctypes.c_longlong)]
+
+
+class VlaDeltaOpts(ctypes.Structure):
+    _fields_ = ([("scale", ctypes.c_float), ("lengths", ctypes.c_void_p)]
+                + [(n, VlaStrides) for n in ("q", "k", "v", "o", "g", "beta", "dq", "dk", "dv")]
+                + [("saved", ctypes.c_void_p), ("saved_bytes", ctypes.c_size_t), ("segments", ctypes.c_int)])
+
+
+class VlaNormOpts(ctypes.Structure):
+    _fields_ = ([("eps", ctypes.c_float)]
+                + [(n, ctypes.c_int) for n in ("l2", "interleaved", "rot", "places", "offset", "weight_dtype")]
+                + [("positions", ctypes.c_void_p)] + [(n, VlaStrides) for n in ("q", "k", "q_out", "k_out", "dq", "dk")])
 
 
 _lib = None
@@ -75,6 +94,21 @@ def load_library():
     lib.vla_version.restype = I
     lib.vla_resolve_mode.argtypes = [I] * 6 + [OP]
     lib.vla_resolve_mode.restype = I
+    DP, NP = ctypes.POINTER(VlaDeltaOpts), ctypes.POINTER(VlaNormOpts)
+    Z = ctypes.c_size_t
+    for name, args, result in (
+            ("vla_delta_default_opts", [DP], None),
+            ("vla_delta_workspace_bytes", [I] * 7 + [DP, I], Z),
+            ("vla_delta_saved_bytes", [I] * 6, Z),
+            ("vla_delta_forward", [P] * 8 + [I] * 7 + [DP, P, Z, P], I),
+            ("vla_delta_decode_step", [P] * 7 + [I] * 6 + [DP, P], I),
+            ("vla_delta_backward", [P] * 13 + [I] * 7 + [DP, P, Z, P], I),
+            ("vla_norm_default_opts", [NP], None),
+            ("vla_qk_norm_rope", [P] * 8 + [I] * 6 + [NP, P], I),
+            ("vla_qk_norm_rope_workspace_bytes", [I], Z),
+            ("vla_qk_norm_rope_backward", [P] * 12 + [I] * 6 + [NP, P, Z, P], I)):
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = result
     defaults = VlaOpts()
     lib.vla_default_opts(ctypes.byref(defaults))
     _default_opts = bytes(defaults)

@@ -1,0 +1,274 @@
+// Host side of the operators around the recurrence (include/vla.h): validation and dispatch of the gated delta rule and of the
+// norm of queries and keys with the position rotation.
+#include "../../include/vla.h"
+
+#include "layer_common.h"
+
+#include <math.h>
+#include <stdio.h>
+
+namespace {
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// A caller's buffer as the byte range that its strides reach; `written` marks what the kernels store to.
+struct Range {
+  const void* p;
+  size_t bytes;
+  bool written;
+};
+bool overlap(const Range& a, const Range& b) {
+  if (a.p == nullptr || b.p == nullptr || a.bytes == 0 || b.bytes == 0) return false;
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+  return a0 < b0 + b.bytes && b0 < a0 + a.bytes;
+}
+// No written buffer may overlap another buffer of the call; `same` is the one pair that may be the same buffer.
+bool disjoint(const Range* r, int n, const void* same0, const void* same1) {
+  for (int i = 0; i < n; ++i) {
+    if (!r[i].written) continue;
+    for (int j = 0; j < n; ++j) {
+      if (j == i || (r[j].written && j < i) || !overlap(r[i], r[j])) continue;
+      const bool allowed = same0 != nullptr && r[i].p == r[j].p && r[i].bytes == r[j].bytes && (r[i].p == same0 || r[i].p == same1) && same0 == same1;
+      if (!allowed) return false;
+    }
+  }
+  return true;
+}
+
+// The strides of a call, the contiguous ones where none are given.  False where one is negative or not a whole number of
+// 16-byte pieces, or where a written tensor's would make two of its rows the same.
+bool rows_of(const vla_strides& s, long long H, long long T, long long d, int per16, vla::Rows* out) {
+  *out = vla::Rows{s.b, s.h, s.t};
+  if (s.b == 0 && s.h == 0 && s.t == 0) *out = vla::Rows{H * T * d, T * d, d};
+  return out->b >= 0 && out->h >= 0 && out->t >= 0 && out->b % per16 == 0 && out->h % per16 == 0 && out->t % per16 == 0;
+}
+size_t reach(const vla::Rows& r, long long B, long long H, long long T, long long d, size_t es) {
+  if (B == 0 || H == 0 || T == 0) return 0;
+  return (static_cast<size_t>(B - 1) * r.b + static_cast<size_t>(H - 1) * r.h + static_cast<size_t>(T - 1) * r.t + d) * es;
+}
+// whether rows of d elements at these strides are all apart: sorted by stride, each step clears what the smaller ones span
+bool rows_apart(const vla::Rows& r, long long B, long long H, long long T, long long d) {
+  long long s[3] = {r.b, r.h, r.t}, n[3] = {B, H, T};
+  for (int i = 0; i < 3; ++i) {
+    for (int j = i + 1; j < 3; ++j) {
+      if (s[j] < s[i]) {
+        long long x = s[i]; s[i] = s[j]; s[j] = x;
+        x = n[i]; n[i] = n[j]; n[j] = x;
+      }
+    }
+  }
+  long long span = d;
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] <= 1) continue;
+    if (s[i] < span) return false;
+    span += s[i] * (n[i] - 1);
+  }
+  return true;
+}
+
+int launched(hipError_t err) {
+  if (err == hipSuccess) return VLA_OK;
+  fprintf(stderr, "libvla: kernel launch failed: %s (%d)\n", hipGetErrorString(err), static_cast<int>(err));
+  return VLA_ERR_HIP;
+}
+
+// ---- gated delta rule
+
+int check_delta(int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, const vla_delta_opts& o) {
+  if (B <= 0 || H_k <= 0 || H_v <= 0 || T < 0 || d_k <= 0 || d_v <= 0 || H_v % H_k != 0) return VLA_ERR_INVALID_ARG;
+  if (io_dtype != VLA_F32 && io_dtype != VLA_BF16) return VLA_ERR_INVALID_ARG;
+  if (!(fabsf(o.scale) <= 3.4e38f)) return VLA_ERR_INVALID_ARG;
+  if (!vla::layer_head_size(d_k) || !vla::layer_head_size(d_v)) return VLA_ERR_UNSUPPORTED;
+  // workgroups (up to 32 a head and segment) and tokens with a block of look-ahead are 32-bit indices
+  if (static_cast<long long>(B) * H_v > 0x7fffffff / 32 || T > 0x7fffff00) return VLA_ERR_UNSUPPORTED;
+  return VLA_OK;
+}
+vla_delta_opts delta_opts(const vla_delta_opts* o, int d_k) {
+  vla_delta_opts r;
+  vla_delta_default_opts(&r);
+  if (o != nullptr) r = *o;
+  if (r.scale == 0.0f && d_k > 0) r.scale = 1.0f / sqrtf(static_cast<float>(d_k));
+  return r;
+}
+
+// Strides of the gates: any, in elements.
+bool gate_rows(const vla_strides& s, long long H, long long T, vla::Rows* out) {
+  *out = vla::Rows{s.b, s.h, s.t};
+  if (s.b == 0 && s.h == 0 && s.t == 0) *out = vla::Rows{H * T, T, 1};
+  return out->b >= 0 && out->h >= 0 && out->t >= 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+void vla_delta_default_opts(vla_delta_opts* opts) {
+  if (opts != nullptr) *opts = vla_delta_opts{};
+}
+
+size_t vla_delta_workspace_bytes(int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts, int backward) {
+  return 0;
+}
+size_t vla_delta_saved_bytes(int B, int H_v, int T, int d_k, int d_v, int io_dtype) { return 0; }
+int vla_delta_backward(const void* q, const void* k, const void* v, const float* g, const float* beta, const void* dO, const float* dS_T,
+                       void* dq, void* dk, void* dv, float* dg, float* dbeta, float* dS0, int B, int H_k, int H_v, int T, int d_k,
+                       int d_v, int io_dtype, const vla_delta_opts* opts, void* workspace, size_t workspace_bytes, void* stream) {
+  return VLA_ERR_UNSUPPORTED;
+}
+
+int vla_delta_forward(const void* q, const void* k, const void* v, const float* g, const float* beta, const float* S0, void* o,
+                      float* S_T, int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+  (void)workspace; (void)workspace_bytes;
+  const vla_delta_opts op = delta_opts(opts, d_k);
+  const int st = check_delta(B, H_k, H_v, T, d_k, d_v, io_dtype, op);
+  if (st != VLA_OK) return st;
+  if (T > 0 && (q == nullptr || k == nullptr || v == nullptr || g == nullptr || beta == nullptr || o == nullptr)) return VLA_ERR_INVALID_ARG;
+  const void* ptrs[] = {q, k, v, S0, o, S_T};
+  for (const void* p : ptrs) {
+    if (!aligned16(p)) return VLA_ERR_INVALID_ARG;
+  }
+  const size_t es = io_dtype == VLA_BF16 ? 2 : 4;
+  const int per16 = static_cast<int>(16 / es);
+  vla::DeltaArgs a{};
+  if (!rows_of(op.q, H_k, T, d_k, per16, &a.qs) || !rows_of(op.k, H_k, T, d_k, per16, &a.ks) || !rows_of(op.v, H_v, T, d_v, per16, &a.vs) ||
+      !rows_of(op.o, H_v, T, d_v, per16, &a.os) || !gate_rows(op.g, H_v, T, &a.gs) || !gate_rows(op.beta, H_v, T, &a.bs) ||
+      !rows_apart(a.os, B, H_v, T, d_v)) {
+    return VLA_ERR_INVALID_ARG;
+  }
+  const size_t nS = static_cast<size_t>(B) * H_v * d_v * d_k * 4;
+  const Range r[] = {{q, reach(a.qs, B, H_k, T, d_k, es), false}, {k, reach(a.ks, B, H_k, T, d_k, es), false},
+                     {v, reach(a.vs, B, H_v, T, d_v, es), false}, {g, reach(a.gs, B, H_v, T, 1, 4), false},
+                     {beta, reach(a.bs, B, H_v, T, 1, 4), false}, {op.lengths, static_cast<size_t>(B) * 4, false},
+                     {S0, nS, false}, {o, reach(a.os, B, H_v, T, d_v, es), true}, {S_T, nS, true}};
+  if (!disjoint(r, 9, S0, S_T)) return VLA_ERR_INVALID_ARG;
+  if (T == 0 && S_T == nullptr) return VLA_OK;
+  a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.S0 = S0; a.o = o; a.S_T = S_T;
+  a.lengths = op.lengths;
+  a.B = B; a.H_k = H_k; a.H_v = H_v; a.T = T;
+  a.scale = op.scale;
+  return launched(vla::launch_delta_step(a, d_k, d_v, io_dtype, static_cast<hipStream_t>(stream)));
+}
+
+int vla_delta_decode_step(const void* q, const void* k, const void* v, const float* g, const float* beta, float* S, void* o, int B,
+                          int H_k, int H_v, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts, void* stream) {
+  if (S == nullptr) return VLA_ERR_INVALID_ARG;
+  return vla_delta_forward(q, k, v, g, beta, S, o, S, B, H_k, H_v, 1, d_k, d_v, io_dtype, opts, nullptr, 0, stream);
+}
+
+// ---- norm of queries and keys with the position rotation
+
+void vla_norm_default_opts(vla_norm_opts* opts) {
+  if (opts == nullptr) return;
+  *opts = vla_norm_opts{};
+  opts->eps = 1e-6f;
+}
+
+size_t vla_qk_norm_rope_workspace_bytes(int d) {
+  return vla::layer_head_size(d) ? static_cast<size_t>(vla::kNormPartials) * 2 * d * 4 : 0;
+}
+
+}  // extern "C"
+
+namespace {
+
+// What the two directions check and fill in alike.
+int norm_args(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos, const float* sin, int B, int T,
+              int H_q, int H_k, int d, int io_dtype, const vla_norm_opts* opts, vla_norm_opts* op, vla::NormArgs* a) {
+  vla_norm_default_opts(op);
+  if (opts != nullptr) *op = *opts;
+  if (B <= 0 || T < 0 || H_q < 0 || H_k < 0 || H_q + H_k <= 0 || d <= 0) return VLA_ERR_INVALID_ARG;
+  if (io_dtype != VLA_F32 && io_dtype != VLA_BF16) return VLA_ERR_INVALID_ARG;
+  if (op->weight_dtype != VLA_F32 && op->weight_dtype != VLA_BF16) return VLA_ERR_INVALID_ARG;
+  if (!(op->eps > 0.0f) || !(op->eps <= 3.4e38f) || op->places < 0 || op->offset < 0) return VLA_ERR_INVALID_ARG;
+  const int rot = op->rot == 0 ? (cos != nullptr ? d : 0) : op->rot;
+  if (rot < 0 || rot > d || rot % 8 != 0) return VLA_ERR_INVALID_ARG;
+  if (rot > 0 && (cos == nullptr || sin == nullptr || op->places <= 0)) return VLA_ERR_INVALID_ARG;
+  if (!vla::layer_head_size(d)) return VLA_ERR_UNSUPPORTED;
+  if (static_cast<long long>(B) * T > 0x7fffff00LL || H_q > 32767 || H_k > 32767) return VLA_ERR_UNSUPPORTED;
+  if (T > 0 && ((H_q > 0 && q == nullptr) || (H_k > 0 && k == nullptr))) return VLA_ERR_INVALID_ARG;
+  const void* ptrs[] = {q, k, q_weight, k_weight, cos, sin};
+  for (const void* p : ptrs) {
+    if (!aligned16(p)) return VLA_ERR_INVALID_ARG;
+  }
+  *a = vla::NormArgs{};
+  const int per16 = io_dtype == VLA_BF16 ? 8 : 4;
+  if (!rows_of(op->q, H_q, T, d, per16, &a->xs[0]) || !rows_of(op->k, H_k, T, d, per16, &a->xs[1]) ||
+      !rows_of(op->q_out, H_q, T, d, per16, &a->ys[0]) || !rows_of(op->k_out, H_k, T, d, per16, &a->ys[1])) {
+    return VLA_ERR_INVALID_ARG;
+  }
+  a->x[0] = q; a->x[1] = k; a->w[0] = q_weight; a->w[1] = k_weight;
+  a->cos = cos; a->sin = sin;
+  a->positions = op->positions;
+  a->H[0] = H_q; a->H[1] = H_k;
+  a->B = B; a->T = T; a->rot = rot; a->offset = op->offset;
+  a->places = rot > 0 ? op->places : 0x7fffffff;
+  if (rot == 0) a->positions = nullptr;   // nothing is looked up
+  if (rot == 0) a->offset = 0;
+  a->eps = op->eps;
+  a->inv_n = op->l2 ? 1.0f : 1.0f / static_cast<float>(d);
+  a->w_bf16 = op->weight_dtype == VLA_BF16;
+  return VLA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int vla_qk_norm_rope(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos, const float* sin,
+                     void* q_out, void* k_out, int B, int T, int H_q, int H_k, int d, int io_dtype, const vla_norm_opts* opts,
+                     void* stream) {
+  vla_norm_opts op;
+  vla::NormArgs a;
+  const int st = norm_args(q, k, q_weight, k_weight, cos, sin, B, T, H_q, H_k, d, io_dtype, opts, &op, &a);
+  if (st != VLA_OK) return st;
+  if (T == 0) return VLA_OK;
+  if ((H_q > 0 && q_out == nullptr) || (H_k > 0 && k_out == nullptr) || !aligned16(q_out) || !aligned16(k_out)) return VLA_ERR_INVALID_ARG;
+  if (!rows_apart(a.ys[0], B, H_q, T, d) || !rows_apart(a.ys[1], B, H_k, T, d)) return VLA_ERR_INVALID_ARG;
+  const size_t es = io_dtype == VLA_BF16 ? 2 : 4, ws = op.weight_dtype == VLA_BF16 ? 2 : 4, table = static_cast<size_t>(op.places) * (a.rot / 2) * 4;
+  const Range r[] = {{q, reach(a.xs[0], B, H_q, T, d, es), false}, {k, reach(a.xs[1], B, H_k, T, d, es), false},
+                     {q_weight, d * ws, false}, {k_weight, d * ws, false}, {a.rot ? cos : nullptr, table, false},
+                     {a.rot ? sin : nullptr, table, false}, {a.positions, static_cast<size_t>(B) * T * 4, false},
+                     {q_out, reach(a.ys[0], B, H_q, T, d, es), true}, {k_out, reach(a.ys[1], B, H_k, T, d, es), true}};
+  if (!disjoint(r, 9, nullptr, nullptr)) return VLA_ERR_INVALID_ARG;
+  a.y[0] = q_out; a.y[1] = k_out;
+  return launched(vla::launch_qk_norm_rope(a, d, io_dtype, op.interleaved != 0, static_cast<hipStream_t>(stream)));
+}
+
+int vla_qk_norm_rope_backward(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos,
+                              const float* sin, const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight,
+                              float* dk_weight, int B, int T, int H_q, int H_k, int d, int io_dtype, const vla_norm_opts* opts,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  vla_norm_opts op;
+  vla::NormArgs a;
+  const int st = norm_args(q, k, q_weight, k_weight, cos, sin, B, T, H_q, H_k, d, io_dtype, opts, &op, &a);
+  if (st != VLA_OK) return st;
+  const int per16 = io_dtype == VLA_BF16 ? 8 : 4;
+  if (!rows_of(op.dq, H_q, T, d, per16, &a.dxs[0]) || !rows_of(op.dk, H_k, T, d, per16, &a.dxs[1])) return VLA_ERR_INVALID_ARG;
+  if (T > 0 && ((H_q > 0 && (dq_out == nullptr || dq == nullptr)) || (H_k > 0 && (dk_out == nullptr || dk == nullptr)))) return VLA_ERR_INVALID_ARG;
+  const void* ptrs[] = {dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace};
+  for (const void* p : ptrs) {
+    if (!aligned16(p)) return VLA_ERR_INVALID_ARG;
+  }
+  if (!rows_apart(a.dxs[0], B, H_q, T, d) || !rows_apart(a.dxs[1], B, H_k, T, d)) return VLA_ERR_INVALID_ARG;
+  const bool sums = dq_weight != nullptr || dk_weight != nullptr;
+  const size_t need = vla_qk_norm_rope_workspace_bytes(d);
+  if (sums && (workspace == nullptr || workspace_bytes < need)) return VLA_ERR_WORKSPACE;
+  const size_t es = io_dtype == VLA_BF16 ? 2 : 4, ws = op.weight_dtype == VLA_BF16 ? 2 : 4, table = static_cast<size_t>(op.places) * (a.rot / 2) * 4;
+  const size_t nq = reach(a.xs[0], B, H_q, T, d, es), nk = reach(a.xs[1], B, H_k, T, d, es);
+  const Range r[] = {{q, nq, false}, {k, nk, false}, {q_weight, d * ws, false}, {k_weight, d * ws, false},
+                     {a.rot ? cos : nullptr, table, false}, {a.rot ? sin : nullptr, table, false},
+                     {a.positions, static_cast<size_t>(B) * T * 4, false},
+                     {dq_out, reach(a.ys[0], B, H_q, T, d, es), false}, {dk_out, reach(a.ys[1], B, H_k, T, d, es), false},
+                     {dq, reach(a.dxs[0], B, H_q, T, d, es), true}, {dk, reach(a.dxs[1], B, H_k, T, d, es), true},
+                     {dq_weight, static_cast<size_t>(d) * 4, true}, {dk_weight, static_cast<size_t>(d) * 4, true},
+                     {sums ? workspace : nullptr, need, true}};
+  if (!disjoint(r, 14, nullptr, nullptr)) return VLA_ERR_INVALID_ARG;
+  a.dy[0] = dq_out; a.dy[1] = dk_out; a.dx[0] = dq; a.dx[1] = dk;
+  a.dw[0] = dq_weight; a.dw[1] = dk_weight;
+  a.dw_part = sums ? static_cast<float*>(workspace) : nullptr;
+  if (T == 0 && !sums) return VLA_OK;
+  return launched(vla::launch_qk_norm_rope_backward(a, d, io_dtype, op.interleaved != 0, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,55 @@
+// Internal declarations of the operators around the recurrence: the gated delta rule and the norm of queries and keys with
+// the position rotation (gfx950 only).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace vla {
+
+// Element strides of a [B, H, T, d] tensor whose last dimension is contiguous.
+struct Rows {
+  long long b, h, t;
+};
+
+struct NormArgs {
+  const void* x[2];        // queries, keys: [B, H, T, d] by strides
+  const void* w[2];        // [d] or nullptr (ones)
+  const float* cos;        // [places][rot / 2]
+  const float* sin;
+  const int* positions;    // [B][T] or nullptr: offset + t
+  void* y[2];              // forward
+  const void* dy[2];       // backward
+  void* dx[2];
+  float* dw_part;          // [workgroups][2][d]
+  float* dw[2];            // [d] or nullptr
+  Rows xs[2], ys[2], dxs[2];
+  int H[2];
+  int B, T, rot, places, offset;
+  float eps, inv_n;        // 1 / d (RMS) or 1 (L2)
+  int w_bf16;
+};
+constexpr int kNormPartials = 1024;   // workgroups of the backward pass at most: rows of dw_part
+hipError_t launch_qk_norm_rope(const NormArgs& a, int d, int io_dtype, bool interleaved, hipStream_t stream);
+hipError_t launch_qk_norm_rope_backward(const NormArgs& a, int d, int io_dtype, bool interleaved, hipStream_t stream);
+
+struct DeltaArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  const float* g;
+  const float* beta;
+  const float* S0;
+  void* o;
+  float* S_T;
+  const int* lengths;      // [B] or nullptr: T
+  Rows qs, ks, vs, os, gs, bs;
+  int B, H_k, H_v, T;
+  float scale;
+};
+// Token by token, the rows of the state on registers (delta_step.hip): single tokens and short sequences.
+hipError_t launch_delta_step(const DeltaArgs& a, int d_k, int d_v, int io_dtype, hipStream_t stream);
+
+inline bool layer_head_size(int d) { return d == 16 || d == 32 || d == 64 || d == 96 || d == 128; }
+
+}  // namespace vla

@@ -1,0 +1,173 @@
+"""The gated delta rule on torch tensors (vla_delta_forward, vla_delta_decode_step and vla_delta_backward of include/vla.h)."""
+import ctypes
+
+from . import binding
+from .binding import VlaDeltaOpts, VlaError
+from .qk_norm import _io, _like, _p, _rows, _steps, _strides
+
+
+def _gate(x):
+    return x if any(_steps(x)) else x.contiguous()
+
+
+def _check(torch, q, k, v, g, beta, state, lengths, tokens):
+    """Shapes of a call over tokens (tokens 1) or of one token (0); state: (name, tensor or None) pairs."""
+    if not (q.is_cuda and k.is_cuda and v.is_cuda):
+        raise ValueError("q, k, v must be GPU tensors (no CPU path exists)")
+    dev = q.device
+    if k.dtype != q.dtype or v.dtype != q.dtype or k.device != dev or v.device != dev:
+        raise ValueError("q, k, v must share a dtype and a device")
+    names = "[B,H,T,d]" if tokens else "[B,H,d]"
+    if q.dim() != 3 + tokens or k.shape != q.shape or v.dim() != q.dim() or v.shape[0] != q.shape[0] or v.shape[2:-1] != q.shape[2:-1]:
+        raise ValueError(f"expected q, k and v as {names} with one batch and length, q and k of one shape")
+    H_k, H_v = q.shape[1], v.shape[1]
+    if H_k < 1 or H_v % H_k:
+        raise ValueError(f"the value heads ({H_v}) must be a multiple of the key heads ({H_k})")
+    for name, x in (("g", g), ("beta", beta)):
+        if x.dtype != torch.float32 or x.shape != v.shape[:-1] or x.device != dev:
+            raise ValueError(f"{name} must be a float32 tensor of shape {tuple(v.shape[:-1])} on {dev}")
+    shape = (q.shape[0], H_v, v.shape[-1], q.shape[-1])
+    for name, S in state:
+        if S is not None and (S.dtype != torch.float32 or S.shape != shape or not S.is_contiguous() or S.device != dev):
+            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {shape} on {dev}")
+    if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != q.shape[:1] or lengths.device != dev):
+        raise ValueError(f"lengths must be an int32 tensor of shape {tuple(q.shape[:1])} on {dev}")
+
+
+def _inputs(q, k, v, g, beta, scale, lengths, segments=0):
+    """The inputs as the kernels take them, kept until the call, and its options."""
+    q, k, v, g, beta = _rows(q), _rows(k), _rows(v), _gate(g), _gate(beta)
+    lengths = None if lengths is None else lengths.contiguous()
+    op = VlaDeltaOpts(scale=scale or 0.0, lengths=_p(lengths), segments=segments)
+    op.q, op.k, op.v, op.g, op.beta = (_strides(x) for x in (q, k, v, g, beta))
+    return (q, k, v, g, beta, lengths), op
+
+
+def gated_delta_forward(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, save_for_backward=False, segments=0, stream=None):
+    """S' = exp(g_t) S;  S <- S' + beta_t (v_t - S' k_t) k_t^T;  o_t = scale S q_t  for every value head.
+
+    q, k [B,H_k,T,d_k], v [B,H_v,T,d_v] on the GPU (float32 or bfloat16; views with a contiguous last dimension are read as they are),
+    g (logarithm of the decay) and beta [B,H_v,T] float32, S0 [B,H_v,d_v,d_k] float32 or None (zero).  Value head h reads key head
+    h // (H_v // H_k).  scale: default 1 / sqrt(d_k).  lengths: int32 [B], tokens of each sequence; o is zero beyond.
+    Returns (o, S_T), o with v's order of dimensions, and with save_for_backward also what gated_delta_backward needs.
+    Workspace, outputs and work are on `stream` (default: torch's current one).
+    """
+    import torch
+
+    _check(torch, q, k, v, g, beta, (("S0", S0),), lengths, 1)
+    io, (B, H_k, T, dk), H_v, dv, dev = _io(torch, q), q.shape, v.shape[1], v.shape[-1], q.device
+    lib = binding.load_library()
+    handle, context, outside = binding._on_stream(torch, dev, stream)
+    with context:
+        kept, op = _inputs(q, k, v, g, beta, scale, lengths, segments)
+        o = _like(torch, v)
+        op.o = _strides(o)
+        S_T = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
+        saved = None
+        if save_for_backward:
+            op.saved_bytes = lib.vla_delta_saved_bytes(B, H_v, T, dk, dv, io)
+            saved = torch.empty((max(op.saved_bytes, 16),), dtype=torch.uint8, device=dev)
+            op.saved = saved.data_ptr()
+        need = lib.vla_delta_workspace_bytes(B, H_k, H_v, T, dk, dv, io, ctypes.byref(op), 0)
+        ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
+        if outside is not None:
+            for t in (o, S_T, saved):
+                if t is not None:
+                    t.record_stream(outside)
+        rc = lib.vla_delta_forward(*(_p(x) for x in kept[:5]), _p(S0), _p(o), _p(S_T), B, H_k, H_v, T, dk, dv, io, ctypes.byref(op),
+                                   _p(ws), need, handle)
+    if rc != 0:
+        raise VlaError(rc, binding.status_string(rc), "vla_delta_forward")
+    return (o, S_T, saved) if save_for_backward else (o, S_T)
+
+
+def gated_delta_decode_step(q, k, v, g, beta, S, *, scale=None, stream=None):
+    """One token for every head: q, k [B,H_k,d_k], v [B,H_v,d_v], g, beta [B,H_v] float32; S [B,H_v,d_v,d_k] float32 is updated in
+    place.  Returns o [B,H_v,d_v]."""
+    import torch
+
+    _check(torch, q, k, v, g, beta, (("S", S),), None, 0)
+    io, (B, H_k, dk), H_v, dv, dev = _io(torch, q), q.shape, v.shape[1], v.shape[-1], q.device
+    lib = binding.load_library()
+    handle, context, outside = binding._on_stream(torch, dev, stream)
+    with context:
+        q, k, v, g, beta = q.contiguous(), k.contiguous(), v.contiguous(), g.contiguous(), beta.contiguous()
+        o = torch.empty_like(v)
+        if outside is not None:
+            o.record_stream(outside)
+        op = VlaDeltaOpts(scale=scale or 0.0)
+        rc = lib.vla_delta_decode_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), S.data_ptr(),
+                                       o.data_ptr(), B, H_k, H_v, dk, dv, io, ctypes.byref(op), handle)
+    if rc != 0:
+        raise VlaError(rc, binding.status_string(rc), "vla_delta_decode_step")
+    return o
+
+
+def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, lengths=None, stream=None):
+    """The gradients (dq, dk, dv, dg, dbeta, dS0) of gated_delta_forward's inputs, given those of o and S_T (None: zero), the same inputs
+    and what it saved.  dg, dbeta and dS0 are float32."""
+    import torch
+
+    _check(torch, q, k, v, g, beta, (("dS_T", dS_T),), lengths, 1)
+    if do.shape != v.shape or do.dtype != v.dtype or do.device != v.device:
+        raise ValueError("do must match v in shape, dtype and device")
+    io, (B, H_k, T, dk), H_v, dv, dev = _io(torch, q), q.shape, v.shape[1], v.shape[-1], q.device
+    lib = binding.load_library()
+    handle, context, outside = binding._on_stream(torch, dev, stream)
+    with context:
+        kept, op = _inputs(q, k, v, g, beta, scale, lengths)
+        do = _rows(do)
+        dq, dk_, dv_ = _like(torch, q), _like(torch, k), _like(torch, v)
+        dg, dbeta = (torch.empty((B, H_v, T), dtype=torch.float32, device=dev) for _ in range(2))
+        dS0 = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
+        op.o, op.dq, op.dk, op.dv = (_strides(x) for x in (do, dq, dk_, dv_))
+        op.saved, op.saved_bytes = saved.data_ptr(), saved.numel()
+        need = lib.vla_delta_workspace_bytes(B, H_k, H_v, T, dk, dv, io, ctypes.byref(op), 1)
+        ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
+        outputs = (dq, dk_, dv_, dg, dbeta, dS0)
+        if outside is not None:
+            for t in outputs:
+                t.record_stream(outside)
+        rc = lib.vla_delta_backward(*(_p(x) for x in kept[:5]), _p(do), _p(dS_T), *(_p(x) for x in outputs), B, H_k, H_v, T, dk, dv, io,
+                                    ctypes.byref(op), _p(ws), need, handle)
+    if rc != 0:
+        raise VlaError(rc, binding.status_string(rc), "vla_delta_backward")
+    return outputs
+
+
+_function = None
+
+
+def _autograd():
+    global _function
+    if _function is None:
+        import torch
+
+        class GatedDelta(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, q, k, v, g, beta, S0, scale, lengths):
+                o, S_T, saved = gated_delta_forward(q, k, v, g, beta, S0, scale=scale, lengths=lengths, save_for_backward=True)
+                ctx.save_for_backward(q, k, v, g, beta, saved, lengths)
+                ctx.scale, ctx.has_state = scale, S0 is not None
+                return o, S_T
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, do, dS_T):
+                q, k, v, g, beta, saved, lengths = ctx.saved_tensors
+                grads = gated_delta_backward(q, k, v, g, beta, saved, do, dS_T.contiguous(), scale=ctx.scale, lengths=lengths)
+                return (*grads[:5], grads[5] if ctx.has_state else None, None, None)
+
+        _function = GatedDelta
+    return _function
+
+
+def gated_delta(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, stream=None):
+    """gated_delta_forward as a differentiable function: (o, S_T), with gradients for q, k, v, g, beta and S0 (on the current stream)."""
+    import torch
+
+    if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in (q, k, v, g, beta, S0)):
+        if stream is not None:
+            raise ValueError("with gradients the work goes to the current stream: leave stream at None")
+        return _autograd().apply(q, k, v, g, beta, S0, scale, lengths)
+    return gated_delta_forward(q, k, v, g, beta, S0, scale=scale, lengths=lengths, stream=stream)
