@@ -1,0 +1,8 @@
+// The block form of the gated delta rule for key heads of 64 (delta_chunk.h).
+#include "delta_chunk.h"
+
+namespace vla {
+hipError_t launch_delta_chunk_64(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream) {
+  return delta::launch_chunk_dk<64>(a, d_v, io_dtype, map, stream);
+}
+}  // namespace vla

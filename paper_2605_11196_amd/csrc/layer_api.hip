@@ -98,6 +98,17 @@ bool gate_rows(const vla_strides& s, long long H, long long T, vla::Rows* out) {
   return out->b >= 0 && out->h >= 0 && out->t >= 0;
 }
 
+hipError_t launch_blocks(const vla::DeltaArgs& a, int d_k, int d_v, int io_dtype, bool map, hipStream_t stream) {
+  switch (d_k) {
+    case 16: return vla::launch_delta_chunk_16(a, d_v, io_dtype, map, stream);
+    case 32: return vla::launch_delta_chunk_32(a, d_v, io_dtype, map, stream);
+    case 64: return vla::launch_delta_chunk_64(a, d_v, io_dtype, map, stream);
+    case 96: return vla::launch_delta_chunk_96(a, d_v, io_dtype, map, stream);
+    case 128: return vla::launch_delta_chunk_128(a, d_v, io_dtype, map, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+
 }  // namespace
 
 extern "C" {
@@ -119,7 +130,6 @@ int vla_delta_backward(const void* q, const void* k, const void* v, const float*
 int vla_delta_forward(const void* q, const void* k, const void* v, const float* g, const float* beta, const float* S0, void* o,
                       float* S_T, int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts,
                       void* workspace, size_t workspace_bytes, void* stream) {
-  (void)workspace; (void)workspace_bytes;
   const vla_delta_opts op = delta_opts(opts, d_k);
   const int st = check_delta(B, H_k, H_v, T, d_k, d_v, io_dtype, op);
   if (st != VLA_OK) return st;
@@ -147,7 +157,12 @@ int vla_delta_forward(const void* q, const void* k, const void* v, const float* 
   a.lengths = op.lengths;
   a.B = B; a.H_k = H_k; a.H_v = H_v; a.T = T;
   a.scale = op.scale;
-  return launched(vla::launch_delta_step(a, d_k, d_v, io_dtype, static_cast<hipStream_t>(stream)));
+  a.n_blocks = (T + 31) / 32;
+  a.n_seg = 1;
+  a.seg_tokens = T;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (T < 16) return launched(vla::launch_delta_step(a, d_k, d_v, io_dtype, s));
+  return launched(launch_blocks(a, d_k, d_v, io_dtype, false, s));
 }
 
 int vla_delta_decode_step(const void* q, const void* k, const void* v, const float* g, const float* beta, float* S, void* o, int B,

@@ -46,9 +46,22 @@ struct DeltaArgs {
   Rows qs, ks, vs, os, gs, bs;
   int B, H_k, H_v, T;
   float scale;
+  float* saved;            // [B * H_v][n_blocks][d_v][d_k] or nullptr: the state at the start of every block of 32 tokens
+  int n_blocks;
+  // time segments
+  int n_seg, seg_tokens;
+  bool seg_states;         // S0 holds a state for each segment: [B * H_v][n_seg][d_v][d_k]
+  float* seg_map;          // [B * H_v][n_seg][d_v + d_k][d_k]: the segments' affine maps, Y then X
 };
 // Token by token, the rows of the state on registers (delta_step.hip): single tokens and short sequences.
 hipError_t launch_delta_step(const DeltaArgs& a, int d_k, int d_v, int io_dtype, hipStream_t stream);
+
+// In blocks of 32 tokens (delta_chunk.h); map: the affine maps of the segments instead of outputs.
+hipError_t launch_delta_chunk_16(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
+hipError_t launch_delta_chunk_32(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
+hipError_t launch_delta_chunk_64(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
+hipError_t launch_delta_chunk_96(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
+hipError_t launch_delta_chunk_128(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
 
 inline bool layer_head_size(int d) { return d == 16 || d == 32 || d == 64 || d == 96 || d == 128; }
 
