@@ -239,7 +239,8 @@ int vla_resolve_mode(int B, int H, int T, int d_k, int d_v, int io_dtype, const 
 
 /* Element strides of a [B, H, T, d] (gates: [B, H, T]) tensor.  All zero: contiguous.  The last dimension of d elements is always
  * contiguous; strides of q, k, v, o and of their gradients are multiples of 16 bytes (of the gates: any), none is negative,
- * and a written tensor's rows do not overlap.  A read tensor may repeat rows (stride 0), but not by three zeros. */
+ * and a written tensor's rows do not overlap.  A read tensor may repeat its rows over b and h (stride 0), a gate also over t, but not
+ * by three zeros; for the gated delta rule its tokens are less than 2^31 / 32 bytes apart. */
 typedef struct vla_strides {
   long long b, h, t;
 } vla_strides;

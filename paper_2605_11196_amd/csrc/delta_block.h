@@ -63,7 +63,10 @@ template <> struct Ops<uint16_t> {
   using TB = TokB;
   template <class R> static __device__ __forceinline__ A rows(const u4* m, int row, int j, int g) { return m[R::at(row, 4 * j + g)]; }
   static __device__ __forceinline__ f4 mul_rows(A a, A b, f4 acc) { return mfma_bf16(a, b, acc); }
-  static __device__ __forceinline__ B pair(f4 x0, f4 x1) { return split_tiles(x0, x1); }
+  // terms of float32 tiles; the residuals come from the matrix unit, 6 vector and 2 matrix instructions a tile for 22 vector ones
+  using One = u2;
+  static __device__ __forceinline__ One one(int c, int g) { return minus_identity(c, g); }
+  static __device__ __forceinline__ B pair(f4 x0, f4 x1, One one) { return split_tiles(x0, x1, one); }
   static __device__ __forceinline__ f4 mul(A a, const B& b, f4 acc) { return mfma_terms(Terms<1>{{a}}, b, acc); }
   // without the lowest term: for results that are rounded to bf16
   static __device__ __forceinline__ f4 mul_out(A a, const B& b, f4 acc) { return mfma_bf16(a, b.t[0], mfma_bf16(a, b.t[1], acc)); }
@@ -79,7 +82,11 @@ template <> struct Ops<uint16_t> {
   template <class R> static __device__ __forceinline__ f4 tile(const u4* m, int n, int t, int c, int g) { return widen4(tile_raw<R>(m, n, t, c, g)); }
   static __device__ __forceinline__ void put(Image& im, int row, int g, f4 x) { tok_store(im.hm, im.l, row, row, g, x); }
   static __device__ __forceinline__ TA image(const Image& im, int c, int g) { return tok_load(im.hm, im.l, c, c, g); }
-  static __device__ __forceinline__ TB tokens(f4 x) { return tok_b(x); }
+  static __device__ __forceinline__ TB tokens(f4 x, One one) {
+    u2 h, m, l;
+    split3_cut_matrix(x, one, h, m, l);
+    return TokB{cat(h, m), cat(m, h), cat(h, l)};
+  }
   static __device__ __forceinline__ f4 mul_tok(const TA& a, const TB& b, f4 acc) { return mfma_tok(a, b, acc); }
   static __device__ __forceinline__ f4 mul_tok_out(const TA& a, const TB& b, f4 acc) {
     return mfma_bf16(a.hm, b.hm, mfma_bf16(a.hm, b.mh, acc));
@@ -103,7 +110,9 @@ template <> struct Ops<float> {
     return A{__builtin_bit_cast(f4, m[R::at(row, 8 * j + 2 * g)]), __builtin_bit_cast(f4, m[R::at(row, 8 * j + 2 * g + 1)])};
   }
   static __device__ __forceinline__ f4 mul_rows(const A& a, const A& b, f4 acc) { return mul4(a.x1, b.x1, mul4(a.x0, b.x0, acc)); }
-  static __device__ __forceinline__ B pair(f4 x0, f4 x1) { return B{x0, x1}; }
+  struct One {};
+  static __device__ __forceinline__ One one(int, int) { return One{}; }
+  static __device__ __forceinline__ B pair(f4 x0, f4 x1, One) { return B{x0, x1}; }
   static __device__ __forceinline__ f4 mul(const A& a, const B& b, f4 acc) { return mul4(a.x1, b.x1, mul4(a.x0, b.x0, acc)); }
   static __device__ __forceinline__ f4 mul_out(const A& a, const B& b, f4 acc) { return mul(a, b, acc); }
   static __device__ __forceinline__ float value(const u4* m, int piece_at, int i) { return reinterpret_cast<const float*>(m + piece_at)[i]; }
@@ -126,10 +135,17 @@ template <> struct Ops<float> {
   template <class R> static __device__ __forceinline__ f4 tile_raw(const u4* m, int n, int t, int c, int g) { return tile<R>(m, n, t, c, g); }
   static __device__ __forceinline__ void put(Image& im, int row, int g, f4 x) { im.x[4 * row + tok_chunk(row, g)] = x; }
   static __device__ __forceinline__ TA image(const Image& im, int c, int g) { return im.x[4 * c + tok_chunk(c, g)]; }
-  static __device__ __forceinline__ TB tokens(f4 x) { return x; }
+  static __device__ __forceinline__ TB tokens(f4 x, One) { return x; }
   static __device__ __forceinline__ f4 mul_tok(const TA& a, const TB& b, f4 acc) { return mul4(a, b, acc); }
   static __device__ __forceinline__ f4 mul_tok_out(const TA& a, const TB& b, f4 acc) { return mul4(a, b, acc); }
 };
+
+// Rows of memory as a buffer whose bounds the hardware checks: loads past the last row give zeros, stores past it are dropped, so that
+// the last block needs no branches.  Rows are at most 2^31 / 32 bytes apart (checked on the host) and do not overlap.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const void* base, long long step_bytes, int rows, int row_bytes) {
+  const int bytes = rows <= 0 ? 0 : static_cast<int>((min(rows, kTok) - 1) * step_bytes) + row_bytes;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
+}
 
 // A block's rows on their way from memory to LDS: N pieces a thread.
 template <int PIECES, int THREADS>
@@ -137,27 +153,43 @@ struct Stage {
   static constexpr int ALL = kTok * PIECES;
   static constexpr int N = (ALL + THREADS - 1) / THREADS;
   u4 x[N];
-  // rows t0 .. t0 + 31 from base, `pieces` 16-byte pieces of each at element stride `step`; zeros from row `end` on
-  template <typename IO>
-  __device__ __forceinline__ void load(const IO* base, long long step, int t0, int end) {
+  int at[N];   // byte offset of each piece from the block's first row
+  __device__ __forceinline__ void init(long long step_bytes) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int at = threadIdx.x + i * THREADS, row = at / PIECES, piece = at % PIECES;
-      x[i] = u4{0, 0, 0, 0};
-      if ((ALL % THREADS == 0 || at < ALL) && t0 + row < end) {
-        x[i] = *reinterpret_cast<const u4*>(base + (t0 + row) * step + piece * Ops<IO>::PER16);
-      }
+      const int p = threadIdx.x + i * THREADS;
+      at[i] = p < ALL ? p / PIECES * static_cast<int>(step_bytes) + p % PIECES * 16 : 0x7fffffff;
     }
+  }
+  // rows t0 .. t0 + 31 of base; zeros from row `end` on
+  __device__ __forceinline__ void load(const char* base, long long step_bytes, int t0, int end) {
+    const __amdgpu_buffer_rsrc_t r = rows_buffer(base + t0 * step_bytes, step_bytes, end - t0, PIECES * 16);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, at[i], 0, 0);
   }
   template <class R>
   __device__ __forceinline__ void store(u4* m) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int at = threadIdx.x + i * THREADS;
-      if (ALL % THREADS == 0 || at < ALL) m[R::at(at / PIECES, at % PIECES)] = x[i];
+      const int p = threadIdx.x + i * THREADS;
+      if (ALL % THREADS == 0 || p < ALL) m[R::at(p / PIECES, p % PIECES)] = x[i];
     }
   }
 };
+
+// four tokens' values of one column, at the byte offset of the first; rows past the end are dropped
+__device__ __forceinline__ void store_column(__amdgpu_buffer_rsrc_t r, int at, int step_bytes, f4 x, float*) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[i]), r, at + i * step_bytes, 0, 0);
+}
+__device__ __forceinline__ void store_column(__amdgpu_buffer_rsrc_t r, int at, int step_bytes, f4 x, uint16_t*) {
+#pragma unroll
+  for (int i = 0; i < 4; i += 2) {
+    const uint32_t two = pack_rne(x[i], x[i + 1]);
+    __builtin_amdgcn_raw_buffer_store_b16(static_cast<uint16_t>(two), r, at + i * step_bytes, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b16(static_cast<uint16_t>(two >> 16), r, at + (i + 1) * step_bytes, 0, 0);
+  }
+}
 
 // The decays of a block.  G is summed in float64 and kept as a float32 pair, in units of log 2: differences stay exact to some 2^-24
 // however far G runs, as it does after a token that forgets the state (g is held at -10000, whose exponential is 0 all the same).
@@ -172,15 +204,30 @@ __device__ __forceinline__ float exp2_of(double x) {
   const float hi = static_cast<float>(x);
   return exp2f(hi) * fmaf(0.69314718f, static_cast<float>(x - static_cast<double>(hi)), 1.0f);
 }
-// by the first wave; g and beta of token `lane` (0 past the end of the sequence)
+// x of lane l - N of the same 16 lanes, 0 where there is none
+template <int N>
+__device__ __forceinline__ double shifted_up(double x) {
+  const uint2 b = __builtin_bit_cast(uint2, x);
+  const uint2 s = {static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b.x), 0x110 + N, 0xf, 0xf, true)),
+                   static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b.y), 0x110 + N, 0xf, 0xf, true))};
+  return __builtin_bit_cast(double, s);
+}
+__device__ __forceinline__ double of_lane(double x, int lane) {
+  const uint2 b = __builtin_bit_cast(uint2, x);
+  return __builtin_bit_cast(double, uint2{static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(b.x), lane)),
+                                          static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(b.y), lane))});
+}
+// by one wave; g and beta of token `lane` (0 past the end of the sequence)
 __device__ __forceinline__ void put_gates(Gates& s, int lane, float g, float beta) {
+  static_assert(kTok == 32, "two rows of lanes");
   double G = static_cast<double>(g < -10000.0f ? -10000.0f : g) * 1.4426950408889634;
-#pragma unroll
-  for (int d = 1; d < kTok; d *= 2) {
-    const double other = __shfl_up(G, d, 64);
-    if (lane >= d) G += other;
-  }
-  const double all = __shfl(G, kTok - 1, 64);
+  G += shifted_up<1>(G);
+  G += shifted_up<2>(G);
+  G += shifted_up<4>(G);
+  G += shifted_up<8>(G);
+  const double first = of_lane(G, 15);
+  if (lane >= 16) G += first;
+  const double all = of_lane(G, kTok - 1);
   if (lane < kTok) {
     const float hi = static_cast<float>(G);
     s.hi[lane] = hi;
@@ -192,27 +239,45 @@ __device__ __forceinline__ void put_gates(Gates& s, int lane, float g, float bet
   }
 }
 
-// (I + M)^-1 of one 16 x 16 tile: `m` holds -M transposed ([column][row], stride 20); lanes 0 to 15 hold a row of the inverse each and go
-// from its last column to the first: t_j = e_j - sum_{k > j} t_k M_kj.
-template <typename IO>
-__device__ __forceinline__ void invert_tile(const float* m, typename Ops<IO>::Image& out, int lane) {
-  if (lane >= 16) return;
-  float t[16];
-#pragma unroll
-  for (int j = 15; j >= 0; --j) {
-    float s = j == lane ? 1.0f : 0.0f;
-#pragma unroll
-    for (int q = j / 4; q < 4; ++q) {
-      const f4 row = *reinterpret_cast<const f4*>(m + 20 * j + 4 * q);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (4 * q + i > j) s = fmaf(t[4 * q + i], row[i], s);
-      }
+// (I + M)^-1 of one 16 x 16 tile.  x: -M, four columns 4 g + r of row c a lane; m: scratch of 16 rows at stride 20.  Each 16 lanes hold the
+// rows of the inverse, one a lane, and go from its last column to the first, t_j = e_j - sum_{k > j} t_k M_kj: what multiplies t_k is a
+// register of lane k, broadcast inside the multiplication (DPP), 120 of them, without LDS in the chain.
+template <int K, int J>
+struct SubstituteColumn {
+  static __device__ __forceinline__ void run(float (&t)[16], const float (&m)[16]) {
+    if constexpr (J >= 0) {
+      fmac_row_bcast<K>(t[J], m[J], t[K]);
+      SubstituteColumn<K, J - 1>::run(t, m);
     }
-    t[j] = s;
   }
+};
+template <int K>
+__device__ __forceinline__ void substitute(float (&t)[16], const float (&m)[16]) {
+  if constexpr (K > 0) {
+    SubstituteColumn<K, K - 1>::run(t, m);
+    substitute<K - 1>(t, m);
+  }
+}
+template <typename IO>
+__device__ __forceinline__ void invert_tile(f4 x, float* m, typename Ops<IO>::Image& out, int c, int g) {
+  *reinterpret_cast<f4*>(m + 20 * c + 4 * g) = x;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  float row[16], t[16];
 #pragma unroll
-  for (int g = 0; g < 4; ++g) Ops<IO>::put(out, lane, g, f4{t[4 * g], t[4 * g + 1], t[4 * g + 2], t[4 * g + 3]});
+  for (int j = 0; j < 16; j += 4) {
+    const f4 y = *reinterpret_cast<const f4*>(m + 20 * c + j);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      row[j + i] = y[i];
+      t[j + i] = j + i == c ? 1.0f : 0.0f;
+    }
+  }
+  substitute<15>(t, row);
+  f4 mine;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) mine[r] = g < 2 ? (g == 0 ? t[r] : t[4 + r]) : (g == 2 ? t[8 + r] : t[12 + r]);
+  Ops<IO>::put(out, c, g, mine);
 }
 
 }  // namespace delta

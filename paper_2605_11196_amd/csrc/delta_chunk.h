@@ -37,18 +37,21 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
   __shared__ u4 sV[kTok * RV::STRIDE];
   __shared__ typename O::Image inverse[kTiles], below[kTiles * (kTiles - 1) / 2], att[MAP ? 1 : kTiles * (kTiles + 1) / 2];
   __shared__ __align__(16) float diagonal[kTiles][16 * 20];
-  __shared__ Gates gates;
+  __shared__ Gates gate_pair[2];
 
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
   const int head = blockIdx.x / a.n_seg, seg = blockIdx.x % a.n_seg;
   const int b = head / a.H_v, h = head % a.H_v, hk = h / (a.H_v / a.H_k);
-  const int len = a.lengths ? max(0, min(a.lengths[b], a.T)) : a.T;
+  const int len = __builtin_amdgcn_readfirstlane(a.lengths ? max(0, min(a.lengths[b], a.T)) : a.T);
   const int first = seg * a.seg_tokens, last = min(a.T, first + a.seg_tokens), end = min(len, last);
-  const IO* q = static_cast<const IO*>(a.q) + b * a.qs.b + hk * a.qs.h;
-  const IO* k = static_cast<const IO*>(a.k) + b * a.ks.b + hk * a.ks.h;
-  const IO* v = static_cast<const IO*>(a.v) + b * a.vs.b + h * a.vs.h;
+  const char* q = reinterpret_cast<const char*>(static_cast<const IO*>(a.q) + b * a.qs.b + hk * a.qs.h);
+  const char* k = reinterpret_cast<const char*>(static_cast<const IO*>(a.k) + b * a.ks.b + hk * a.ks.h);
+  const char* v = reinterpret_cast<const char*>(static_cast<const IO*>(a.v) + b * a.vs.b + h * a.vs.h);
+  char* o = MAP ? nullptr : reinterpret_cast<char*>(static_cast<IO*>(a.o) + b * a.os.b + h * a.os.h);
+  const long long q_step = a.qs.t * sizeof(IO), k_step = a.ks.t * sizeof(IO), v_step = a.vs.t * sizeof(IO), o_step = a.os.t * sizeof(IO);
   const float* gp = a.g + b * a.gs.b + h * a.gs.h;
   const float* bp = a.beta + b * a.bs.b + h * a.bs.h;
+  const typename O::One one = O::one(c, g);
   const int col0 = wave * 16 * NT + c;      // first column of this lane
 
   // ---- the state: tile kt holds key columns 32 (kt / 2) + 8 g + 4 (kt % 2) + r
@@ -79,18 +82,30 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
 
   Stage<PK, THREADS> stK, stQ;
   Stage<PV, THREADS> stV;
-  float gate = 0.0f, beta = 0.0f;
+  stK.init(k_step);
+  if constexpr (!MAP) stQ.init(q_step);
+  stV.init(v_step);
+  float gate = 0.0f, beta = 0.0f;   // of one token a lane, a block ahead of the rows
   auto request = [&](int t0) {
-    stK.load(k, a.ks.t, t0, end);
-    if constexpr (!MAP) stQ.load(q, a.qs.t, t0, end);
-    stV.load(v, a.vs.t, t0, end);
-    if (wave == 0) {
-      const bool live = lane < kTok && t0 + lane < end;
-      gate = live ? gp[(t0 + lane) * a.gs.t] : 0.0f;
-      beta = live ? bp[(t0 + lane) * a.bs.t] : 0.0f;
-    }
+    stK.load(k, k_step, t0, end);
+    if constexpr (!MAP) stQ.load(q, q_step, t0, end);
+    stV.load(v, v_step, t0, end);
   };
-  if (first < end) request(first);
+  auto request_gates = [&](int t0) {
+    const int t = min(t0 + (lane & (kTok - 1)), end - 1);
+    gate = gp[t * a.gs.t];
+    beta = bp[t * a.bs.t];
+  };
+  auto next_gates = [&](int t0, Gates& to) {
+    if (wave == WAVES - 1) put_gates(to, lane, t0 + lane < end ? gate : 0.0f, t0 + lane < end ? beta : 0.0f);
+  };
+  if (first < end) {
+    request_gates(first);
+    request(first);
+    next_gates(first, gate_pair[0]);
+    request_gates(first + kTok);
+  }
+  int turn = 0;
 
   for (int t0 = first; t0 < end; t0 += kTok) {
     if (!MAP && a.saved != nullptr) {
@@ -107,7 +122,8 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
     stK.template store<RK>(sK);
     if constexpr (!MAP) stQ.template store<RK>(sQ);
     stV.template store<RV>(sV);
-    if (wave == 0) put_gates(gates, lane, gate, beta);
+    const Gates& gates = gate_pair[turn];
+    turn ^= 1;
     __syncthreads();
 
     // ---- matrices between tokens, tile (i, j), j <= i: transposed products, so that a lane has four tokens j of row i = c
@@ -139,10 +155,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
         x[r] = before > 0 ? x[r] * w : 0.0f;
       }
       if (keys && i == j) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) diagonal[i][20 * (4 * g + r) + c] = x[r];
-        __builtin_amdgcn_wave_barrier();
-        invert_tile<IO>(diagonal[i], inverse[i], lane);
+        invert_tile<IO>(x, diagonal[i], inverse[i], c, g);
       } else if (keys) {
         O::put(below[i * (i - 1) / 2 + j], c, g, x);
       } else {
@@ -167,7 +180,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const typename O::B x = O::pair(S[n][2 * s], S[n][2 * s + 1]);
+        const typename O::B x = O::pair(S[n][2 * s], S[n][2 * s + 1], one);
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
           P[n][i] = O::mul(ka[i], x, P[n][i]);
@@ -180,47 +193,68 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
 
     // ---- what is written, the read-out, the state
     const float decay = gates.end;
+    f4 R[NT][kTiles];
+    typename O::TB rb[NT][kTiles];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int col = col0 + 16 * n;
-      f4 R[kTiles];
-      typename O::TB rb[kTiles];
+    for (int i = 0; i < kTiles; ++i) {
+      const f4 gamma = *reinterpret_cast<const f4*>(&gates.gamma[16 * i + 4 * g]);
+      const typename O::TA inv = O::image(inverse[i], c, g);
+      f4 x[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        x[n] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (!MAP || wave * 16 * NT + 16 * n < DV) x[n] = O::template tile<RV>(sV, wave * NT + n, i, c, g);
+        x[n] -= gamma * P[n][i];
+      }
+#pragma unroll
+      for (int j = 0; j < i; ++j) {
+        const typename O::TA m = O::image(below[i * (i - 1) / 2 + j], c, g);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) x[n] = O::mul_tok(m, rb[n][j], x[n]);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        R[n][i] = O::mul_tok(inv, O::tokens(x[n], one), f4{0.0f, 0.0f, 0.0f, 0.0f});
+        if (!MAP || i + 1 < kTiles) rb[n][i] = O::tokens(R[n][i], one);
+      }
+    }
+    typename O::B w[NT];
+    static_assert(kTiles == 2, "one pair of token tiles");
+    {
+      const f4 w0 = *reinterpret_cast<const f4*>(&gates.rest[4 * g]) * *reinterpret_cast<const f4*>(&gates.beta[4 * g]);
+      const f4 w1 = *reinterpret_cast<const f4*>(&gates.rest[16 + 4 * g]) * *reinterpret_cast<const f4*>(&gates.beta[16 + 4 * g]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) w[n] = O::pair(R[n][0] * w0, R[n][1] * w1, one);
+    }
+    if constexpr (!MAP) {
+      const __amdgpu_buffer_rsrc_t out = rows_buffer(o + t0 * o_step, o_step, last - t0, DV * static_cast<int>(sizeof(IO)));
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
-        f4 x = f4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (!MAP || wave * 16 * NT + 16 * n < DV) x = O::template tile<RV>(sV, wave * NT + n, i, c, g);
-        x -= *reinterpret_cast<const f4*>(&gates.gamma[16 * i + 4 * g]) * P[n][i];
+        const f4 gamma = *reinterpret_cast<const f4*>(&gates.gamma[16 * i + 4 * g]) * a.scale;
+        f4 x[NT];
 #pragma unroll
-        for (int j = 0; j < i; ++j) x = O::mul_tok(O::image(below[i * (i - 1) / 2 + j], c, g), rb[j], x);
-        R[i] = O::mul_tok(O::image(inverse[i], c, g), O::tokens(x), f4{0.0f, 0.0f, 0.0f, 0.0f});
-        if (!MAP || i + 1 < kTiles) rb[i] = O::tokens(R[i]);
-      }
-      if constexpr (!MAP) {
+        for (int n = 0; n < NT; ++n) x[n] = gamma * QS[n][i];
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          f4 x = *reinterpret_cast<const f4*>(&gates.gamma[16 * i + 4 * g]) * QS[n][i] * a.scale;
+        for (int j = 0; j <= i; ++j) {
+          const typename O::TA m = O::image(att[i * (i + 1) / 2 + j], c, g);
 #pragma unroll
-          for (int j = 0; j <= i; ++j) x = O::mul_tok_out(O::image(att[i * (i + 1) / 2 + j], c, g), rb[j], x);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int t = t0 + 16 * i + 4 * g + r;
-            if (t < last) io_store(static_cast<IO*>(a.o) + b * a.os.b + h * a.os.h + t * a.os.t + col, x[r]);
-          }
+          for (int n = 0; n < NT; ++n) x[n] = O::mul_tok_out(m, rb[n][j], x[n]);
         }
-      }
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        R[i] *= *reinterpret_cast<const f4*>(&gates.rest[16 * i + 4 * g]) * *reinterpret_cast<const f4*>(&gates.beta[16 * i + 4 * g]);
-      }
-#pragma unroll
-      for (int i = 0; i < kTiles; i += 2) {
-        const typename O::B x = O::pair(R[i], R[i + 1]);
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-          S[n][kt] = O::mul(O::template columns<RK>(sK, kt, i, c, g), x, i == 0 ? S[n][kt] * decay : S[n][kt]);
+        for (int n = 0; n < NT; ++n) {
+          store_column(out, (16 * i + 4 * g) * static_cast<int>(o_step) + (col0 + 16 * n) * static_cast<int>(sizeof(IO)), static_cast<int>(o_step), x[n],
+                       static_cast<IO*>(nullptr));
         }
       }
     }
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      const typename O::A kc = O::template columns<RK>(sK, kt, 0, c, g);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) S[n][kt] = O::mul(kc, w[n], S[n][kt] * decay);
+    }
+    next_gates(t0 + kTok, gate_pair[turn]);
+    request_gates(t0 + 2 * kTok);
     __syncthreads();
   }
 
@@ -228,7 +262,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
   if constexpr (!MAP) {
     const int done = first < end ? first + (end - first + kTok - 1) / kTok * kTok : first;
     for (int t = done + wave; t < last; t += WAVES) {
-      for (int i = lane; i < DV; i += 64) io_store(static_cast<IO*>(a.o) + b * a.os.b + h * a.os.h + t * a.os.t + i, 0.0f);
+      for (int i = lane; i < DV; i += 64) io_store(reinterpret_cast<IO*>(o + t * o_step) + i, 0.0f);
     }
   }
   float* out = nullptr;

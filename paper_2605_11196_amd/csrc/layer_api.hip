@@ -66,6 +66,11 @@ bool rows_apart(const vla::Rows& r, long long B, long long H, long long T, long 
   return true;
 }
 
+// the tokens of a read tensor do not overlap either
+bool tokens_apart(const vla::Rows& r, long long T, long long d) { return T <= 1 || r.t >= d; }
+// the kernels address the rows of a block of 32 tokens with 31-bit byte offsets
+bool rows_near(const vla::Rows& r, size_t es) { return r.t < 0x7fffffffLL / 32 / static_cast<long long>(es); }
+
 int launched(hipError_t err) {
   if (err == hipSuccess) return VLA_OK;
   fprintf(stderr, "libvla: kernel launch failed: %s (%d)\n", hipGetErrorString(err), static_cast<int>(err));
@@ -143,8 +148,11 @@ int vla_delta_forward(const void* q, const void* k, const void* v, const float* 
   vla::DeltaArgs a{};
   if (!rows_of(op.q, H_k, T, d_k, per16, &a.qs) || !rows_of(op.k, H_k, T, d_k, per16, &a.ks) || !rows_of(op.v, H_v, T, d_v, per16, &a.vs) ||
       !rows_of(op.o, H_v, T, d_v, per16, &a.os) || !gate_rows(op.g, H_v, T, &a.gs) || !gate_rows(op.beta, H_v, T, &a.bs) ||
-      !rows_apart(a.os, B, H_v, T, d_v)) {
+      !rows_apart(a.os, B, H_v, T, d_v) || !tokens_apart(a.qs, T, d_k) || !tokens_apart(a.ks, T, d_k) || !tokens_apart(a.vs, T, d_v)) {
     return VLA_ERR_INVALID_ARG;
+  }
+  for (const vla::Rows* r : {&a.qs, &a.ks, &a.vs, &a.os}) {
+    if (!rows_near(*r, es)) return VLA_ERR_UNSUPPORTED;
   }
   const size_t nS = static_cast<size_t>(B) * H_v * d_v * d_k * 4;
   const Range r[] = {{q, reach(a.qs, B, H_k, T, d_k, es), false}, {k, reach(a.ks, B, H_k, T, d_k, es), false},

@@ -20,10 +20,11 @@ def _steps(x):
 
 def _rows(x):
     """x, or a contiguous copy where it is not laid out as the kernels take it: the last dimension together, the other strides
-    multiples of 16 bytes and not all zero for rows that repeat, 16-byte alignment."""
+    multiples of 16 bytes and not all zero for rows that repeat, tokens apart but not too far, 16-byte alignment."""
     per16 = 16 // x.element_size()
     s = _steps(x)
-    fits = x.stride(-1) == 1 and not any(step % per16 for step in s) and (any(s) or x.is_contiguous())
+    fits = (x.stride(-1) == 1 and not any(step % per16 for step in s) and (any(s) or x.is_contiguous())
+            and (x.shape[2] <= 1 or x.shape[-1] <= s[2] < 2 ** 26 // x.element_size()))
     if fits and x.data_ptr() % 16 == 0:
         return x
     return x.clone() if x.is_contiguous() else x.contiguous()
