@@ -11,7 +11,7 @@
 // tokens or key columns along the rows (4 g + r) and d_v along the 16 lanes.  Such a tile is the right operand of the next product as it
 // stands, because the order of the contraction is free: row 4 g + r of the two tiles of a pair is slot r (4 + r) of lane group g.  For a
 // contraction over key columns slot i of group g is column 32 j + 8 g + i, so that rows of K and Q lie in LDS as they lie in memory, in
-// 16-byte pieces whose place in a row is turned by the row (banks).  No value of a wave's columns ever leaves the wave.
+// 16-byte pieces.  No value of a wave's columns ever leaves the wave.
 //
 // Precision.  bf16: K, Q, V and dO are exact operands, the state and the writes three bf16 terms (all 24 bits); matrices between tokens
 // six of nine products of three terms each.  float32: the FP32 matrix instruction.
@@ -28,14 +28,18 @@ constexpr int kTiles = kTok / 16;
 
 __host__ __device__ constexpr int pow2_at_least(int n) { return n <= 1 ? 1 : 2 * pow2_at_least((n + 1) / 2); }
 
-// Rows of 16-byte pieces in LDS, PIECES used of a row.
+// Rows of 16-byte pieces in LDS, a power of two of them, in an order that the row turns, so that the pieces of one place in 16 rows lie in
+// different banks.  Places differ by exclusive or with the place, so that one register holds the address of a lane's row and the
+// places of a tile are constants applied to it.
 template <int PIECES>
 struct PieceRows {
-  static constexpr int STRIDE = pow2_at_least(PIECES < 4 ? 4 : PIECES);
-  static __device__ __forceinline__ int at(int row, int piece) {
-    const int turn = STRIDE >= 16 ? (row & 15) : ((row / (16 / STRIDE)) & (STRIDE - 1));
-    return row * STRIDE + (piece ^ turn);
+  static constexpr int STRIDE = pow2_at_least(PIECES < 2 ? 2 : PIECES);
+  static __device__ __forceinline__ int turn(int row) {   // of the row modulo 16
+    return STRIDE >= 16 ? row & 15 : (row / (16 / STRIDE)) & (STRIDE - 1);
   }
+  static __device__ __forceinline__ int at(int row, int piece) { return row * STRIDE + (piece ^ turn(row)); }
+  // `place` (a constant) has no bits in common with `piece`
+  static __device__ __forceinline__ int at(int tile, int row, int piece, int place) { return (at(row, piece) ^ place) + 16 * tile * STRIDE; }
 };
 
 typedef short s4v __attribute__((ext_vector_type(4)));
@@ -61,7 +65,8 @@ template <> struct Ops<uint16_t> {
   struct Image { u4 hm[64]; u2 l[64]; };     // a 16 x 16 matrix between tokens as a left operand
   using TA = TokA;
   using TB = TokB;
-  template <class R> static __device__ __forceinline__ A rows(const u4* m, int row, int j, int g) { return m[R::at(row, 4 * j + g)]; }
+  // row c of tile t, columns of pair j
+  template <class R> static __device__ __forceinline__ A rows(const u4* m, int t, int j, int c, int g) { return m[R::at(t, c, g, 4 * j)]; }
   static __device__ __forceinline__ f4 mul_rows(A a, A b, f4 acc) { return mfma_bf16(a, b, acc); }
   // terms of float32 tiles; the residuals come from the matrix unit, 6 vector and 2 matrix instructions a tile for 22 vector ones
   using One = u2;
@@ -72,12 +77,12 @@ template <> struct Ops<uint16_t> {
   static __device__ __forceinline__ f4 mul_out(A a, const B& b, f4 acc) { return mfma_bf16(a, b.t[0], mfma_bf16(a, b.t[1], acc)); }
   // rows of the state's tile kt (m = key column 32 (kt / 2) + 8 (m / 4) + 4 (kt % 2) + m % 4) against the tokens of tiles t and t + 1
   template <class R> static __device__ __forceinline__ A columns(const u4* m, int kt, int t, int c, int g) {
-    const int piece = 4 * (kt / 2) + c % 4, row = 16 * t + 4 * g + c / 4;
-    return cat(read_transposed(m, R::at(row, piece), kt % 2), read_transposed(m, R::at(row + 16, piece), kt % 2));
+    const int row = 4 * g + c / 4, piece = c % 4, place = 4 * (kt / 2);
+    return cat(read_transposed(m, R::at(t, row, piece, place), kt % 2), read_transposed(m, R::at(t + 1, row, piece, place), kt % 2));
   }
   // accumulator tile of columns 16 n + lane, tokens of tile t; exact
   template <class R> static __device__ __forceinline__ u2 tile_raw(const u4* m, int n, int t, int c, int g) {
-    return read_transposed(m, R::at(16 * t + 4 * g + c / 4, 2 * n + (c % 4) / 2), c % 2);
+    return read_transposed(m, R::at(t, 4 * g + c / 4, (c % 4) / 2, 2 * n), c % 2);
   }
   template <class R> static __device__ __forceinline__ f4 tile(const u4* m, int n, int t, int c, int g) { return widen4(tile_raw<R>(m, n, t, c, g)); }
   static __device__ __forceinline__ void put(Image& im, int row, int g, f4 x) { tok_store(im.hm, im.l, row, row, g, x); }
@@ -106,8 +111,8 @@ template <> struct Ops<float> {
     for (int r = 0; r < 4; ++r) acc = mfma16(a[r], b[r], acc);
     return acc;
   }
-  template <class R> static __device__ __forceinline__ A rows(const u4* m, int row, int j, int g) {
-    return A{__builtin_bit_cast(f4, m[R::at(row, 8 * j + 2 * g)]), __builtin_bit_cast(f4, m[R::at(row, 8 * j + 2 * g + 1)])};
+  template <class R> static __device__ __forceinline__ A rows(const u4* m, int t, int j, int c, int g) {
+    return A{__builtin_bit_cast(f4, m[R::at(t, c, 2 * g, 8 * j)]), __builtin_bit_cast(f4, m[R::at(t, c, 2 * g, 8 * j + 1)])};
   }
   static __device__ __forceinline__ f4 mul_rows(const A& a, const A& b, f4 acc) { return mul4(a.x1, b.x1, mul4(a.x0, b.x0, acc)); }
   struct One {};
@@ -118,18 +123,18 @@ template <> struct Ops<float> {
   static __device__ __forceinline__ float value(const u4* m, int piece_at, int i) { return reinterpret_cast<const float*>(m + piece_at)[i]; }
   template <class R> static __device__ __forceinline__ A columns(const u4* m, int kt, int t, int c, int g) {
     A a;
-    const int piece = 8 * (kt / 2) + 2 * (c / 4) + kt % 2, row = 16 * t + 4 * g;
+    const int piece = 2 * (c / 4), place = 8 * (kt / 2) + kt % 2;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      a.x0[r] = value(m, R::at(row + r, piece), c % 4);
-      a.x1[r] = value(m, R::at(row + 16 + r, piece), c % 4);
+      a.x0[r] = value(m, R::at(t, 4 * g + r, piece, place), c % 4);
+      a.x1[r] = value(m, R::at(t + 1, 4 * g + r, piece, place), c % 4);
     }
     return a;
   }
   template <class R> static __device__ __forceinline__ f4 tile(const u4* m, int n, int t, int c, int g) {
     f4 x;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) x[r] = value(m, R::at(16 * t + 4 * g + r, 4 * n + c / 4), c % 4);
+    for (int r = 0; r < 4; ++r) x[r] = value(m, R::at(t, 4 * g + r, c / 4, 4 * n), c % 4);
     return x;
   }
   template <class R> static __device__ __forceinline__ f4 tile_raw(const u4* m, int n, int t, int c, int g) { return tile<R>(m, n, t, c, g); }

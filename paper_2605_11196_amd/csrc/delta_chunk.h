@@ -17,7 +17,7 @@ namespace delta {
 template <int DK, int DV, bool MAP>
 struct Shape {
   static constexpr int COLS = DV + (MAP ? DK : 0);
-  static constexpr int NT = COLS % 32 == 0 ? 2 : 1;           // column tiles of a wave
+  static constexpr int NT = 1;           // column tiles of a wave
   static constexpr int WAVES = COLS / (16 * NT);
   static constexpr int THREADS = 64 * WAVES;
   static constexpr int DKP = DK < 32 ? 32 : DK;               // key columns in pairs of tiles
@@ -25,7 +25,7 @@ struct Shape {
 };
 
 template <typename IO, int DK, int DV, bool MAP>
-__global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_kernel(DeltaArgs a) {
+__global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_kernel(DeltaArgs a) {
   using Sh = Shape<DK, DV, MAP>;
   using O = Ops<IO>;
   constexpr int NT = Sh::NT, KT = Sh::KT, WAVES = Sh::WAVES, THREADS = Sh::THREADS;
@@ -39,7 +39,8 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
   __shared__ __align__(16) float diagonal[kTiles][16 * 20];
   __shared__ Gates gate_pair[2];
 
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  int c = lane % 16, g = lane / 16;
   const int head = blockIdx.x / a.n_seg, seg = blockIdx.x % a.n_seg;
   const int b = head / a.H_v, h = head % a.H_v, hk = h / (a.H_v / a.H_k);
   const int len = __builtin_amdgcn_readfirstlane(a.lengths ? max(0, min(a.lengths[b], a.T)) : a.T);
@@ -57,7 +58,6 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
   // ---- the state: tile kt holds key columns 32 (kt / 2) + 8 g + 4 (kt % 2) + r
   f4 S[NT][KT];
   const float* S0 = a.S0 ? a.S0 + (static_cast<size_t>(head) * (a.seg_states ? a.n_seg : 1) + (a.seg_states ? seg : 0)) * DV * DK : nullptr;
-  if (MAP && seg > 0) S0 = nullptr;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int col = col0 + 16 * n;
@@ -108,6 +108,8 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
   int turn = 0;
 
   for (int t0 = first; t0 < end; t0 += kTok) {
+    // the LDS addresses are formed anew in each block: kept over the loop they would take the registers of the state
+    asm volatile("" : "+v"(c), "+v"(g));
     if (!MAP && a.saved != nullptr) {
       float* out = a.saved + (static_cast<size_t>(head) * a.n_blocks + t0 / kTok) * DV * DK;
 #pragma unroll
@@ -143,7 +145,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
       f4 x = f4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int s = 0; s < KT / 2; ++s) {
-        x = O::mul_rows(O::template rows<RK>(sK, 16 * j + c, s, g), O::template rows<RK>(keys || MAP ? sK : sQ, 16 * i + c, s, g), x);
+        x = O::mul_rows(O::template rows<RK>(sK, j, s, c, g), O::template rows<RK>(keys || MAP ? sK : sQ, i, s, c, g), x);
       }
       const float hi = gates.hi[16 * i + c], lo = gates.lo[16 * i + c];
       const f4 hj = *reinterpret_cast<const f4*>(&gates.hi[16 * j + 4 * g]), lj = *reinterpret_cast<const f4*>(&gates.lo[16 * j + 4 * g]);
@@ -175,8 +177,8 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 2) delta_chunk_
       typename O::A ka[kTiles], qa[kTiles];
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
-        ka[i] = O::template rows<RK>(sK, 16 * i + c, s, g);
-        if constexpr (!MAP) qa[i] = O::template rows<RK>(sQ, 16 * i + c, s, g);
+        ka[i] = O::template rows<RK>(sK, i, s, c, g);
+        if constexpr (!MAP) qa[i] = O::template rows<RK>(sQ, i, s, c, g);
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {

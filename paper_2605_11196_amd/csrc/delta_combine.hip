@@ -1,0 +1,82 @@
+// The states between time segments of the gated delta rule.  A segment's map is affine in the state that it starts from, row by row:
+// S_end = S_start X + Y (delta_chunk.h forms X and Y of every segment at once), so
+//   seg_S[0] = S0;  seg_S[s + 1] = seg_S[s] X_s + Y_s.
+//
+// A workgroup takes 16 rows of S of one head, which need nothing of the others, and goes through the segments; a wave forms 16
+// columns of the product on the FP32 matrix instruction, from the rows that the waves leave in LDS.  The product is transposed: a
+// result tile (columns of S along its rows) is the right operand of the next product as it stands.  X of the next segment is
+// requested before the present product.  Bound by the latency of a step: 0.7 us at d_k = 128.
+#include "layer_common.h"
+#include "vla_mfma_util.h"
+
+namespace vla {
+namespace {
+
+template <int DK>
+__global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, float* seg_S, int d_v) {
+  constexpr int KT = DK / 16;
+  __shared__ f4 state[2][KT][64];
+  const int tiles = d_v / 16, head = blockIdx.x / tiles, row = 16 * (blockIdx.x % tiles);
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
+  const size_t map = static_cast<size_t>(d_v + DK) * DK, one = static_cast<size_t>(d_v) * DK;
+  const float* maps = a.seg_map + static_cast<size_t>(head) * a.n_seg * map;
+  float* out = seg_S + static_cast<size_t>(head) * a.n_seg * one + static_cast<size_t>(row + c) * DK + 16 * wave + 4 * g;
+  f4 own = f4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (a.S0 != nullptr) own = *reinterpret_cast<const f4*>(a.S0 + head * one + static_cast<size_t>(row + c) * DK + 16 * wave + 4 * g);
+  float x[KT][4];
+  f4 y;
+  auto request = [&](int s) {
+    const float* m = maps + s * map;
+    y = *reinterpret_cast<const f4*>(m + static_cast<size_t>(row + c) * DK + 16 * wave + 4 * g);
+    const float* X = m + one + 16 * wave + c;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[kt][r] = X[(16 * kt + 4 * g + r) * DK];
+    }
+  };
+  if (a.n_seg > 1) request(0);
+  for (int s = 0; s + 1 < a.n_seg; ++s) {
+    *reinterpret_cast<f4*>(out + s * one) = own;
+    state[s & 1][wave][lane] = own;
+    __syncthreads();
+    f4 acc[2] = {y, f4{0.0f, 0.0f, 0.0f, 0.0f}};
+    float now[KT][4];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) now[kt][r] = x[kt][r];
+    }
+    request(min(s + 1, a.n_seg - 2));
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      const f4 b = state[s & 1][kt][lane];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[r & 1] = mfma16(now[kt][r], b[r], acc[r & 1]);
+    }
+    own = acc[0] + acc[1];
+  }
+  *reinterpret_cast<f4*>(out + (a.n_seg - 1) * one) = own;
+}
+
+template <int DK>
+hipError_t launch(const DeltaArgs& a, float* seg_S, int d_v, hipStream_t stream) {
+  DeltaArgs args = a;
+  void* params[] = {&args, &seg_S, &d_v};
+  return hipLaunchKernel(reinterpret_cast<const void*>(&delta_combine_kernel<DK>), dim3(a.B * a.H_v * (d_v / 16)), dim3(4 * DK), params, 0, stream);
+}
+
+}  // namespace
+
+hipError_t launch_delta_combine(const DeltaArgs& a, float* seg_S, int d_k, int d_v, hipStream_t stream) {
+  switch (d_k) {
+    case 16: return launch<16>(a, seg_S, d_v, stream);
+    case 32: return launch<32>(a, seg_S, d_v, stream);
+    case 64: return launch<64>(a, seg_S, d_v, stream);
+    case 96: return launch<96>(a, seg_S, d_v, stream);
+    case 128: return launch<128>(a, seg_S, d_v, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace vla

@@ -82,7 +82,7 @@ int launched(hipError_t err) {
 int check_delta(int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, const vla_delta_opts& o) {
   if (B <= 0 || H_k <= 0 || H_v <= 0 || T < 0 || d_k <= 0 || d_v <= 0 || H_v % H_k != 0) return VLA_ERR_INVALID_ARG;
   if (io_dtype != VLA_F32 && io_dtype != VLA_BF16) return VLA_ERR_INVALID_ARG;
-  if (!(fabsf(o.scale) <= 3.4e38f)) return VLA_ERR_INVALID_ARG;
+  if (!(fabsf(o.scale) <= 3.4e38f) || o.segments < 0) return VLA_ERR_INVALID_ARG;
   if (!vla::layer_head_size(d_k) || !vla::layer_head_size(d_v)) return VLA_ERR_UNSUPPORTED;
   // workgroups (up to 32 a head and segment) and tokens with a block of look-ahead are 32-bit indices
   if (static_cast<long long>(B) * H_v > 0x7fffffff / 32 || T > 0x7fffff00) return VLA_ERR_UNSUPPORTED;
@@ -101,6 +101,32 @@ bool gate_rows(const vla_strides& s, long long H, long long T, vla::Rows* out) {
   *out = vla::Rows{s.b, s.h, s.t};
   if (s.b == 0 && s.h == 0 && s.t == 0) *out = vla::Rows{H * T, T, 1};
   return out->b >= 0 && out->h >= 0 && out->t >= 0;
+}
+
+// Time segments of a sequence.  Few heads leave most of the card idle; in segments the sequence goes through twice (maps, then outputs: 2.7
+// times the work) with about `waves` waves on the card.
+struct Segments {
+  int n, tokens;
+  size_t map_bytes, bytes;   // of the maps, of both arrays
+};
+Segments delta_segments(long long heads, int T, int d_k, int d_v, int requested) {
+  Segments s{1, T, 0, 0};
+  const int blocks = (T + 31) / 32;
+  long long n = requested;
+  if (requested == 0) {
+    n = 4096 / (heads * (d_v / 16));      // 16 waves a compute unit, d_v / 16 a workgroup
+    if (n > blocks / 4) n = blocks / 4;
+    if (n < 6) n = 1;
+  }
+  if (n > blocks) n = blocks;
+  if (n > 256) n = 256;
+  if (n <= 1) return s;
+  const int each = static_cast<int>((blocks + n - 1) / n);
+  s.n = (blocks + each - 1) / each;
+  s.tokens = 32 * each;
+  s.map_bytes = static_cast<size_t>(heads) * s.n * (d_v + d_k) * d_k * 4;
+  s.bytes = s.map_bytes + static_cast<size_t>(heads) * s.n * d_v * d_k * 4;
+  return s;
 }
 
 hipError_t launch_blocks(const vla::DeltaArgs& a, int d_k, int d_v, int io_dtype, bool map, hipStream_t stream) {
@@ -123,7 +149,9 @@ void vla_delta_default_opts(vla_delta_opts* opts) {
 }
 
 size_t vla_delta_workspace_bytes(int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts, int backward) {
-  return 0;
+  const vla_delta_opts op = delta_opts(opts, d_k);
+  if (check_delta(B, H_k, H_v, T, d_k, d_v, io_dtype, op) != VLA_OK) return 0;
+  return delta_segments(static_cast<long long>(B) * H_v, T, d_k, d_v, op.segments).bytes;
 }
 size_t vla_delta_saved_bytes(int B, int H_v, int T, int d_k, int d_v, int io_dtype) { return 0; }
 int vla_delta_backward(const void* q, const void* k, const void* v, const float* g, const float* beta, const void* dO, const float* dS_T,
@@ -158,8 +186,8 @@ int vla_delta_forward(const void* q, const void* k, const void* v, const float* 
   const Range r[] = {{q, reach(a.qs, B, H_k, T, d_k, es), false}, {k, reach(a.ks, B, H_k, T, d_k, es), false},
                      {v, reach(a.vs, B, H_v, T, d_v, es), false}, {g, reach(a.gs, B, H_v, T, 1, 4), false},
                      {beta, reach(a.bs, B, H_v, T, 1, 4), false}, {op.lengths, static_cast<size_t>(B) * 4, false},
-                     {S0, nS, false}, {o, reach(a.os, B, H_v, T, d_v, es), true}, {S_T, nS, true}};
-  if (!disjoint(r, 9, S0, S_T)) return VLA_ERR_INVALID_ARG;
+                     {S0, nS, false}, {o, reach(a.os, B, H_v, T, d_v, es), true}, {S_T, nS, true}, {workspace, workspace_bytes, true}};
+  if (!aligned16(workspace) || !disjoint(r, 10, S0, S_T)) return VLA_ERR_INVALID_ARG;
   if (T == 0 && S_T == nullptr) return VLA_OK;
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.S0 = S0; a.o = o; a.S_T = S_T;
   a.lengths = op.lengths;
@@ -170,6 +198,19 @@ int vla_delta_forward(const void* q, const void* k, const void* v, const float* 
   a.seg_tokens = T;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (T < 16) return launched(vla::launch_delta_step(a, d_k, d_v, io_dtype, s));
+  Segments seg = delta_segments(static_cast<long long>(B) * H_v, T, d_k, d_v, op.segments);
+  if (seg.n == 1 || workspace == nullptr || workspace_bytes < seg.bytes) return launched(launch_blocks(a, d_k, d_v, io_dtype, false, s));
+  a.n_seg = seg.n;
+  a.seg_tokens = seg.tokens;
+  a.seg_map = static_cast<float*>(workspace);
+  float* states = reinterpret_cast<float*>(static_cast<char*>(workspace) + seg.map_bytes);
+  vla::DeltaArgs maps = a;
+  maps.S0 = nullptr;
+  hipError_t err = launch_blocks(maps, d_k, d_v, io_dtype, true, s);
+  if (err == hipSuccess) err = vla::launch_delta_combine(a, states, d_k, d_v, s);
+  if (err != hipSuccess) return launched(err);
+  a.S0 = states;
+  a.seg_states = true;
   return launched(launch_blocks(a, d_k, d_v, io_dtype, false, s));
 }
 

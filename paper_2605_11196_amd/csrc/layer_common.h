@@ -63,6 +63,9 @@ hipError_t launch_delta_chunk_64(const DeltaArgs& a, int d_v, int io_dtype, bool
 hipError_t launch_delta_chunk_96(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
 hipError_t launch_delta_chunk_128(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
 
+// seg_S[h][0] = S0[h], seg_S[h][s + 1] = seg_S[h][s] X + Y of segment s (delta_combine.hip)
+hipError_t launch_delta_combine(const DeltaArgs& a, float* seg_S, int d_k, int d_v, hipStream_t stream);
+
 inline bool layer_head_size(int d) { return d == 16 || d == 32 || d == 64 || d == 96 || d == 128; }
 
 }  // namespace vla

@@ -198,3 +198,17 @@ def test_runs_on_the_given_stream():
     got = vla.gated_delta_forward(*inputs, stream=s)
     torch.cuda.current_stream().wait_stream(s)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d_k,d_v,T,segments", [(16, 16, 100, 2), (16, 96, 333, 4), (32, 64, 200, 7), (64, 64, 1000, 5), (64, 32, 97, 256), (96, 128, 300, 3),
+                                                (128, 128, 500, 8), (128, 16, 129, 4)])
+def test_time_segments(d_k, d_v, T, segments, dtype):
+    """Cut into segments: the same results, with a given state and ragged lengths that end inside and before a segment."""
+    inputs = make(3, 1, 2, T, d_k, d_v, dtype, seed=T + d_k, rate=0.05)
+    lengths = torch.tensor([T, T // 2 + 3, 0], device="cuda", dtype=torch.int32)
+    check(inputs, dtype, segments=segments, lengths=lengths)
+    check((*inputs[:5], None), dtype, segments=segments)
+    whole = vla.gated_delta_forward(*inputs, segments=1)
+    cut = vla.gated_delta_forward(*inputs, segments=segments)
+    close(cut[1], whole[1].double(), 2 * TOL["f32"], "S_T against one segment")
