@@ -93,6 +93,50 @@ template <> struct Ops<uint16_t> {
     return TokB{cat(h, m), cat(m, h), cat(h, l)};
   }
   static __device__ __forceinline__ f4 mul_tok(const TA& a, const TB& b, f4 acc) { return mfma_tok(a, b, acc); }
+  // Matrices that are kept in float32 (R, W) are staged in terms, one set of rows for each (a right operand is laid out alike).
+  static constexpr int TERMS = 3;
+  using Split = Terms<3>;
+  template <int N, class R> static __device__ __forceinline__ Split rows_split(const u4* m, int t, int j, int c, int g) {
+    Split s{};
+#pragma unroll
+    for (int i = 0; i < N; ++i) s.t[i] = m[i * kTok * R::STRIDE + R::at(t, c, g, 4 * j)];
+    return s;
+  }
+  template <int N, class R> static __device__ __forceinline__ Split columns_split(const u4* m, int kt, int t, int c, int g) {
+    Split s{};
+#pragma unroll
+    for (int i = 0; i < N; ++i) s.t[i] = columns<R>(m + i * kTok * R::STRIDE, kt, t, c, g);
+    return s;
+  }
+  // four values of a row, the p-th four
+  template <int N, class R> static __device__ __forceinline__ void put_split(u4* m, int row, int p, f4 x) {
+    u2 t[3];
+    split3_rne(x, t[0], t[1], t[2]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) reinterpret_cast<u2*>(m + i * kTok * R::STRIDE + R::at(row, p / 2))[p % 2] = t[i];
+  }
+  static __device__ __forceinline__ f4 mul_split(const Split& a, const B& b, f4 acc) { return mfma_terms(a, b, acc); }
+  static __device__ __forceinline__ f4 mul_split_exact(const Split& a, A b, f4 acc) { return mfma_terms_left(a, Terms<1>{{b}}, acc); }
+  // 16 bits of each factor: for gradients that are rounded to bf16
+  static __device__ __forceinline__ f4 mul_split_out(const Split& a, const B& b, f4 acc) {
+    acc = mfma_bf16(a.t[1], b.t[0], acc);
+    acc = mfma_bf16(a.t[0], b.t[1], acc);
+    return mfma_bf16(a.t[0], b.t[0], acc);
+  }
+  struct ImageOut { u4 hm[64]; };
+  static __device__ __forceinline__ void put(ImageOut& im, int row, int g, f4 x) {
+    u2 h, m, l;
+    split3_rne(x, h, m, l);
+    im.hm[4 * row + tok_chunk(row, g)] = cat(h, m);
+  }
+  static __device__ __forceinline__ u4 image(const ImageOut& im, int c, int g) { return im.hm[4 * c + tok_chunk(c, g)]; }
+  // an exact right operand
+  using Raw = u2;
+  static __device__ __forceinline__ f4 mul_tok_raw(u4 a, Raw b, f4 acc) { return mfma_bf16(a, cat(b, b), acc); }
+  static __device__ __forceinline__ f4 value(Raw x) { return widen4(x); }
+  static __device__ __forceinline__ f4 mul_tok_raw(const TA& a, Raw b, f4 acc) {
+    return mfma_bf16(a.hm, cat(b, b), mfma_bf16(a.lh, cat(b, u2{0, 0}), acc));
+  }
   static __device__ __forceinline__ f4 mul_tok_out(const TA& a, const TB& b, f4 acc) {
     return mfma_bf16(a.hm, b.hm, mfma_bf16(a.hm, b.mh, acc));
   }
@@ -143,6 +187,20 @@ template <> struct Ops<float> {
   static __device__ __forceinline__ TB tokens(f4 x, One) { return x; }
   static __device__ __forceinline__ f4 mul_tok(const TA& a, const TB& b, f4 acc) { return mul4(a, b, acc); }
   static __device__ __forceinline__ f4 mul_tok_out(const TA& a, const TB& b, f4 acc) { return mul4(a, b, acc); }
+  static constexpr int TERMS = 1;
+  using Split = A;
+  template <int N, class R> static __device__ __forceinline__ Split rows_split(const u4* m, int t, int j, int c, int g) { return rows<R>(m, t, j, c, g); }
+  template <int N, class R> static __device__ __forceinline__ Split columns_split(const u4* m, int kt, int t, int c, int g) { return columns<R>(m, kt, t, c, g); }
+  template <int N, class R> static __device__ __forceinline__ void put_split(u4* m, int row, int p, f4 x) { m[R::at(row, p)] = __builtin_bit_cast(u4, x); }
+  static __device__ __forceinline__ f4 mul_split(const A& a, const B& b, f4 acc) { return mul(a, b, acc); }
+  static __device__ __forceinline__ f4 mul_split_exact(const A& a, const A& b, f4 acc) { return mul_rows(a, b, acc); }
+  static __device__ __forceinline__ f4 mul_split_out(const A& a, const B& b, f4 acc) { return mul(a, b, acc); }
+  static __device__ __forceinline__ f4 mul(const A& a, const A& b, f4 acc) { return mul_rows(a, b, acc); }
+  static __device__ __forceinline__ f4 mul_split_out(const A& a, const A& b, f4 acc) { return mul_rows(a, b, acc); }
+  using ImageOut = Image;
+  using Raw = f4;
+  static __device__ __forceinline__ f4 value(Raw x) { return x; }
+  static __device__ __forceinline__ f4 mul_tok_raw(const TA& a, Raw b, f4 acc) { return mul4(a, b, acc); }
 };
 
 // Rows of memory as a buffer whose bounds the hardware checks: loads past the last row give zeros, stores past it are dropped, so that
@@ -164,6 +222,14 @@ struct Stage {
     for (int i = 0; i < N; ++i) {
       const int p = threadIdx.x + i * THREADS;
       at[i] = p < ALL ? p / PIECES * static_cast<int>(step_bytes) + p % PIECES * 16 : 0x7fffffff;
+    }
+  }
+  // the last token in the first row
+  __device__ __forceinline__ void init_reversed(long long step_bytes) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int p = threadIdx.x + i * THREADS;
+      at[i] = p < ALL ? (kTok - 1 - p / PIECES) * static_cast<int>(step_bytes) + p % PIECES * 16 : 0x7fffffff;
     }
   }
   // rows t0 .. t0 + 31 of base; zeros from row `end` on
@@ -222,8 +288,8 @@ __device__ __forceinline__ double of_lane(double x, int lane) {
   return __builtin_bit_cast(double, uint2{static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(b.x), lane)),
                                           static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(b.y), lane))});
 }
-// by one wave; g and beta of token `lane` (0 past the end of the sequence)
-__device__ __forceinline__ void put_gates(Gates& s, int lane, float g, float beta) {
+// by one wave; g and beta of token `lane` (0 past the end of the sequence), whose place in the arrays is `at`
+__device__ __forceinline__ void put_gates(Gates& s, int lane, int at, float g, float beta) {
   static_assert(kTok == 32, "two rows of lanes");
   double G = static_cast<double>(g < -10000.0f ? -10000.0f : g) * 1.4426950408889634;
   G += shifted_up<1>(G);
@@ -235,11 +301,11 @@ __device__ __forceinline__ void put_gates(Gates& s, int lane, float g, float bet
   const double all = of_lane(G, kTok - 1);
   if (lane < kTok) {
     const float hi = static_cast<float>(G);
-    s.hi[lane] = hi;
-    s.lo[lane] = static_cast<float>(G - static_cast<double>(hi));
-    s.gamma[lane] = exp2_of(G);
-    s.rest[lane] = exp2_of(all - G);
-    s.beta[lane] = beta;
+    s.hi[at] = hi;
+    s.lo[at] = static_cast<float>(G - static_cast<double>(hi));
+    s.gamma[at] = exp2_of(G);
+    s.rest[at] = exp2_of(all - G);
+    s.beta[at] = beta;
     if (lane == 0) s.end = exp2_of(all);
   }
 }

@@ -65,7 +65,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
     for (int kt = 0; kt < KT; ++kt) {
       const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
       S[n][kt] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-      if (dk < DK && col < DV && S0 != nullptr) S[n][kt] = *reinterpret_cast<const f4*>(S0 + static_cast<size_t>(col) * DK + dk);
+      if ((DK == Sh::DKP || dk < DK) && (!MAP || col < DV) && S0 != nullptr) S[n][kt] = *reinterpret_cast<const f4*>(S0 + static_cast<size_t>(col) * DK + dk);
       if (MAP && col >= DV) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[n][kt][r] = col - DV == dk + r ? 1.0f : 0.0f;
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
     beta = bp[t * a.bs.t];
   };
   auto next_gates = [&](int t0, Gates& to) {
-    if (wave == WAVES - 1) put_gates(to, lane, t0 + lane < end ? gate : 0.0f, t0 + lane < end ? beta : 0.0f);
+    if (wave == WAVES - 1) put_gates(to, lane, lane, t0 + lane < end ? gate : 0.0f, t0 + lane < end ? beta : 0.0f);
   };
   if (first < end) {
     request_gates(first);
@@ -107,20 +107,23 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
   }
   int turn = 0;
 
-  for (int t0 = first; t0 < end; t0 += kTok) {
-    // the LDS addresses are formed anew in each block: kept over the loop they would take the registers of the state
-    asm volatile("" : "+v"(c), "+v"(g));
-    if (!MAP && a.saved != nullptr) {
-      float* out = a.saved + (static_cast<size_t>(head) * a.n_blocks + t0 / kTok) * DV * DK;
+  for (int t0 = first; t0 < end;) {
+    // the state at the start of every 256 tokens; the blocks between two such places in a loop of their own
+    if (!MAP && a.kept != nullptr && t0 % kKeep == 0) {
+      float* out = a.kept + (static_cast<size_t>(head) * a.n_kept + t0 / kKeep) * DV * DK;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
           const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-          if (dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col0 + 16 * n) * DK + dk) = S[n][kt];
+          if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col0 + 16 * n) * DK + dk) = S[n][kt];
         }
       }
     }
+    const int stop = min(end, (t0 / kKeep + 1) * kKeep);
+    for (; t0 < stop; t0 += kTok) {
+    // the LDS addresses are formed anew in each block: kept over the loop they would take the registers of the state
+    asm volatile("" : "+v"(c), "+v"(g));
     stK.template store<RK>(sK);
     if constexpr (!MAP) stQ.template store<RK>(sQ);
     stV.template store<RV>(sV);
@@ -220,6 +223,14 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
         if (!MAP || i + 1 < kTiles) rb[n][i] = O::tokens(R[n][i], one);
       }
     }
+    if (!MAP && a.rows != nullptr) {
+      const __amdgpu_buffer_rsrc_t out = rows_buffer(a.rows + (static_cast<size_t>(head) * a.T + t0) * DV, DV * 4, last - t0, DV * 4);
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) store_column(out, ((16 * i + 4 * g) * DV + col0 + 16 * n) * 4, DV * 4, R[n][i], static_cast<float*>(nullptr));
+      }
+    }
     typename O::B w[NT];
     static_assert(kTiles == 2, "one pair of token tiles");
     {
@@ -258,6 +269,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
     next_gates(t0 + kTok, gate_pair[turn]);
     request_gates(t0 + 2 * kTok);
     __syncthreads();
+    }
   }
 
   // ---- outputs of tokens past the end of the sequence, the state
@@ -276,7 +288,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
       const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-      if (dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col0 + 16 * n) * DK + dk) = S[n][kt];
+      if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col0 + 16 * n) * DK + dk) = S[n][kt];
     }
   }
 }

@@ -1,6 +1,7 @@
 // The states between time segments of the gated delta rule.  A segment's map is affine in the state that it starts from, row by row:
 // S_end = S_start X + Y (delta_chunk.h forms X and Y of every segment at once), so
-//   seg_S[0] = S0;  seg_S[s + 1] = seg_S[s] X_s + Y_s.
+//   seg_S[0] = S0;  seg_S[s + 1] = seg_S[s] X_s + Y_s,
+// and in the backward pass from the last segment to the first.
 //
 // A workgroup takes 16 rows of S of one head, which need nothing of the others, and goes through the segments; a wave forms 16
 // columns of the product on the FP32 matrix instruction, from the rows that the waves leave in LDS.  The product is transposed: a
@@ -13,7 +14,7 @@ namespace vla {
 namespace {
 
 template <int DK>
-__global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, float* seg_S, int d_v) {
+__global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, float* seg_S, int d_v, int backward) {
   constexpr int KT = DK / 16;
   __shared__ f4 state[2][KT][64];
   const int tiles = d_v / 16, head = blockIdx.x / tiles, row = 16 * (blockIdx.x % tiles);
@@ -35,9 +36,10 @@ __global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, floa
       for (int r = 0; r < 4; ++r) x[kt][r] = X[(16 * kt + 4 * g + r) * DK];
     }
   };
-  if (a.n_seg > 1) request(0);
+  const auto place = [&](int s) { return backward ? a.n_seg - 1 - s : s; };
+  if (a.n_seg > 1) request(place(0));
   for (int s = 0; s + 1 < a.n_seg; ++s) {
-    *reinterpret_cast<f4*>(out + s * one) = own;
+    *reinterpret_cast<f4*>(out + place(s) * one) = own;
     state[s & 1][wave][lane] = own;
     __syncthreads();
     f4 acc[2] = {y, f4{0.0f, 0.0f, 0.0f, 0.0f}};
@@ -47,7 +49,7 @@ __global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, floa
 #pragma unroll
       for (int r = 0; r < 4; ++r) now[kt][r] = x[kt][r];
     }
-    request(min(s + 1, a.n_seg - 2));
+    request(place(min(s + 1, a.n_seg - 2)));
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
       const f4 b = state[s & 1][kt][lane];
@@ -56,25 +58,25 @@ __global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, floa
     }
     own = acc[0] + acc[1];
   }
-  *reinterpret_cast<f4*>(out + (a.n_seg - 1) * one) = own;
+  *reinterpret_cast<f4*>(out + place(a.n_seg - 1) * one) = own;
 }
 
 template <int DK>
-hipError_t launch(const DeltaArgs& a, float* seg_S, int d_v, hipStream_t stream) {
+hipError_t launch(const DeltaArgs& a, float* seg_S, int d_v, int backward, hipStream_t stream) {
   DeltaArgs args = a;
-  void* params[] = {&args, &seg_S, &d_v};
+  void* params[] = {&args, &seg_S, &d_v, &backward};
   return hipLaunchKernel(reinterpret_cast<const void*>(&delta_combine_kernel<DK>), dim3(a.B * a.H_v * (d_v / 16)), dim3(4 * DK), params, 0, stream);
 }
 
 }  // namespace
 
-hipError_t launch_delta_combine(const DeltaArgs& a, float* seg_S, int d_k, int d_v, hipStream_t stream) {
+hipError_t launch_delta_combine(const DeltaArgs& a, float* seg_S, int d_k, int d_v, bool backward, hipStream_t stream) {
   switch (d_k) {
-    case 16: return launch<16>(a, seg_S, d_v, stream);
-    case 32: return launch<32>(a, seg_S, d_v, stream);
-    case 64: return launch<64>(a, seg_S, d_v, stream);
-    case 96: return launch<96>(a, seg_S, d_v, stream);
-    case 128: return launch<128>(a, seg_S, d_v, stream);
+    case 16: return launch<16>(a, seg_S, d_v, backward, stream);
+    case 32: return launch<32>(a, seg_S, d_v, backward, stream);
+    case 64: return launch<64>(a, seg_S, d_v, backward, stream);
+    case 96: return launch<96>(a, seg_S, d_v, backward, stream);
+    case 128: return launch<128>(a, seg_S, d_v, backward, stream);
     default: return hipErrorInvalidValue;
   }
 }

@@ -1,0 +1,8 @@
+// The chain of the state's gradient of the gated delta rule for key heads of 64 (delta_reverse.h).
+#include "delta_reverse.h"
+
+namespace vla {
+hipError_t launch_delta_reverse_64(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream) {
+  return delta::launch_reverse_dk<64>(a, d_v, io_dtype, map, stream);
+}
+}  // namespace vla

@@ -40,6 +40,7 @@ bool disjoint(const Range* r, int n, const void* same0, const void* same1) {
 bool rows_of(const vla_strides& s, long long H, long long T, long long d, int per16, vla::Rows* out) {
   *out = vla::Rows{s.b, s.h, s.t};
   if (s.b == 0 && s.h == 0 && s.t == 0) *out = vla::Rows{H * T * d, T * d, d};
+  if (T == 1) out->t = d;   // the step to a token that is not there: the kernels' bounds need it to be one
   return out->b >= 0 && out->h >= 0 && out->t >= 0 && out->b % per16 == 0 && out->h % per16 == 0 && out->t % per16 == 0;
 }
 size_t reach(const vla::Rows& r, long long B, long long H, long long T, long long d, size_t es) {
@@ -129,6 +130,49 @@ Segments delta_segments(long long heads, int T, int d_k, int d_v, int requested)
   return s;
 }
 
+// What the forward pass keeps, and what the backward pass works on; each part starts at a multiple of 256 bytes.
+size_t padded(size_t n) { return (n + 255) / 256 * 256; }
+int kept_states(int T) { return (T + vla::kKeep - 1) / vla::kKeep; }
+size_t kept_bytes(long long heads, int T, int d_k, int d_v) { return padded(static_cast<size_t>(heads) * kept_states(T) * d_v * d_k * 4); }
+size_t row_bytes(long long heads, int T, int d) { return padded(static_cast<size_t>(heads) * T * d * 4); }
+struct BackwardParts {
+  Segments seg;
+  size_t kept, rows, dk, dq, seg_map, seg_S, bytes;   // offsets
+};
+BackwardParts backward_parts(long long heads, int T, int d_k, int d_v, bool shared, int requested) {
+  BackwardParts p{};
+  p.seg = delta_segments(heads, T, d_k, d_v, requested);
+  p.kept = 0;
+  p.rows = p.kept + kept_bytes(heads, T, d_k, d_v);
+  p.dk = p.rows + row_bytes(heads, T, d_v);
+  p.dq = p.dk + row_bytes(heads, T, d_k);
+  p.seg_map = p.dq + (shared ? row_bytes(heads, T, d_k) : 0);
+  p.seg_S = p.seg_map + padded(p.seg.map_bytes);
+  p.bytes = p.seg_S + padded(p.seg.bytes - p.seg.map_bytes);
+  return p;
+}
+
+hipError_t launch_reverse(const vla::DeltaArgs& a, int d_k, int d_v, int io_dtype, bool map, hipStream_t stream) {
+  switch (d_k) {
+    case 16: return vla::launch_delta_reverse_16(a, d_v, io_dtype, map, stream);
+    case 32: return vla::launch_delta_reverse_32(a, d_v, io_dtype, map, stream);
+    case 64: return vla::launch_delta_reverse_64(a, d_v, io_dtype, map, stream);
+    case 96: return vla::launch_delta_reverse_96(a, d_v, io_dtype, map, stream);
+    case 128: return vla::launch_delta_reverse_128(a, d_v, io_dtype, map, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+hipError_t launch_grad(const vla::DeltaArgs& a, int d_k, int d_v, int io_dtype, hipStream_t stream) {
+  switch (d_k) {
+    case 16: return vla::launch_delta_grad_16(a, d_v, io_dtype, stream);
+    case 32: return vla::launch_delta_grad_32(a, d_v, io_dtype, stream);
+    case 64: return vla::launch_delta_grad_64(a, d_v, io_dtype, stream);
+    case 96: return vla::launch_delta_grad_96(a, d_v, io_dtype, stream);
+    case 128: return vla::launch_delta_grad_128(a, d_v, io_dtype, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+
 hipError_t launch_blocks(const vla::DeltaArgs& a, int d_k, int d_v, int io_dtype, bool map, hipStream_t stream) {
   switch (d_k) {
     case 16: return vla::launch_delta_chunk_16(a, d_v, io_dtype, map, stream);
@@ -151,15 +195,17 @@ void vla_delta_default_opts(vla_delta_opts* opts) {
 size_t vla_delta_workspace_bytes(int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts, int backward) {
   const vla_delta_opts op = delta_opts(opts, d_k);
   if (check_delta(B, H_k, H_v, T, d_k, d_v, io_dtype, op) != VLA_OK) return 0;
-  return delta_segments(static_cast<long long>(B) * H_v, T, d_k, d_v, op.segments).bytes;
-}
-size_t vla_delta_saved_bytes(int B, int H_v, int T, int d_k, int d_v, int io_dtype) { return 0; }
-int vla_delta_backward(const void* q, const void* k, const void* v, const float* g, const float* beta, const void* dO, const float* dS_T,
-                       void* dq, void* dk, void* dv, float* dg, float* dbeta, float* dS0, int B, int H_k, int H_v, int T, int d_k,
-                       int d_v, int io_dtype, const vla_delta_opts* opts, void* workspace, size_t workspace_bytes, void* stream) {
-  return VLA_ERR_UNSUPPORTED;
+  const long long heads = static_cast<long long>(B) * H_v;
+  if (!backward) return delta_segments(heads, T, d_k, d_v, op.segments).bytes;
+  return backward_parts(heads, T, d_k, d_v, H_v != H_k, op.segments).bytes;
 }
 
+size_t vla_delta_saved_bytes(int B, int H_v, int T, int d_k, int d_v, int io_dtype) {
+  vla_delta_opts op;
+  vla_delta_default_opts(&op);
+  if (check_delta(B, 1, H_v, T, d_k, d_v, io_dtype, op) != VLA_OK) return 0;
+  return kept_bytes(static_cast<long long>(B) * H_v, T, d_k, d_v) + row_bytes(static_cast<long long>(B) * H_v, T, d_v);
+}
 int vla_delta_forward(const void* q, const void* k, const void* v, const float* g, const float* beta, const float* S0, void* o,
                       float* S_T, int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts,
                       void* workspace, size_t workspace_bytes, void* stream) {
@@ -186,18 +232,24 @@ int vla_delta_forward(const void* q, const void* k, const void* v, const float* 
   const Range r[] = {{q, reach(a.qs, B, H_k, T, d_k, es), false}, {k, reach(a.ks, B, H_k, T, d_k, es), false},
                      {v, reach(a.vs, B, H_v, T, d_v, es), false}, {g, reach(a.gs, B, H_v, T, 1, 4), false},
                      {beta, reach(a.bs, B, H_v, T, 1, 4), false}, {op.lengths, static_cast<size_t>(B) * 4, false},
-                     {S0, nS, false}, {o, reach(a.os, B, H_v, T, d_v, es), true}, {S_T, nS, true}, {workspace, workspace_bytes, true}};
-  if (!aligned16(workspace) || !disjoint(r, 10, S0, S_T)) return VLA_ERR_INVALID_ARG;
+                     {S0, nS, false}, {o, reach(a.os, B, H_v, T, d_v, es), true}, {S_T, nS, true}, {workspace, workspace_bytes, true},
+                     {op.saved, op.saved_bytes, true}};
+  if (!aligned16(workspace) || !aligned16(op.saved) || !disjoint(r, 11, S0, S_T)) return VLA_ERR_INVALID_ARG;
+  if (op.saved != nullptr && op.saved_bytes < vla_delta_saved_bytes(B, H_v, T, d_k, d_v, io_dtype)) return VLA_ERR_WORKSPACE;
   if (T == 0 && S_T == nullptr) return VLA_OK;
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.S0 = S0; a.o = o; a.S_T = S_T;
   a.lengths = op.lengths;
   a.B = B; a.H_k = H_k; a.H_v = H_v; a.T = T;
   a.scale = op.scale;
-  a.n_blocks = (T + 31) / 32;
   a.n_seg = 1;
   a.seg_tokens = T;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (T < 16) return launched(vla::launch_delta_step(a, d_k, d_v, io_dtype, s));
+  if (op.saved != nullptr) {
+    a.n_kept = kept_states(T);
+    a.kept = static_cast<float*>(op.saved);
+    a.rows = reinterpret_cast<float*>(static_cast<char*>(op.saved) + kept_bytes(static_cast<long long>(B) * H_v, T, d_k, d_v));
+  }
+  if (T < 16 && op.saved == nullptr) return launched(vla::launch_delta_step(a, d_k, d_v, io_dtype, s));
   Segments seg = delta_segments(static_cast<long long>(B) * H_v, T, d_k, d_v, op.segments);
   if (seg.n == 1 || workspace == nullptr || workspace_bytes < seg.bytes) return launched(launch_blocks(a, d_k, d_v, io_dtype, false, s));
   a.n_seg = seg.n;
@@ -207,7 +259,7 @@ int vla_delta_forward(const void* q, const void* k, const void* v, const float* 
   vla::DeltaArgs maps = a;
   maps.S0 = nullptr;
   hipError_t err = launch_blocks(maps, d_k, d_v, io_dtype, true, s);
-  if (err == hipSuccess) err = vla::launch_delta_combine(a, states, d_k, d_v, s);
+  if (err == hipSuccess) err = vla::launch_delta_combine(a, states, d_k, d_v, false, s);
   if (err != hipSuccess) return launched(err);
   a.S0 = states;
   a.seg_states = true;
@@ -218,6 +270,84 @@ int vla_delta_decode_step(const void* q, const void* k, const void* v, const flo
                           int H_k, int H_v, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts, void* stream) {
   if (S == nullptr) return VLA_ERR_INVALID_ARG;
   return vla_delta_forward(q, k, v, g, beta, S, o, S, B, H_k, H_v, 1, d_k, d_v, io_dtype, opts, nullptr, 0, stream);
+}
+
+int vla_delta_backward(const void* q, const void* k, const void* v, const float* g, const float* beta, const void* dO, const float* dS_T,
+                       void* dq, void* dk, void* dv, float* dg, float* dbeta, float* dS0, int B, int H_k, int H_v, int T, int d_k,
+                       int d_v, int io_dtype, const vla_delta_opts* opts, void* workspace, size_t workspace_bytes, void* stream) {
+  const vla_delta_opts op = delta_opts(opts, d_k);
+  const int st = check_delta(B, H_k, H_v, T, d_k, d_v, io_dtype, op);
+  if (st != VLA_OK) return st;
+  const void* needed[] = {q, k, v, g, beta, dO, dq, dk, dv, dg, dbeta, op.saved};
+  for (const void* p : needed) {
+    if (T > 0 && p == nullptr) return VLA_ERR_INVALID_ARG;
+  }
+  const void* ptrs[] = {q, k, v, dO, dS_T, dq, dk, dv, dS0, op.saved, workspace};
+  for (const void* p : ptrs) {
+    if (!aligned16(p)) return VLA_ERR_INVALID_ARG;
+  }
+  const size_t es = io_dtype == VLA_BF16 ? 2 : 4;
+  const int per16 = static_cast<int>(16 / es);
+  vla::DeltaArgs a{};
+  if (!rows_of(op.q, H_k, T, d_k, per16, &a.qs) || !rows_of(op.k, H_k, T, d_k, per16, &a.ks) || !rows_of(op.v, H_v, T, d_v, per16, &a.vs) ||
+      !rows_of(op.o, H_v, T, d_v, per16, &a.os) || !rows_of(op.dq, H_k, T, d_k, per16, &a.dqs) || !rows_of(op.dk, H_k, T, d_k, per16, &a.dks) ||
+      !rows_of(op.dv, H_v, T, d_v, per16, &a.dvs) || !gate_rows(op.g, H_v, T, &a.gs) || !gate_rows(op.beta, H_v, T, &a.bs) ||
+      !tokens_apart(a.qs, T, d_k) || !tokens_apart(a.ks, T, d_k) || !tokens_apart(a.vs, T, d_v) || !tokens_apart(a.os, T, d_v) ||
+      !rows_apart(a.dqs, B, H_k, T, d_k) || !rows_apart(a.dks, B, H_k, T, d_k) || !rows_apart(a.dvs, B, H_v, T, d_v)) {
+    return VLA_ERR_INVALID_ARG;
+  }
+  for (const vla::Rows* r : {&a.qs, &a.ks, &a.vs, &a.os, &a.dqs, &a.dks, &a.dvs}) {
+    if (!rows_near(*r, es)) return VLA_ERR_UNSUPPORTED;
+  }
+  const long long heads = static_cast<long long>(B) * H_v;
+  const BackwardParts parts = backward_parts(heads, T, d_k, d_v, H_v != H_k, op.segments);
+  const size_t nS = static_cast<size_t>(heads) * d_v * d_k * 4, nG = static_cast<size_t>(heads) * T * 4;
+  const size_t saved = vla_delta_saved_bytes(B, H_v, T, d_k, d_v, io_dtype);
+  const Range r[] = {{q, reach(a.qs, B, H_k, T, d_k, es), false}, {k, reach(a.ks, B, H_k, T, d_k, es), false},
+                     {v, reach(a.vs, B, H_v, T, d_v, es), false}, {g, reach(a.gs, B, H_v, T, 1, 4), false},
+                     {beta, reach(a.bs, B, H_v, T, 1, 4), false}, {op.lengths, static_cast<size_t>(B) * 4, false},
+                     {dO, reach(a.os, B, H_v, T, d_v, es), false}, {dS_T, nS, false}, {op.saved, saved, false},
+                     {dq, reach(a.dqs, B, H_k, T, d_k, es), true}, {dk, reach(a.dks, B, H_k, T, d_k, es), true},
+                     {dv, reach(a.dvs, B, H_v, T, d_v, es), true}, {dg, nG, true}, {dbeta, nG, true}, {dS0, nS, true},
+                     {workspace, parts.bytes, true}};
+  if (!disjoint(r, 16, nullptr, nullptr)) return VLA_ERR_INVALID_ARG;
+  if (op.saved_bytes < saved || (parts.bytes > 0 && (workspace == nullptr || workspace_bytes < parts.bytes))) return VLA_ERR_WORKSPACE;
+  if (T == 0 && dS0 == nullptr) return VLA_OK;
+  char* ws = static_cast<char*>(workspace);
+  const auto at = [&](size_t offset) { return reinterpret_cast<float*>(ws + offset); };
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.dO = dO; a.S0 = dS_T; a.S_T = dS0; a.dv = dv;
+  a.lengths = op.lengths;
+  a.B = B; a.H_k = H_k; a.H_v = H_v; a.T = T;
+  a.scale = op.scale;
+  a.kept = at(parts.kept);
+  a.rows = at(parts.rows);
+  a.n_kept = kept_states(T);
+  a.n_seg = parts.seg.n;
+  a.seg_tokens = parts.seg.tokens;
+  // W, dv, the state's gradient at the places that are kept
+  vla::DeltaArgs chain = a;
+  hipError_t err = hipSuccess;
+  if (a.n_seg > 1) {
+    chain.seg_map = at(parts.seg_map);
+    vla::DeltaArgs maps = chain;
+    maps.S0 = nullptr;
+    err = launch_reverse(maps, d_k, d_v, io_dtype, true, s);
+    if (err == hipSuccess) err = vla::launch_delta_combine(chain, at(parts.seg_S), d_k, d_v, true, s);
+    chain.S0 = at(parts.seg_S);
+    chain.seg_states = true;
+  }
+  if (err == hipSuccess) err = launch_reverse(chain, d_k, d_v, io_dtype, false, s);
+  if (err != hipSuccess || T == 0) return launched(err);
+  // the other gradients
+  a.kept_state = static_cast<const float*>(op.saved);
+  a.R = reinterpret_cast<const float*>(static_cast<const char*>(op.saved) + kept_bytes(heads, T, d_k, d_v));
+  a.dq = dq; a.dk = dk; a.dg = dg; a.dbeta = dbeta;
+  a.dk_part = at(parts.dk);
+  a.dq_part = H_v != H_k ? at(parts.dq) : nullptr;
+  err = launch_grad(a, d_k, d_v, io_dtype, s);
+  if (err == hipSuccess && H_v != H_k) err = vla::launch_delta_shared(a, d_k, io_dtype, s);
+  return launched(err);
 }
 
 // ---- norm of queries and keys with the position rotation

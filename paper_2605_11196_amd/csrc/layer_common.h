@@ -33,6 +33,8 @@ constexpr int kNormPartials = 1024;   // workgroups of the backward pass at most
 hipError_t launch_qk_norm_rope(const NormArgs& a, int d, int io_dtype, bool interleaved, hipStream_t stream);
 hipError_t launch_qk_norm_rope_backward(const NormArgs& a, int d, int io_dtype, bool interleaved, hipStream_t stream);
 
+constexpr int kKeep = 256;   // tokens between two states that are kept for the backward pass
+
 struct DeltaArgs {
   const void* q;
   const void* k;
@@ -46,8 +48,22 @@ struct DeltaArgs {
   Rows qs, ks, vs, os, gs, bs;
   int B, H_k, H_v, T;
   float scale;
-  float* saved;            // [B * H_v][n_blocks][d_v][d_k] or nullptr: the state at the start of every block of 32 tokens
-  int n_blocks;
+  // for the backward pass, or nullptr
+  float* kept;             // [B * H_v][n_kept][d_v][d_k]: the state at the start of every 256 tokens (backward: its gradient at their end)
+  float* rows;             // [B * H_v][T][d_v]: R, beta R is what a token writes (backward: W, beta W is the gradient of v)
+  int n_kept;
+  // backward
+  const void* dO;          // strides os
+  void* dv;
+  void* dq;                // share of a value head: [B * H_v][T][d_k] float32 where heads share a key head, else by strides
+  void* dk;
+  Rows dvs, dqs, dks;
+  const float* kept_state; // of the forward pass: kept, rows
+  const float* R;
+  float* dk_part;          // [B * H_v][T][d_k]: what the sweep along the tokens gives of dk
+  float* dq_part;          // the same of dq, where heads share a key head
+  float* dg;               // [B * H_v][T]
+  float* dbeta;
   // time segments
   int n_seg, seg_tokens;
   bool seg_states;         // S0 holds a state for each segment: [B * H_v][n_seg][d_v][d_k]
@@ -64,7 +80,23 @@ hipError_t launch_delta_chunk_96(const DeltaArgs& a, int d_v, int io_dtype, bool
 hipError_t launch_delta_chunk_128(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
 
 // seg_S[h][0] = S0[h], seg_S[h][s + 1] = seg_S[h][s] X + Y of segment s (delta_combine.hip)
-hipError_t launch_delta_combine(const DeltaArgs& a, float* seg_S, int d_k, int d_v, hipStream_t stream);
+// (backward: seg_S[h][n_seg - 1] = S0[h], seg_S[h][s - 1] = seg_S[h][s] X + Y of segment s)
+hipError_t launch_delta_combine(const DeltaArgs& a, float* seg_S, int d_k, int d_v, bool backward, hipStream_t stream);
+
+// The chain of the state's gradient from the last block to the first (delta_reverse.h): S0 is the gradient of S_T and S_T that of S0.
+hipError_t launch_delta_reverse_16(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
+hipError_t launch_delta_reverse_32(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
+hipError_t launch_delta_reverse_64(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
+hipError_t launch_delta_reverse_96(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
+hipError_t launch_delta_reverse_128(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
+
+// The gradients of q, k, g and beta, every 256 tokens at once (delta_grad.h), and the sum over the heads that share a key head.
+hipError_t launch_delta_grad_16(const DeltaArgs& a, int d_v, int io_dtype, hipStream_t stream);
+hipError_t launch_delta_grad_32(const DeltaArgs& a, int d_v, int io_dtype, hipStream_t stream);
+hipError_t launch_delta_grad_64(const DeltaArgs& a, int d_v, int io_dtype, hipStream_t stream);
+hipError_t launch_delta_grad_96(const DeltaArgs& a, int d_v, int io_dtype, hipStream_t stream);
+hipError_t launch_delta_grad_128(const DeltaArgs& a, int d_v, int io_dtype, hipStream_t stream);
+hipError_t launch_delta_shared(const DeltaArgs& a, int d_k, int io_dtype, hipStream_t stream);
 
 inline bool layer_head_size(int d) { return d == 16 || d == 32 || d == 64 || d == 96 || d == 128; }
 

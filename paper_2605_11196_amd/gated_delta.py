@@ -103,7 +103,7 @@ def gated_delta_decode_step(q, k, v, g, beta, S, *, scale=None, stream=None):
     return o
 
 
-def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, lengths=None, stream=None):
+def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, lengths=None, segments=0, stream=None):
     """The gradients (dq, dk, dv, dg, dbeta, dS0) of gated_delta_forward's inputs, given those of o and S_T (None: zero), the same inputs
     and what it saved.  dg, dbeta and dS0 are float32."""
     import torch
@@ -115,7 +115,7 @@ def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, 
     lib = binding.load_library()
     handle, context, outside = binding._on_stream(torch, dev, stream)
     with context:
-        kept, op = _inputs(q, k, v, g, beta, scale, lengths)
+        kept, op = _inputs(q, k, v, g, beta, scale, lengths, segments)
         do = _rows(do)
         dq, dk_, dv_ = _like(torch, q), _like(torch, k), _like(torch, v)
         dg, dbeta = (torch.empty((B, H_v, T), dtype=torch.float32, device=dev) for _ in range(2))
