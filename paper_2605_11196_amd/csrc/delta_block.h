@@ -137,9 +137,7 @@ template <> struct Ops<uint16_t> {
   static __device__ __forceinline__ f4 mul_tok_raw(const TA& a, Raw b, f4 acc) {
     return mfma_bf16(a.hm, cat(b, b), mfma_bf16(a.lh, cat(b, u2{0, 0}), acc));
   }
-  static __device__ __forceinline__ f4 mul_tok_out(const TA& a, const TB& b, f4 acc) {
-    return mfma_bf16(a.hm, b.hm, mfma_bf16(a.hm, b.mh, acc));
-  }
+  static __device__ __forceinline__ f4 mul_tok_out(u4 a, const TB& b, f4 acc) { return mfma_bf16(a, b.hm, mfma_bf16(a, b.mh, acc)); }
 };
 
 // float32 numbers, products on the FP32 matrix instruction
@@ -264,7 +262,7 @@ __device__ __forceinline__ void store_column(__amdgpu_buffer_rsrc_t r, int at, i
 
 // The decays of a block.  G is summed in float64 and kept as a float32 pair, in units of log 2: differences stay exact to some 2^-24
 // however far G runs, as it does after a token that forgets the state (g is held at -10000, whose exponential is 0 all the same).
-struct Gates {
+struct __align__(16) Gates {
   float hi[kTok], lo[kTok];
   float gamma[kTok];    // exp(G_i)
   float rest[kTok];     // exp(G_end - G_i)
@@ -349,6 +347,58 @@ __device__ __forceinline__ void invert_tile(f4 x, float* m, typename Ops<IO>::Im
 #pragma unroll
   for (int r = 0; r < 4; ++r) mine[r] = g < 2 ? (g == 0 ? t[r] : t[4 + r]) : (g == 2 ? t[8 + r] : t[12 + r]);
   Ops<IO>::put(out, c, g, mine);
+}
+
+// The matrices between the tokens of a block, tile by tile on different waves, as left operands of the products that follow:
+//   inverse  (I + M)^-1 of the diagonal tiles,  below  -M of the tiles below,  att  A (with ATT)
+// Products are transposed, so that a lane has four tokens j of row i.  REVERSE: rows are the block's tokens with the last one first, M =
+// exp(G_j - G_i) (k_i . k_j) beta_j of them, A = scale exp(G_j - G_i) (q_j . k_i).
+template <typename IO, class RK, int PAIRS, int WAVES, bool REVERSE, bool ATT, typename AttImage>
+__device__ __forceinline__ void token_matrices(const u4* sK, const u4* sQ, const Gates& gates, typename Ops<IO>::Image* inverse,
+                                               typename Ops<IO>::Image* below, AttImage* att, float (*scratch)[16 * 20], float scale, int wave, int c, int g) {
+  using O = Ops<IO>;
+  constexpr int TILES = kTiles * (kTiles + 1) / 2;
+  for (int job = wave; job < (ATT ? 2 : 1) * TILES; job += WAVES) {
+    // the diagonal tiles of k k^T first: their inverses take longest
+    const bool keys = job < TILES;
+    int p = keys ? job : job - TILES, i, j;
+    if (p < kTiles) {
+      i = j = p;
+    } else {
+      p -= kTiles;
+      i = 1;
+      while (p >= i) p -= i++;
+      j = p;
+    }
+    const u4* from_j = REVERSE && !keys ? sQ : sK;
+    const u4* from_i = !REVERSE && !keys ? sQ : sK;
+    typename O::A rj[PAIRS], ri[PAIRS];
+#pragma unroll
+    for (int s = 0; s < PAIRS; ++s) {
+      rj[s] = O::template rows<RK>(from_j, j, s, c, g);
+      ri[s] = O::template rows<RK>(from_i, i, s, c, g);
+    }
+    const float hi = gates.hi[16 * i + c], lo = gates.lo[16 * i + c];
+    const f4 hj = *reinterpret_cast<const f4*>(&gates.hi[16 * j + 4 * g]), lj = *reinterpret_cast<const f4*>(&gates.lo[16 * j + 4 * g]);
+    const f4 bj = *reinterpret_cast<const f4*>(&gates.beta[16 * j + 4 * g]);
+    f4 x = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < PAIRS; ++s) x = O::mul_rows(rj[s], ri[s], x);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int before = i - j > 0 ? 1 : (keys ? c - (4 * g + r) : c - (4 * g + r) + 1);   // > 0: token j counts for token i
+      const float apart = REVERSE ? (hj[r] - hi) + (lj[r] - lo) : (hi - hj[r]) + (lo - lj[r]);
+      const float w = __builtin_amdgcn_exp2f(apart) * (keys ? -bj[r] : (REVERSE ? scale : scale * bj[r]));
+      x[r] = before > 0 ? x[r] * w : 0.0f;
+    }
+    if (keys && i == j) {
+      invert_tile<IO>(x, scratch[i], inverse[i], c, g);
+    } else if (keys) {
+      O::put(below[i * (i - 1) / 2 + j], c, g, x);
+    } else if constexpr (ATT) {
+      O::put(att[i * (i + 1) / 2 + j], c, g, x);
+    }
+  }
 }
 
 }  // namespace delta

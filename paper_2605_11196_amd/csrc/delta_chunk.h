@@ -1,9 +1,8 @@
 // The gated delta rule in blocks of 32 tokens (delta_block.h has the mathematics): one workgroup per head (and time segment) goes
 // through the blocks with the state on registers.
 //
-// A wave has 32 rows of S (16 where they do not divide); the four waves of d_v = 128 share the matrices between tokens: they are
-// formed once, with the inverses of the diagonal tiles, by different waves at once, beside the products of K and Q with the state.
-// Three barriers a block: rows staged, matrices ready, rows no longer needed.
+// A wave has 16 rows of S; the waves of a head share the matrices between tokens, which different waves form at once, beside the products
+// of K and Q with the state.  Three barriers a block: rows staged; matrices ready; rows no longer needed.
 //
 // MAP: the affine map of a segment instead of its outputs, S_end = S_start X + Y: Y from d_v columns that start from zero, X from d_k
 // columns without values that start from the identity.
@@ -17,8 +16,7 @@ namespace delta {
 template <int DK, int DV, bool MAP>
 struct Shape {
   static constexpr int COLS = DV + (MAP ? DK : 0);
-  static constexpr int NT = 1;           // column tiles of a wave
-  static constexpr int WAVES = COLS / (16 * NT);
+  static constexpr int WAVES = COLS / 16;
   static constexpr int THREADS = 64 * WAVES;
   static constexpr int DKP = DK < 32 ? 32 : DK;               // key columns in pairs of tiles
   static constexpr int KT = DKP / 16;
@@ -28,16 +26,17 @@ template <typename IO, int DK, int DV, bool MAP>
 __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_kernel(DeltaArgs a) {
   using Sh = Shape<DK, DV, MAP>;
   using O = Ops<IO>;
-  constexpr int NT = Sh::NT, KT = Sh::KT, WAVES = Sh::WAVES, THREADS = Sh::THREADS;
+  constexpr int KT = Sh::KT, WAVES = Sh::WAVES, THREADS = Sh::THREADS;
   constexpr int PK = DK / O::PER16, PV = DV / O::PER16;
   using RK = PieceRows<Sh::DKP / O::PER16>;
   using RV = PieceRows<PV>;
   __shared__ u4 sK[kTok * RK::STRIDE];
   __shared__ u4 sQ[MAP ? 1 : kTok * RK::STRIDE];
   __shared__ u4 sV[kTok * RV::STRIDE];
-  __shared__ typename O::Image inverse[kTiles], below[kTiles * (kTiles - 1) / 2], att[MAP ? 1 : kTiles * (kTiles + 1) / 2];
-  __shared__ __align__(16) float diagonal[kTiles][16 * 20];
-  __shared__ Gates gate_pair[2];
+  __shared__ typename O::Image inverse[kTiles], below[kTiles * (kTiles - 1) / 2];
+  __shared__ typename O::ImageOut att[MAP ? 1 : kTiles * (kTiles + 1) / 2];
+  __shared__ __align__(16) float scratch[kTiles][16 * 20];
+  __shared__ Gates gates[2];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   int c = lane % 16, g = lane / 16;
@@ -53,26 +52,23 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
   const float* gp = a.g + b * a.gs.b + h * a.gs.h;
   const float* bp = a.beta + b * a.bs.b + h * a.bs.h;
   const typename O::One one = O::one(c, g);
-  const int col0 = wave * 16 * NT + c;      // first column of this lane
+  const int col = wave * 16 + c;            // column of this lane
+  const f4 zero = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
   // ---- the state: tile kt holds key columns 32 (kt / 2) + 8 g + 4 (kt % 2) + r
-  f4 S[NT][KT];
+  f4 S[KT];
   const float* S0 = a.S0 ? a.S0 + (static_cast<size_t>(head) * (a.seg_states ? a.n_seg : 1) + (a.seg_states ? seg : 0)) * DV * DK : nullptr;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int col = col0 + 16 * n;
+  for (int kt = 0; kt < KT; ++kt) {
+    const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
+    S[kt] = zero;
+    if ((DK == Sh::DKP || dk < DK) && (!MAP || col < DV) && S0 != nullptr) S[kt] = *reinterpret_cast<const f4*>(S0 + static_cast<size_t>(col) * DK + dk);
+    if (MAP && col >= DV) {
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-      S[n][kt] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-      if ((DK == Sh::DKP || dk < DK) && (!MAP || col < DV) && S0 != nullptr) S[n][kt] = *reinterpret_cast<const f4*>(S0 + static_cast<size_t>(col) * DK + dk);
-      if (MAP && col >= DV) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[n][kt][r] = col - DV == dk + r ? 1.0f : 0.0f;
-      }
+      for (int r = 0; r < 4; ++r) S[kt][r] = col - DV == dk + r ? 1.0f : 0.0f;
     }
   }
-  if constexpr (Sh::DKP > DK) {            // columns that no row fills
+  if constexpr (Sh::DKP > DK) {             // columns that no row fills
     for (int i = threadIdx.x; i < kTok * RK::STRIDE; i += THREADS) {
       sK[i] = u4{0, 0, 0, 0};
       if constexpr (!MAP) sQ[i] = u4{0, 0, 0, 0};
@@ -85,14 +81,14 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
   stK.init(k_step);
   if constexpr (!MAP) stQ.init(q_step);
   stV.init(v_step);
-  float gate = 0.0f, beta = 0.0f;   // of one token a lane, a block ahead of the rows
+  float gate = 0.0f, beta = 0.0f;           // of one token a lane, a block ahead of the rows
   auto request = [&](int t0) {
     stK.load(k, k_step, t0, end);
     if constexpr (!MAP) stQ.load(q, q_step, t0, end);
     stV.load(v, v_step, t0, end);
   };
   auto request_gates = [&](int t0) {
-    const int t = min(t0 + (lane & (kTok - 1)), end - 1);
+    const int t = max(min(t0 + (lane & (kTok - 1)), end - 1), first);
     gate = gp[t * a.gs.t];
     beta = bp[t * a.bs.t];
   };
@@ -102,7 +98,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
   if (first < end) {
     request_gates(first);
     request(first);
-    next_gates(first, gate_pair[0]);
+    next_gates(first, gates[0]);
     request_gates(first + kTok);
   }
   int turn = 0;
@@ -112,163 +108,87 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
     if (!MAP && a.kept != nullptr && t0 % kKeep == 0) {
       float* out = a.kept + (static_cast<size_t>(head) * a.n_kept + t0 / kKeep) * DV * DK;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-          const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-          if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col0 + 16 * n) * DK + dk) = S[n][kt];
-        }
+      for (int kt = 0; kt < KT; ++kt) {
+        const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
+        if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col) * DK + dk) = S[kt];
       }
     }
     const int stop = min(end, (t0 / kKeep + 1) * kKeep);
     for (; t0 < stop; t0 += kTok) {
-    // the LDS addresses are formed anew in each block: kept over the loop they would take the registers of the state
-    asm volatile("" : "+v"(c), "+v"(g));
-    stK.template store<RK>(sK);
-    if constexpr (!MAP) stQ.template store<RK>(sQ);
-    stV.template store<RV>(sV);
-    const Gates& gates = gate_pair[turn];
-    turn ^= 1;
-    __syncthreads();
+      // the LDS addresses are formed anew in each block: kept over the loop they would take the registers of the state
+      asm volatile("" : "+v"(c), "+v"(g));
+      stK.template store<RK>(sK);
+      if constexpr (!MAP) stQ.template store<RK>(sQ);
+      stV.template store<RV>(sV);
+      const Gates& gt = gates[turn];
+      turn ^= 1;
+      __syncthreads();
+      token_matrices<IO, RK, KT / 2, WAVES, false, !MAP>(sK, sQ, gt, inverse, below, att, scratch, a.scale, wave, c, g);
 
-    // ---- matrices between tokens, tile (i, j), j <= i: transposed products, so that a lane has four tokens j of row i = c
-    constexpr int PAIRS = kTiles * (kTiles + 1) / 2;
-    for (int job = wave; job < (MAP ? 1 : 2) * PAIRS; job += WAVES) {
-      // the diagonal tiles of k k^T first: their inverses take longest
-      const bool keys = job < PAIRS;
-      int p = keys ? job : job - PAIRS, i, j;
-      if (p < kTiles) {
-        i = j = p;
-      } else {
-        p -= kTiles;
-        i = 1;
-        while (p >= i) p -= i++;
-        j = p;
-      }
-      f4 x = f4{0.0f, 0.0f, 0.0f, 0.0f};
+      // ---- P = K S^T, Q S^T
+      f4 P[kTiles] = {zero, zero}, QS[kTiles] = {zero, zero};
 #pragma unroll
       for (int s = 0; s < KT / 2; ++s) {
-        x = O::mul_rows(O::template rows<RK>(sK, j, s, c, g), O::template rows<RK>(keys || MAP ? sK : sQ, i, s, c, g), x);
-      }
-      const float hi = gates.hi[16 * i + c], lo = gates.lo[16 * i + c];
-      const f4 hj = *reinterpret_cast<const f4*>(&gates.hi[16 * j + 4 * g]), lj = *reinterpret_cast<const f4*>(&gates.lo[16 * j + 4 * g]);
-      const f4 bj = *reinterpret_cast<const f4*>(&gates.beta[16 * j + 4 * g]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int before = i - j > 0 ? 1 : (keys ? c - (4 * g + r) : c - (4 * g + r) + 1);   // > 0: token j counts for token i
-        const float w = bj[r] * __builtin_amdgcn_exp2f((hi - hj[r]) + (lo - lj[r])) * (keys ? -1.0f : a.scale);
-        x[r] = before > 0 ? x[r] * w : 0.0f;
-      }
-      if (keys && i == j) {
-        invert_tile<IO>(x, diagonal[i], inverse[i], c, g);
-      } else if (keys) {
-        O::put(below[i * (i - 1) / 2 + j], c, g, x);
-      } else {
-        O::put(att[i * (i + 1) / 2 + j], c, g, x);
-      }
-    }
-
-    // ---- P = K S^T, Q S^T
-    f4 P[NT][kTiles], QS[NT][kTiles];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i) P[n][i] = QS[n][i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-#pragma unroll
-    for (int s = 0; s < KT / 2; ++s) {
-      typename O::A ka[kTiles], qa[kTiles];
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        ka[i] = O::template rows<RK>(sK, i, s, c, g);
-        if constexpr (!MAP) qa[i] = O::template rows<RK>(sQ, i, s, c, g);
-      }
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const typename O::B x = O::pair(S[n][2 * s], S[n][2 * s + 1], one);
+        typename O::A ka[kTiles], qa[kTiles];
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
-          P[n][i] = O::mul(ka[i], x, P[n][i]);
-          if constexpr (!MAP) QS[n][i] = O::mul_out(qa[i], x, QS[n][i]);
+          ka[i] = O::template rows<RK>(sK, i, s, c, g);
+          if constexpr (!MAP) qa[i] = O::template rows<RK>(sQ, i, s, c, g);
+        }
+        const typename O::B x = O::pair(S[2 * s], S[2 * s + 1], one);
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          P[i] = O::mul(ka[i], x, P[i]);
+          if constexpr (!MAP) QS[i] = O::mul_out(qa[i], x, QS[i]);
         }
       }
-    }
-    __syncthreads();
-    if (t0 + kTok < end) request(t0 + kTok);
+      __syncthreads();
+      if (t0 + kTok < end) request(t0 + kTok);
 
-    // ---- what is written, the read-out, the state
-    const float decay = gates.end;
-    f4 R[NT][kTiles];
-    typename O::TB rb[NT][kTiles];
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      const f4 gamma = *reinterpret_cast<const f4*>(&gates.gamma[16 * i + 4 * g]);
-      const typename O::TA inv = O::image(inverse[i], c, g);
-      f4 x[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        x[n] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (!MAP || wave * 16 * NT + 16 * n < DV) x[n] = O::template tile<RV>(sV, wave * NT + n, i, c, g);
-        x[n] -= gamma * P[n][i];
-      }
-#pragma unroll
-      for (int j = 0; j < i; ++j) {
-        const typename O::TA m = O::image(below[i * (i - 1) / 2 + j], c, g);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) x[n] = O::mul_tok(m, rb[n][j], x[n]);
-      }
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        R[n][i] = O::mul_tok(inv, O::tokens(x[n], one), f4{0.0f, 0.0f, 0.0f, 0.0f});
-        if (!MAP || i + 1 < kTiles) rb[n][i] = O::tokens(R[n][i], one);
-      }
-    }
-    if (!MAP && a.rows != nullptr) {
-      const __amdgpu_buffer_rsrc_t out = rows_buffer(a.rows + (static_cast<size_t>(head) * a.T + t0) * DV, DV * 4, last - t0, DV * 4);
+      // ---- what is written, the read-out, the state
+      const auto gate4 = [&](const float* from, int tile) { return *reinterpret_cast<const f4*>(from + 16 * tile + 4 * g); };
+      static_assert(kTiles == 2, "one pair of token tiles");
+      // what comes from LDS is asked for well before it is used: the compiler keeps that order
+      f4 R[kTiles], gamma[kTiles];
+      typename O::TB rb[kTiles];
+      typename O::TA inv[kTiles];
+      typename O::Raw vr[kTiles] = {};
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) store_column(out, ((16 * i + 4 * g) * DV + col0 + 16 * n) * 4, DV * 4, R[n][i], static_cast<float*>(nullptr));
+        gamma[i] = gate4(gt.gamma, i);
+        inv[i] = O::image(inverse[i], c, g);
+        if (!MAP || wave * 16 < DV) vr[i] = O::template tile_raw<RV>(sV, wave, i, c, g);
       }
-    }
-    typename O::B w[NT];
-    static_assert(kTiles == 2, "one pair of token tiles");
-    {
-      const f4 w0 = *reinterpret_cast<const f4*>(&gates.rest[4 * g]) * *reinterpret_cast<const f4*>(&gates.beta[4 * g]);
-      const f4 w1 = *reinterpret_cast<const f4*>(&gates.rest[16 + 4 * g]) * *reinterpret_cast<const f4*>(&gates.beta[16 + 4 * g]);
+      const typename O::TA under = O::image(below[0], c, g);
+      R[0] = O::mul_tok(inv[0], O::tokens(O::value(vr[0]) - gamma[0] * P[0], one), zero);
+      const f4 w0 = gate4(gt.rest, 0) * gate4(gt.beta, 0), w1 = gate4(gt.rest, 1) * gate4(gt.beta, 1);
+      rb[0] = O::tokens(R[0], one);
+      R[1] = O::mul_tok(inv[1], O::tokens(O::mul_tok(under, rb[0], O::value(vr[1]) - gamma[1] * P[1]), one), zero);
+      if (!MAP) rb[1] = O::tokens(R[1], one);
+      if (!MAP && a.rows != nullptr) {
+        const __amdgpu_buffer_rsrc_t out = rows_buffer(a.rows + (static_cast<size_t>(head) * a.T + t0) * DV, DV * 4, last - t0, DV * 4);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) w[n] = O::pair(R[n][0] * w0, R[n][1] * w1, one);
-    }
-    if constexpr (!MAP) {
-      const __amdgpu_buffer_rsrc_t out = rows_buffer(o + t0 * o_step, o_step, last - t0, DV * static_cast<int>(sizeof(IO)));
+        for (int i = 0; i < kTiles; ++i) store_column(out, ((16 * i + 4 * g) * DV + col) * 4, DV * 4, R[i], static_cast<float*>(nullptr));
+      }
+      const typename O::B w = O::pair(R[0] * w0, R[1] * w1, one);
+      if constexpr (!MAP) {
+        const decltype(O::image(att[0], c, g)) at[3] = {O::image(att[0], c, g), O::image(att[1], c, g), O::image(att[2], c, g)};
+        const __amdgpu_buffer_rsrc_t out = rows_buffer(o + t0 * o_step, o_step, last - t0, DV * static_cast<int>(sizeof(IO)));
 #pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        const f4 gamma = *reinterpret_cast<const f4*>(&gates.gamma[16 * i + 4 * g]) * a.scale;
-        f4 x[NT];
+        for (int i = 0; i < kTiles; ++i) {
+          f4 x = gamma[i] * a.scale * QS[i];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) x[n] = gamma * QS[n][i];
-#pragma unroll
-        for (int j = 0; j <= i; ++j) {
-          const typename O::TA m = O::image(att[i * (i + 1) / 2 + j], c, g);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) x[n] = O::mul_tok_out(m, rb[n][j], x[n]);
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          store_column(out, (16 * i + 4 * g) * static_cast<int>(o_step) + (col0 + 16 * n) * static_cast<int>(sizeof(IO)), static_cast<int>(o_step), x[n],
+          for (int j = 0; j <= i; ++j) x = O::mul_tok_out(at[i + j], rb[j], x);
+          store_column(out, (16 * i + 4 * g) * static_cast<int>(o_step) + col * static_cast<int>(sizeof(IO)), static_cast<int>(o_step), x,
                        static_cast<IO*>(nullptr));
         }
       }
-    }
+      const float decay = gt.end;
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      const typename O::A kc = O::template columns<RK>(sK, kt, 0, c, g);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) S[n][kt] = O::mul(kc, w[n], S[n][kt] * decay);
-    }
-    next_gates(t0 + kTok, gate_pair[turn]);
-    request_gates(t0 + 2 * kTok);
-    __syncthreads();
+      for (int kt = 0; kt < KT; ++kt) S[kt] = O::mul(O::template columns<RK>(sK, kt, 0, c, g), w, S[kt] * decay);
+      next_gates(t0 + kTok, gates[turn]);
+      request_gates(t0 + 2 * kTok);
+      __syncthreads();
     }
   }
 
@@ -284,12 +204,9 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
   else if (a.S_T != nullptr && seg == a.n_seg - 1) out = a.S_T + static_cast<size_t>(head) * DV * DK;
   if (out == nullptr) return;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-      if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col0 + 16 * n) * DK + dk) = S[n][kt];
-    }
+  for (int kt = 0; kt < KT; ++kt) {
+    const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
+    if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col) * DK + dk) = S[kt];
   }
 }
 

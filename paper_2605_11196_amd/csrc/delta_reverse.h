@@ -18,7 +18,7 @@ template <typename IO, int DK, int DV, bool MAP>
 __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_reverse_kernel(DeltaArgs a) {
   using Sh = Shape<DK, DV, MAP>;
   using O = Ops<IO>;
-  constexpr int NT = Sh::NT, KT = Sh::KT, WAVES = Sh::WAVES, THREADS = Sh::THREADS;
+  constexpr int KT = Sh::KT, WAVES = Sh::WAVES, THREADS = Sh::THREADS;
   constexpr int PK = DK / O::PER16, PV = DV / O::PER16;
   using RK = PieceRows<Sh::DKP / O::PER16>;
   using RV = PieceRows<PV>;
@@ -26,8 +26,8 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
   __shared__ u4 sQ[kTok * RK::STRIDE];
   __shared__ u4 sD[kTok * RV::STRIDE];
   __shared__ typename O::Image inverse[kTiles], below[kTiles * (kTiles - 1) / 2], att[kTiles * (kTiles + 1) / 2];
-  __shared__ __align__(16) float diagonal[kTiles][16 * 20];
-  __shared__ Gates gate_pair[2];
+  __shared__ __align__(16) float scratch[kTiles][16 * 20];
+  __shared__ Gates gates[2];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   int c = lane % 16, g = lane / 16;
@@ -43,26 +43,23 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
   const float* gp = a.g + b * a.gs.b + h * a.gs.h;
   const float* bp = a.beta + b * a.bs.b + h * a.bs.h;
   const typename O::One one = O::one(c, g);
-  const int col0 = wave * 16 * NT + c;      // first column of this lane
+  const int col = wave * 16 + c;            // column of this lane
+  const f4 zero = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
   // ---- the state: tile kt holds key columns 32 (kt / 2) + 8 g + 4 (kt % 2) + r
-  f4 S[NT][KT];
+  f4 S[KT];
   const float* S0 = a.S0 ? a.S0 + (static_cast<size_t>(head) * (a.seg_states ? a.n_seg : 1) + (a.seg_states ? seg : 0)) * DV * DK : nullptr;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int col = col0 + 16 * n;
+  for (int kt = 0; kt < KT; ++kt) {
+    const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
+    S[kt] = zero;
+    if ((DK == Sh::DKP || dk < DK) && (!MAP || col < DV) && S0 != nullptr) S[kt] = *reinterpret_cast<const f4*>(S0 + static_cast<size_t>(col) * DK + dk);
+    if (MAP && col >= DV) {
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-      S[n][kt] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-      if ((DK == Sh::DKP || dk < DK) && (!MAP || col < DV) && S0 != nullptr) S[n][kt] = *reinterpret_cast<const f4*>(S0 + static_cast<size_t>(col) * DK + dk);
-      if (MAP && col >= DV) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[n][kt][r] = col - DV == dk + r ? 1.0f : 0.0f;
-      }
+      for (int r = 0; r < 4; ++r) S[kt][r] = col - DV == dk + r ? 1.0f : 0.0f;
     }
   }
-  if constexpr (Sh::DKP > DK) {            // columns that no row fills
+  if constexpr (Sh::DKP > DK) {             // columns that no row fills
     for (int i = threadIdx.x; i < kTok * RK::STRIDE; i += THREADS) {
       sK[i] = u4{0, 0, 0, 0};
       sQ[i] = u4{0, 0, 0, 0};
@@ -75,7 +72,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
   stK.init_reversed(k_step);
   stQ.init_reversed(q_step);
   stD.init_reversed(o_step);
-  float gate = 0.0f, beta = 0.0f;   // of one token a lane, a block ahead of the rows
+  float gate = 0.0f, beta = 0.0f;           // of one token a lane, a block ahead of the rows
   auto request = [&](int t0) {
     stK.load(k, k_step, t0, end);
     stQ.load(q, q_step, t0, end);
@@ -89,150 +86,116 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
   auto next_gates = [&](int t0, Gates& to) {
     if (wave == WAVES - 1) put_gates(to, lane, kTok - 1 - lane, t0 + lane < end ? gate : 0.0f, t0 + lane < end ? beta : 0.0f);
   };
-  const int start = first < end ? first + (end - first - 1) / kTok * kTok : first;
-  if (first < end) {
+  const int blocks = first < end ? (end - first + kTok - 1) / kTok : 0, start = first + max(0, blocks - 1) * kTok;
+  if (blocks > 0) {
     request_gates(start);
     request(start);
-    next_gates(start, gate_pair[0]);
+    next_gates(start, gates[0]);
     request_gates(start - kTok);
   }
   int turn = 0;
 
-  for (int t0 = start, left = first < end ? (end - first + kTok - 1) / kTok : 0; left > 0;) {
+  for (int t0 = start, left = blocks; left > 0;) {
     // dS at the end of every 256 tokens; the blocks between two such places in a loop of their own
     if (!MAP && ((t0 + kTok) % kKeep == 0 || t0 + kTok >= len)) {
       float* out = a.kept + (static_cast<size_t>(head) * a.n_kept + t0 / kKeep) * DV * DK;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-          const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-          if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col0 + 16 * n) * DK + dk) = S[n][kt];
-        }
+      for (int kt = 0; kt < KT; ++kt) {
+        const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
+        if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col) * DK + dk) = S[kt];
       }
     }
     for (int inner = min(left, t0 % kKeep / kTok + 1); inner > 0; --inner, --left, t0 -= kTok) {
-    // the LDS addresses are formed anew in each block: kept over the loop they would take the registers of the state
-    asm volatile("" : "+v"(c), "+v"(g));
-    stK.template store<RK>(sK);
-    stQ.template store<RK>(sQ);
-    stD.template store<RV>(sD);
-    const Gates& gates = gate_pair[turn];
-    turn ^= 1;
-    __syncthreads();
+      // the LDS addresses are formed anew in each block: kept over the loop they would take the registers of the state
+      asm volatile("" : "+v"(c), "+v"(g));
+      stK.template store<RK>(sK);
+      stQ.template store<RK>(sQ);
+      stD.template store<RV>(sD);
+      const Gates& gt = gates[turn];
+      turn ^= 1;
+      __syncthreads();
+      token_matrices<IO, RK, KT / 2, WAVES, true, true>(sK, sQ, gt, inverse, below, att, scratch, a.scale, wave, c, g);
 
-    // ---- matrices between tokens, tile (i, j), j <= i: transposed products, so that a lane has four tokens j of row i = c
-    constexpr int PAIRS = kTiles * (kTiles + 1) / 2;
-    for (int job = wave; job < 2 * PAIRS; job += WAVES) {
-      // the diagonal tiles of k k^T first: their inverses take longest
-      const bool keys = job < PAIRS;
-      int p = keys ? job : job - PAIRS, i, j;
-      if (p < kTiles) {
-        i = j = p;
-      } else {
-        p -= kTiles;
-        i = 1;
-        while (p >= i) p -= i++;
-        j = p;
-      }
-      f4 x = f4{0.0f, 0.0f, 0.0f, 0.0f};
+      // ---- P = K dS^T
+      f4 P[kTiles] = {zero, zero};
 #pragma unroll
       for (int s = 0; s < KT / 2; ++s) {
-        x = O::mul_rows(O::template rows<RK>(keys ? sK : sQ, j, s, c, g), O::template rows<RK>(sK, i, s, c, g), x);
-      }
-      const float hi = gates.hi[16 * i + c], lo = gates.lo[16 * i + c];
-      const f4 hj = *reinterpret_cast<const f4*>(&gates.hi[16 * j + 4 * g]), lj = *reinterpret_cast<const f4*>(&gates.lo[16 * j + 4 * g]);
-      const f4 bj = *reinterpret_cast<const f4*>(&gates.beta[16 * j + 4 * g]);
+        typename O::A ka[kTiles];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int before = i - j > 0 ? 1 : (keys ? c - (4 * g + r) : c - (4 * g + r) + 1);   // > 0: token j counts for token i
-        const float w = __builtin_amdgcn_exp2f((hj[r] - hi) + (lj[r] - lo)) * (keys ? -bj[r] : a.scale);
-        x[r] = before > 0 ? x[r] * w : 0.0f;
+        for (int i = 0; i < kTiles; ++i) ka[i] = O::template rows<RK>(sK, i, s, c, g);
+        const typename O::B x = O::pair(S[2 * s], S[2 * s + 1], one);
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) P[i] = O::mul(ka[i], x, P[i]);
       }
-      if (keys && i == j) {
-        invert_tile<IO>(x, diagonal[i], inverse[i], c, g);
-      } else if (keys) {
-        O::put(below[i * (i - 1) / 2 + j], c, g, x);
-      } else {
-        O::put(att[i * (i + 1) / 2 + j], c, g, x);
-      }
-    }
+      __syncthreads();
+      if (left > 1) request(t0 - kTok);
 
-    // ---- P = K dS^T
-    f4 P[NT][kTiles];
+      // ---- W, the gradient of v, the state's gradient
+      const auto gate4 = [&](const float* from, int tile) { return *reinterpret_cast<const f4*>(from + 16 * tile + 4 * g); };
+      static_assert(kTiles == 2, "one pair of token tiles");
+      const bool values = !MAP || wave * 16 < DV;      // the columns of the map have no dO
+      const float decay = gt.end;
+      typename O::Raw d[kTiles];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i) P[n][i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-#pragma unroll
-    for (int s = 0; s < KT / 2; ++s) {
-      typename O::A ka[kTiles];
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i) ka[i] = O::template rows<RK>(sK, i, s, c, g);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const typename O::B x = O::pair(S[n][2 * s], S[n][2 * s + 1], one);
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) P[n][i] = O::mul(ka[i], x, P[n][i]);
-      }
-    }
-    __syncthreads();
-    if (t0 > first) request(t0 - kTok);
-
-    // ---- W, the gradient of v, the state's gradient
-    const float decay = gates.end;
-    static_assert(kTiles == 2 && NT == 1, "one pair of token tiles, one tile of columns");
-    const bool values = !MAP || wave * 16 < DV;      // the columns of the map have no dO
-    typename O::Raw d[kTiles];
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) d[i] = values ? O::template tile_raw<RV>(sD, wave, i, c, g) : typename O::Raw{};
-    f4 W[kTiles];
-    typename O::TB wb[kTiles];
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      f4 x = *reinterpret_cast<const f4*>(&gates.rest[16 * i + 4 * g]) * P[0][i];
-#pragma unroll
-      for (int j = 0; j <= i; ++j) x = O::mul_tok_raw(O::image(att[i * (i + 1) / 2 + j], c, g), d[j], x);
-#pragma unroll
-      for (int j = 0; j < i; ++j) x = O::mul_tok(O::image(below[i * (i - 1) / 2 + j], c, g), wb[j], x);
-      W[i] = O::mul_tok(O::image(inverse[i], c, g), O::tokens(x, one), f4{0.0f, 0.0f, 0.0f, 0.0f});
-      if (i + 1 < kTiles) wb[i] = O::tokens(W[i], one);
-    }
-    if constexpr (!MAP) {
-      const __amdgpu_buffer_rsrc_t rows = rows_buffer(a.rows + (static_cast<size_t>(head) * a.T + t0) * DV, DV * 4, last - t0, DV * 4);
-      const __amdgpu_buffer_rsrc_t out = rows_buffer(dv + t0 * dv_step, dv_step, last - t0, DV * static_cast<int>(sizeof(IO)));
+      for (int i = 0; i < kTiles; ++i) d[i] = values ? O::template tile_raw<RV>(sD, wave, i, c, g) : typename O::Raw{};
+      f4 W[kTiles];
+      typename O::TB wb[kTiles];
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
-        const int t = kTok - 1 - (16 * i + 4 * g);
-        store_column(rows, (t * DV + col0) * 4, -DV * 4, W[i], static_cast<float*>(nullptr));
-        store_column(out, t * static_cast<int>(dv_step) + col0 * static_cast<int>(sizeof(IO)), -static_cast<int>(dv_step),
-                     W[i] * *reinterpret_cast<const f4*>(&gates.beta[16 * i + 4 * g]), static_cast<IO*>(nullptr));
+        const f4 rest = gate4(gt.rest, i);
+        const typename O::TA inv = O::image(inverse[i], c, g);
+        f4 x = rest * P[i];
+#pragma unroll
+        for (int j = 0; j <= i; ++j) {
+          const typename O::TA m = O::image(att[i * (i + 1) / 2 + j], c, g);
+          x = O::mul_tok_raw(m, d[j], x);
+        }
+#pragma unroll
+        for (int j = 0; j < i; ++j) {
+          const typename O::TA m = O::image(below[i * (i - 1) / 2 + j], c, g);
+          x = O::mul_tok(m, wb[j], x);
+        }
+        W[i] = O::mul_tok(inv, O::tokens(x, one), zero);
+        if (i + 1 < kTiles) wb[i] = O::tokens(W[i], one);
       }
-    }
-    f4 e[kTiles];
+      if constexpr (!MAP) {
+        const __amdgpu_buffer_rsrc_t rows = rows_buffer(a.rows + (static_cast<size_t>(head) * a.T + t0) * DV, DV * 4, last - t0, DV * 4);
+        const __amdgpu_buffer_rsrc_t out = rows_buffer(dv + t0 * dv_step, dv_step, last - t0, DV * static_cast<int>(sizeof(IO)));
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      const f4 gamma = *reinterpret_cast<const f4*>(&gates.gamma[16 * i + 4 * g]);
-      W[i] *= -gamma * *reinterpret_cast<const f4*>(&gates.beta[16 * i + 4 * g]);
-      e[i] = O::value(d[i]) * (gamma * a.scale);
-    }
-    const typename O::B wp = O::pair(W[0], W[1], one), ep = O::pair(e[0], e[1], one);
+        for (int i = 0; i < kTiles; ++i) {
+          const int t = kTok - 1 - (16 * i + 4 * g);
+          store_column(rows, (t * DV + col) * 4, -DV * 4, W[i], static_cast<float*>(nullptr));
+          store_column(out, t * static_cast<int>(dv_step) + col * static_cast<int>(sizeof(IO)), -static_cast<int>(dv_step), W[i] * gate4(gt.beta, i),
+                       static_cast<IO*>(nullptr));
+        }
+      }
+      f4 e[kTiles];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      f4 x = O::mul(O::template columns<RK>(sK, kt, 0, c, g), wp, S[0][kt] * decay);
-      if (values) x = O::mul(O::template columns<RK>(sQ, kt, 0, c, g), ep, x);
-      S[0][kt] = x;
-    }
-    next_gates(t0 - kTok, gate_pair[turn]);
-    request_gates(t0 - 2 * kTok);
-    __syncthreads();
+      for (int i = 0; i < kTiles; ++i) {
+        const f4 gamma = gate4(gt.gamma, i);
+        W[i] *= -gamma * gate4(gt.beta, i);
+        e[i] = O::value(d[i]) * (gamma * a.scale);
+      }
+      const typename O::B wp = O::pair(W[0], W[1], one), ep = O::pair(e[0], e[1], one);
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        const typename O::A kc = O::template columns<RK>(sK, kt, 0, c, g);
+        f4 x = O::mul(kc, wp, S[kt] * decay);
+        if (values) {
+          const typename O::A qc = O::template columns<RK>(sQ, kt, 0, c, g);
+          x = O::mul(qc, ep, x);
+        }
+        S[kt] = x;
+      }
+      next_gates(t0 - kTok, gates[turn]);
+      request_gates(t0 - 2 * kTok);
+      __syncthreads();
     }
   }
 
   // ---- gradients of tokens past the end of the sequence, of the state
   if constexpr (!MAP) {
-    const int done = first < end ? first + (end - first + kTok - 1) / kTok * kTok : first;
+    const int done = first + blocks * kTok;
     for (int t = done + wave; t < last; t += WAVES) {
       for (int i = lane; i < DV; i += 64) io_store(reinterpret_cast<IO*>(dv + t * dv_step) + i, 0.0f);
     }
@@ -242,12 +205,9 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
   else if (a.S_T != nullptr && seg == 0) out = a.S_T + static_cast<size_t>(head) * DV * DK;
   if (out == nullptr) return;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-      if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col0 + 16 * n) * DK + dk) = S[n][kt];
-    }
+  for (int kt = 0; kt < KT; ++kt) {
+    const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
+    if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col) * DK + dk) = S[kt];
   }
 }
 
