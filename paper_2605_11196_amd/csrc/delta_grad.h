@@ -42,9 +42,9 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
   const int first = seg * kKeep, last = min(a.T, first + kKeep), end = min(len, last);
   const char* q = reinterpret_cast<const char*>(static_cast<const IO*>(a.q) + b * a.qs.b + hk * a.qs.h);
   const char* k = reinterpret_cast<const char*>(static_cast<const IO*>(a.k) + b * a.ks.b + hk * a.ks.h);
-  const IO* v = static_cast<const IO*>(a.v) + b * a.vs.b + h * a.vs.h;
+  const char* v = reinterpret_cast<const char*>(static_cast<const IO*>(a.v) + b * a.vs.b + h * a.vs.h);
   const char* dO = reinterpret_cast<const char*>(static_cast<const IO*>(a.dO) + b * a.os.b + h * a.os.h);
-  const long long q_step = a.qs.t * sizeof(IO), k_step = a.ks.t * sizeof(IO), o_step = a.os.t * sizeof(IO);
+  const long long q_step = a.qs.t * sizeof(IO), k_step = a.ks.t * sizeof(IO), o_step = a.os.t * sizeof(IO), v_step = a.vs.t * sizeof(IO);
   const float* gp = a.g + b * a.gs.b + h * a.gs.h;
   const float* bp = a.beta + b * a.bs.b + h * a.bs.h;
   const size_t row0 = static_cast<size_t>(head) * a.T;
@@ -73,40 +73,47 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
       for (int r = 0; r < 4; ++r) S[vt][r] = DV == DVP || row + r < DV ? from[static_cast<size_t>(row + r) * DK + col] : 0.0f;
     }
   };
-  auto stage = [&](int t0) {
-    {
-      Stage<PK, THREADS> sk, sq;
-      Stage<PV, THREADS> sd;
-      sk.init(k_step);
-      sq.init(q_step);
-      sd.init(o_step);
-      sk.load(k, k_step, t0, end);
-      sq.load(q, q_step, t0, end);
-      sd.load(dO, o_step, t0, end);
-      sk.template store<RK>(sK);
-      sq.template store<RK>(sQ);
-      sd.template store<RV>(sD);
-    }
-    {
-      Stage<DV / 4, THREADS> sr, sw;
-      sr.init(DV * 4);
-      sw.init(DV * 4);
-      sr.load(reinterpret_cast<const char*>(a.R + row0 * DV), DV * 4, t0, end);
-      sw.load(reinterpret_cast<const char*>(a.rows + row0 * DV), DV * 4, t0, end);
+  // the rows of a block on their way from memory to LDS, a block ahead where the state leaves the registers for it (d_v = 64: 118 -> 97 us for
+  // 128 heads of 1024 tokens; d_v = 128 would keep 140 bytes a lane in scratch memory: 420 -> 540 us for 64 heads of 4096)
+  constexpr bool AHEAD = DV <= 64;
+  Stage<PK, THREADS> stK, stQ;
+  Stage<PV, THREADS> stD;
+  constexpr int ROWS4 = kTok * DV / 4, NR = (ROWS4 + THREADS - 1) / THREADS;
+  f4 stR[NR], stW[NR];                      // four columns of R and W, rows one after the other
+  stK.init(k_step);
+  stQ.init(q_step);
+  stD.init(o_step);
+  float gate = 0.0f, beta = 0.0f;
+  auto request = [&](int t0) {
+    stK.load(k, k_step, t0, end);
+    stQ.load(q, q_step, t0, end);
+    stD.load(dO, o_step, t0, end);
+    const __amdgpu_buffer_rsrc_t R = rows_buffer(a.R + (row0 + t0) * DV, DV * 4, end - t0, DV * 4);
+    const __amdgpu_buffer_rsrc_t W = rows_buffer(a.rows + (row0 + t0) * DV, DV * 4, end - t0, DV * 4);
 #pragma unroll
-      for (int i = 0; i < sr.N; ++i) {
-        const int p = threadIdx.x + i * THREADS;
-        if (sr.ALL % THREADS == 0 || p < sr.ALL) {
-          O::template put_split<TR, RV>(sR, p / (DV / 4), p % (DV / 4), __builtin_bit_cast(f4, sr.x[i]));
-          O::template put_split<TW, RV>(sW, p / (DV / 4), p % (DV / 4), __builtin_bit_cast(f4, sw.x[i]));
-        }
+    for (int i = 0; i < NR; ++i) {
+      const int p = threadIdx.x + i * THREADS;
+      stR[i] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(R, p * 16, 0, 0));
+      stW[i] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(W, p * 16, 0, 0));
+    }
+    const int t = min(t0 + (lane & (kTok - 1)), end - 1);
+    gate = gp[t * a.gs.t];
+    beta = bp[t * a.bs.t];
+  };
+  auto stage = [&](int t0) {
+    stK.template store<RK>(sK);
+    stQ.template store<RK>(sQ);
+    stD.template store<RV>(sD);
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int p = threadIdx.x + i * THREADS, row = p / (DV / 4), piece = p % (DV / 4);
+      const f4 r = stR[i], w = stW[i];
+      if (ROWS4 % THREADS == 0 || p < ROWS4) {
+        O::template put_split<TR, RV>(sR, row, piece, r);
+        O::template put_split<TW, RV>(sW, row, piece, w);
       }
     }
-    if (wave == 0) {
-      const int t = min(t0 + (lane & (kTok - 1)), end - 1);
-      const float gate = gp[t * a.gs.t], beta = bp[t * a.bs.t];
-      put_gates(gates, lane, lane, t0 + lane < end ? gate : 0.0f, t0 + lane < end ? beta : 0.0f);
-    }
+    if (wave == WAVES - 1) put_gates(gates, lane, lane, t0 + lane < end ? gate : 0.0f, t0 + lane < end ? beta : 0.0f);
   };
   const f4 zero = f4{0.0f, 0.0f, 0.0f, 0.0f};
   auto gate4 = [&](const float* from, int tile) { return *reinterpret_cast<const f4*>(from + 16 * tile + 4 * g); };
@@ -117,8 +124,10 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
 #pragma unroll
     for (int vt = 0; vt < VT; ++vt) S[vt] = zero;
   }
+  if (AHEAD && first < end) request(first);
   for (int t0 = first; t0 < end; t0 += kTok) {
     asm volatile("" : "+v"(c), "+v"(g));
+    if (!AHEAD) request(t0);
     stage(t0);
     __syncthreads();
 
@@ -129,10 +138,12 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
       if (t < end) {
         const float* W = a.rows + (row0 + t) * DV;
         const float* R = a.R + (row0 + t) * DV;
-        for (int x = threadIdx.x % 16; x < DV; x += 16) {
-          const float w = W[x];
-          wr = fmaf(w, R[x], wr);
-          wv = fmaf(w, widen(v[t * a.vs.t + x]), wv);
+        const IO* values = reinterpret_cast<const IO*>(v + t * v_step);
+#pragma unroll
+        for (int x = 0; x < DV; x += 16) {
+          const int at = x + threadIdx.x % 16;
+          wr = fmaf(W[at], R[at], wr);
+          wv = fmaf(W[at], widen(values[at]), wv);
         }
       }
       wr = row_sum16(wr);
@@ -143,43 +154,49 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
       }
     }
     // ---- matrices between tokens
-    for (int job = wave; job < 10; job += WAVES) {
-      // 0-2: X (0,0), (1,0), (1,1); 3-5: X^T of the same; 6: Z (1,0), 7: Z (0,1), 8: Z (0,0), 9: Z (1,1)
-      const int kind = job < 3 ? 0 : (job < 6 ? 1 : (job < 8 ? 2 + job - 6 : 4));
-      const int tile = job < 6 ? job % 3 : (job < 8 ? 1 : (job == 8 ? 0 : 2));
+    // 0, 1: Z (0,0) and (1,1), twice the work of the others; 2-4: X (0,0), (1,0), (1,1); 5-7: X^T of the same; 8: Z (1,0), 9: Z (0,1), which the
+    // waves after those of 0 and 1 take as their second
+    for (int job = (wave + (WAVES == 8 ? 6 : 0)) % WAVES; job < 10; job += WAVES) {
+      const int order = WAVES == 8 ? (job < 2 ? 2 + job : (job < 6 ? 4 + job - 2 : (job < 8 ? job - 6 : job))) : job;
+      const int kind = order < 2 ? 4 : (order < 5 ? 0 : (order < 8 ? 1 : order - 6));
+      const int tile = order < 2 ? 2 * order : (order < 8 ? (order - 2) % 3 : 1);
       const int i = tile > 0 ? 1 : 0, j = tile > 1 ? 1 : 0;       // row tile i, column tile j of X and Y
+      // x: rows j = 4 g + r of tile j, column i = c of tile i; y: rows i, column j
+      const bool writes = kind >= 2;          // Y and not X
       f4 x = zero, y = zero;
 #pragma unroll
       for (int s = 0; s < DVP / 32; ++s) {
         const typename O::Split rj = O::template rows_split<TR, RV>(sR, j, s, c, g);
-        if (kind <= 1) {
+        if (!writes) {
           const typename O::A di = O::template rows<RV>(sD, i, s, c, g);
-          x = kind == 0 ? O::mul_split_exact(rj, di, x) : O::mul(di, rj, x);
+          if (kind == 0) x = O::mul_split_exact(rj, di, x);
+          else y = O::mul(di, rj, y);
         } else {
           const typename O::Split wi = O::template rows_split<TW, RV>(sW, i, s, c, g);
           if (kind != 3) x = O::mul_split_out(rj, wi, x);
           if (kind != 2) y = O::mul_split_out(wi, rj, y);
         }
       }
-      // x: rows j = 4 g + r of tile j, column i = c of tile i; y (and x of X^T): rows i, column j
-      const float hi_i = gates.hi[16 * i + c], lo_i = gates.lo[16 * i + c], beta_i = gates.beta[16 * i + c];
-      const float hi_j = gates.hi[16 * j + c], lo_j = gates.lo[16 * j + c], beta_j = gates.beta[16 * j + c];
-      const f4 hj = gate4(gates.hi, j), lj = gate4(gates.lo, j), bj = gate4(gates.beta, j);
-      const f4 hi = gate4(gates.hi, i), li = gate4(gates.lo, i), bi = gate4(gates.beta, i);
+      if (kind % 2 == 0) {
+        const float hi = gates.hi[16 * i + c], lo = gates.lo[16 * i + c], factor = writes ? -gates.beta[16 * i + c] : a.scale;
+        const f4 hj = gate4(gates.hi, j), lj = gate4(gates.lo, j), bj = gate4(gates.beta, j);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int apart = c - (4 * g + r);            // i - j within a diagonal tile, of x; of y it is the negative
-        const float dx = __builtin_amdgcn_exp2f((hi_i - hj[r]) + (lo_i - lj[r]));
-        const float dy = __builtin_amdgcn_exp2f((hi[r] - hi_j) + (li[r] - lo_j));
-        if (kind == 0) x[r] = i > j || apart >= 0 ? x[r] * dx * bj[r] * a.scale : 0.0f;
-        if (kind == 1) x[r] = i > j || apart <= 0 ? x[r] * dy * beta_j * a.scale : 0.0f;
-        if (kind >= 2) {
-          x[r] = i > j || apart > 0 ? -x[r] * dx * bj[r] * beta_i : 0.0f;
-          y[r] = i > j || apart < 0 ? -y[r] * dy * bi[r] * beta_j : 0.0f;
+        for (int r = 0; r < 4; ++r) {
+          const int before = i > j ? 1 : c - (4 * g + r) + (writes ? 0 : 1);
+          x[r] = before > 0 ? x[r] * (__builtin_amdgcn_exp2f((hi - hj[r]) + (lo - lj[r])) * bj[r] * factor) : 0.0f;
+        }
+      }
+      if (kind == 1 || kind >= 3) {
+        const float hj = gates.hi[16 * j + c], lj = gates.lo[16 * j + c], bj = gates.beta[16 * j + c];
+        const f4 hi = gate4(gates.hi, i), lo = gate4(gates.lo, i), bi = gate4(gates.beta, i);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int before = i > j ? 1 : (4 * g + r) - c + (writes ? 0 : 1);
+          y[r] = before > 0 ? y[r] * (__builtin_amdgcn_exp2f((hi[r] - hj) + (lo[r] - lj)) * bj * (writes ? -bi[r] : a.scale)) : 0.0f;
         }
       }
       if (kind == 0) O::put(X[tile], c, g, x);
-      else if (kind == 1) O::put(Xt[tile], c, g, x);
+      else if (kind == 1) O::put(Xt[tile], c, g, y);
       else if (kind == 2) O::put(Z[2], c, g, x);
       else if (kind == 3) O::put(Z[1], c, g, y);
       else O::put(Z[3 * i], c, g, x + y);
@@ -238,6 +255,7 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
                                     O::value(kr[1]) * (gate4(gates.rest, 1) * gate4(gates.beta, 1)), one);
 #pragma unroll
     for (int vt = 0; vt < VT; ++vt) S[vt] = O::mul_split(O::template columns_split<TR, RV>(sR, vt, 0, c, g), x, S[vt] * decay);
+    if (AHEAD && t0 + kTok < end) request(t0 + kTok);
     __syncthreads();
     if (threadIdx.x < kTok) {
       float sum = 0.0f;
@@ -267,9 +285,11 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
   for (int t0 = start; t0 >= first && first < end; t0 -= kTok) {
     asm volatile("" : "+v"(c), "+v"(g));
     if (t0 != start) {      // the last block is still staged
+      if (!AHEAD) request(t0);
       stage(t0);
       __syncthreads();
     }
+    if (AHEAD && t0 > first) request(t0 - kTok);
     f4 dK[kTiles] = {zero, zero};
 #pragma unroll
     for (int s = 0; s < VT / 2; ++s) {

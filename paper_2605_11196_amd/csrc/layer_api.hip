@@ -104,8 +104,12 @@ bool gate_rows(const vla_strides& s, long long H, long long T, vla::Rows* out) {
   return out->b >= 0 && out->h >= 0 && out->t >= 0;
 }
 
-// Time segments of a sequence.  Few heads leave most of the card idle; in segments the sequence goes through twice (maps, then outputs: 2.7
-// times the work) with about `waves` waves on the card.
+// Time segments of a sequence.  Few heads leave most of the card idle; in segments the sequence goes through twice (maps, then outputs:
+// 2.5 times the work).  The maps' workgroups of (d_v + d_k) / 16 waves decide how many segments the card holds at once; with small heads
+// twice as many still gain.  Forward, one segment against the rule's (us, bf16 but where said): 64 heads of 128, 4096 tokens, 4: 467, 295
+// (2: 519, 8: 304); 128 heads, 2: 476, 550 (the rule: none); 16 heads of 128, 32768 tokens, 16: 3770, 559; 128 heads of 64, 4096 tokens, 8:
+// 381, 226; 256 heads, 4: 387, 420 (none); 39 heads of 128 x 64, float32, 1537 tokens, 6: 352, 175; 8 heads of 64, 512 tokens, 4: 52, 36;
+// 256 tokens, 2: 28, 33 (none).
 struct Segments {
   int n, tokens;
   size_t map_bytes, bytes;   // of the maps, of both arrays
@@ -115,9 +119,11 @@ Segments delta_segments(long long heads, int T, int d_k, int d_v, int requested)
   const int blocks = (T + 31) / 32;
   long long n = requested;
   if (requested == 0) {
-    n = 4096 / (heads * (d_v / 16));      // 16 waves a compute unit, d_v / 16 a workgroup
+    const int waves = (d_v + d_k) / 16;
+    const long long slots = 256 * (waves < 16 ? 16 / waves : 1);
+    n = (waves <= 8 ? 2 : 1) * slots / heads;
     if (n > blocks / 4) n = blocks / 4;
-    if (n < 6) n = 1;
+    if (blocks < 16 || n < (heads * n <= slots ? 3 : 6)) n = 1;
   }
   if (n > blocks) n = blocks;
   if (n > 256) n = 256;
