@@ -58,6 +58,7 @@ bool rows_apart(const vla::Rows& r, long long B, long long H, long long T, long 
       }
     }
   }
+  if (B == 0 || H == 0 || T == 0) return true;
   long long span = d;
   for (int i = 0; i < 3; ++i) {
     if (n[i] <= 1) continue;

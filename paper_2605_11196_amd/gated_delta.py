@@ -2,44 +2,53 @@
 import ctypes
 
 from . import binding
-from .binding import VlaDeltaOpts, VlaError
-from .qk_norm import _io, _like, _p, _rows, _steps, _strides
+from .binding import VlaDeltaOpts, VlaError, VlaStrides
+from .qk_norm import _io, _laid_out, _like, _p, _steps, _strides
 
 
 def _gate(x):
-    return x if any(_steps(x)) else x.contiguous()
+    """A gate [B,H,T] and its strides: any that do not repeat one value over everything."""
+    if x.is_contiguous():
+        return x, None
+    s = _steps(x)
+    return (x, VlaStrides(*s)) if any(s) else (x.contiguous(), None)
 
 
-def _check(torch, q, k, v, g, beta, state, lengths, tokens):
-    """Shapes of a call over tokens (tokens 1) or of one token (0); state: (name, tensor or None) pairs."""
+def _check(torch, q, k, v, g, beta, state, state_name, lengths, tokens):
+    """Shapes of a call over tokens (tokens 1) or of one token (0); state: the given state or gradient of it, or None."""
+    dev, dtype, shape, v_shape = q.device, q.dtype, q.shape, v.shape
     if not (q.is_cuda and k.is_cuda and v.is_cuda):
         raise ValueError("q, k, v must be GPU tensors (no CPU path exists)")
-    dev = q.device
-    if k.dtype != q.dtype or v.dtype != q.dtype or k.device != dev or v.device != dev:
+    if k.dtype != dtype or v.dtype != dtype or k.device != dev or v.device != dev:
         raise ValueError("q, k, v must share a dtype and a device")
-    names = "[B,H,T,d]" if tokens else "[B,H,d]"
-    if q.dim() != 3 + tokens or k.shape != q.shape or v.dim() != q.dim() or v.shape[0] != q.shape[0] or v.shape[2:-1] != q.shape[2:-1]:
-        raise ValueError(f"expected q, k and v as {names} with one batch and length, q and k of one shape")
-    H_k, H_v = q.shape[1], v.shape[1]
+    if len(shape) != 3 + tokens or k.shape != shape or len(v_shape) != len(shape) or v_shape[0] != shape[0] or v_shape[2:-1] != shape[2:-1]:
+        raise ValueError(f"expected q, k and v as {'[B,H,T,d]' if tokens else '[B,H,d]'} with one batch and length, q and k of one shape")
+    H_k, H_v = shape[1], v_shape[1]
     if H_k < 1 or H_v % H_k:
         raise ValueError(f"the value heads ({H_v}) must be a multiple of the key heads ({H_k})")
-    for name, x in (("g", g), ("beta", beta)):
-        if x.dtype != torch.float32 or x.shape != v.shape[:-1] or x.device != dev:
-            raise ValueError(f"{name} must be a float32 tensor of shape {tuple(v.shape[:-1])} on {dev}")
-    shape = (q.shape[0], H_v, v.shape[-1], q.shape[-1])
-    for name, S in state:
-        if S is not None and (S.dtype != torch.float32 or S.shape != shape or not S.is_contiguous() or S.device != dev):
-            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {shape} on {dev}")
-    if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != q.shape[:1] or lengths.device != dev):
-        raise ValueError(f"lengths must be an int32 tensor of shape {tuple(q.shape[:1])} on {dev}")
+    gate = v_shape[:-1]
+    if g.dtype != torch.float32 or beta.dtype != torch.float32 or g.shape != gate or beta.shape != gate or g.device != dev or beta.device != dev:
+        raise ValueError(f"g and beta must be float32 tensors of shape {tuple(gate)} on {dev}")
+    if state is not None and (state.dtype != torch.float32 or state.shape != (shape[0], H_v, v_shape[-1], shape[-1]) or not state.is_contiguous()
+                              or state.device != dev):
+        raise ValueError(f"{state_name} must be a contiguous float32 tensor of shape {(shape[0], H_v, v_shape[-1], shape[-1])} on {dev}")
+    if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != shape[:1] or lengths.device != dev):
+        raise ValueError(f"lengths must be an int32 tensor of shape {tuple(shape[:1])} on {dev}")
 
 
 def _inputs(q, k, v, g, beta, scale, lengths, segments=0):
     """The inputs as the kernels take them, kept until the call, and its options."""
-    q, k, v, g, beta = _rows(q), _rows(k), _rows(v), _gate(g), _gate(beta)
-    lengths = None if lengths is None else lengths.contiguous()
-    op = VlaDeltaOpts(scale=scale or 0.0, lengths=_p(lengths), segments=segments)
-    op.q, op.k, op.v, op.g, op.beta = (_strides(x) for x in (q, k, v, g, beta))
+    op = VlaDeltaOpts(scale or 0.0)
+    op.segments = segments
+    (q, op.q), (k, op.k), (v, op.v) = _laid_out(q), _laid_out(k), _laid_out(v)
+    (g, g_strides), (beta, beta_strides) = _gate(g), _gate(beta)
+    if g_strides is not None:
+        op.g = g_strides
+    if beta_strides is not None:
+        op.beta = beta_strides
+    if lengths is not None:
+        lengths = lengths.contiguous()
+        op.lengths = lengths.data_ptr()
     return (q, k, v, g, beta, lengths), op
 
 
@@ -54,14 +63,15 @@ def gated_delta_forward(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, 
     """
     import torch
 
-    _check(torch, q, k, v, g, beta, (("S0", S0),), lengths, 1)
+    _check(torch, q, k, v, g, beta, S0, "S0", lengths, 1)
     io, (B, H_k, T, dk), H_v, dv, dev = _io(torch, q), q.shape, v.shape[1], v.shape[-1], q.device
     lib = binding.load_library()
     handle, context, outside = binding._on_stream(torch, dev, stream)
     with context:
         kept, op = _inputs(q, k, v, g, beta, scale, lengths, segments)
         o = _like(torch, v)
-        op.o = _strides(o)
+        if not o.is_contiguous():
+            op.o = _strides(o)
         S_T = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
         saved = None
         if save_for_backward:
@@ -86,7 +96,7 @@ def gated_delta_decode_step(q, k, v, g, beta, S, *, scale=None, stream=None):
     place.  Returns o [B,H_v,d_v]."""
     import torch
 
-    _check(torch, q, k, v, g, beta, (("S", S),), None, 0)
+    _check(torch, q, k, v, g, beta, S, "S", None, 0)
     io, (B, H_k, dk), H_v, dv, dev = _io(torch, q), q.shape, v.shape[1], v.shape[-1], q.device
     lib = binding.load_library()
     handle, context, outside = binding._on_stream(torch, dev, stream)
@@ -108,7 +118,7 @@ def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, 
     and what it saved.  dg, dbeta and dS0 are float32."""
     import torch
 
-    _check(torch, q, k, v, g, beta, (("dS_T", dS_T),), lengths, 1)
+    _check(torch, q, k, v, g, beta, dS_T, "dS_T", lengths, 1)
     if do.shape != v.shape or do.dtype != v.dtype or do.device != v.device:
         raise ValueError("do must match v in shape, dtype and device")
     io, (B, H_k, T, dk), H_v, dv, dev = _io(torch, q), q.shape, v.shape[1], v.shape[-1], q.device
@@ -116,11 +126,11 @@ def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, 
     handle, context, outside = binding._on_stream(torch, dev, stream)
     with context:
         kept, op = _inputs(q, k, v, g, beta, scale, lengths, segments)
-        do = _rows(do)
+        do, op.o = _laid_out(do)
         dq, dk_, dv_ = _like(torch, q), _like(torch, k), _like(torch, v)
         dg, dbeta = (torch.empty((B, H_v, T), dtype=torch.float32, device=dev) for _ in range(2))
         dS0 = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
-        op.o, op.dq, op.dk, op.dv = (_strides(x) for x in (do, dq, dk_, dv_))
+        op.dq, op.dk, op.dv = _strides(dq), _strides(dk_), _strides(dv_)
         op.saved, op.saved_bytes = saved.data_ptr(), saved.numel()
         need = lib.vla_delta_workspace_bytes(B, H_k, H_v, T, dk, dv, io, ctypes.byref(op), 1)
         ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None

@@ -18,16 +18,21 @@ def _steps(x):
     return [step if n > 1 else 0 for step, n in zip(x.stride(), x.shape[:3])]
 
 
-def _rows(x):
-    """x, or a contiguous copy where it is not laid out as the kernels take it: the last dimension together, the other strides
-    multiples of 16 bytes and not all zero for rows that repeat, tokens apart but not too far, 16-byte alignment."""
-    per16 = 16 // x.element_size()
-    s = _steps(x)
-    fits = (x.stride(-1) == 1 and not any(step % per16 for step in s) and (any(s) or x.is_contiguous())
-            and (x.shape[2] <= 1 or x.shape[-1] <= s[2] < 2 ** 26 // x.element_size()))
-    if fits and x.data_ptr() % 16 == 0:
-        return x
-    return x.clone() if x.is_contiguous() else x.contiguous()
+def _laid_out(x):
+    """x and its strides for the C call, or a contiguous copy where it is not laid out as the kernels take it: the last dimension
+    together, the other strides multiples of 16 bytes and not all zero for rows that repeat, tokens apart but not too far, 16-byte
+    alignment."""
+    aligned = not x.data_ptr() & 15
+    if x.is_contiguous():
+        return (x if aligned else x.clone()), _CONTIGUOUS
+    s, size = _steps(x), x.element_size()
+    if (aligned and x.stride(-1) == 1 and not any(step * size & 15 for step in s) and any(s)
+            and (x.shape[2] <= 1 or x.shape[-1] <= s[2] < 2 ** 26 // size)):
+        return x, VlaStrides(*s)
+    return x.contiguous(), _CONTIGUOUS
+
+
+_CONTIGUOUS = VlaStrides(0, 0, 0)
 
 
 def _strides(x):
@@ -41,45 +46,55 @@ def _like(torch, x):
 
 
 def _check(torch, q, k, q_weight, k_weight, cos, sin, positions, norm):
+    dev, dtype, shape, k_shape = q.device, q.dtype, q.shape, k.shape
     if not (q.is_cuda and k.is_cuda):
         raise ValueError("q and k must be GPU tensors (no CPU path exists)")
-    if k.dtype != q.dtype or q.dim() != 4 or k.dim() != 4 or (k.shape[0], *k.shape[2:]) != (q.shape[0], *q.shape[2:]) or k.device != q.device:
+    if k.dtype != dtype or len(shape) != 4 or len(k_shape) != 4 or shape[0] != k_shape[0] or shape[2:] != k_shape[2:] or k.device != dev:
         raise ValueError("expected q [B,H_q,T,d] and k [B,H_k,T,d] of one dtype on one device")
     if norm not in ("rms", "l2"):
         raise ValueError(f"norm must be 'rms' or 'l2', not {norm!r}")
-    d = q.shape[-1]
+    d = shape[3]
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None and (w.shape != (d,) or w.dtype not in (torch.float32, torch.bfloat16) or w.device != q.device):
-            raise ValueError(f"{name} must be a float32 or bfloat16 tensor of shape {(d,)} on {q.device}")
+        if w is not None and (w.shape != (d,) or w.dtype not in (torch.float32, torch.bfloat16) or w.device != dev):
+            raise ValueError(f"{name} must be a float32 or bfloat16 tensor of shape {(d,)} on {dev}")
     if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
         raise ValueError("q_weight and k_weight must share a dtype")
     if (cos is None) != (sin is None):
         raise ValueError("cos and sin come together")
     if cos is not None:
-        for name, t in (("cos", cos), ("sin", sin)):
-            if t.dtype != torch.float32 or t.dim() != 2 or t.shape != cos.shape or t.device != q.device or not 0 < 2 * t.shape[1] <= d or t.shape[0] < 1:
-                raise ValueError(f"{name} must be a float32 tensor [positions, rot / 2] on {q.device}")
-    if positions is not None and (positions.dtype != torch.int32 or tuple(positions.shape) != (q.shape[0], q.shape[2]) or positions.device != q.device):
-        raise ValueError(f"positions must be an int32 tensor of shape {(q.shape[0], q.shape[2])} on {q.device}")
+        table = cos.shape
+        if (cos.dtype != torch.float32 or sin.dtype != torch.float32 or len(table) != 2 or sin.shape != table or cos.device != dev
+                or sin.device != dev or not 0 < 2 * table[1] <= d or table[0] < 1):
+            raise ValueError(f"cos and sin must be float32 tensors [positions, rot / 2] on {dev}")
+    if positions is not None and (positions.dtype != torch.int32 or positions.shape != (shape[0], shape[2]) or positions.device != dev):
+        raise ValueError(f"positions must be an int32 tensor of shape {(shape[0], shape[2])} on {dev}")
+
+
+def _together(x):
+    """x contiguous and 16-byte aligned."""
+    x = x.contiguous()
+    return x.clone() if x.data_ptr() & 15 else x
 
 
 def _call(torch, q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, interleaved):
-    """The arguments that both directions share, ready for the C call: tensors that have to live until it, and the options."""
-    q, k = _rows(q), _rows(k)
-    same = lambda x: None if x is None else x.contiguous()
-    kept = [q, k, same(q_weight), same(k_weight), same(cos), same(sin), same(positions)]
-    for i in (2, 3, 4, 5):
-        if kept[i] is not None and kept[i].data_ptr() % 16:
-            kept[i] = kept[i].clone()
-    op = VlaNormOpts(eps=eps, l2=norm == "l2", interleaved=bool(interleaved), offset=offset)
+    """What both directions share: the tensors as the kernels take them, which have to live until the call, and the options."""
+    op = VlaNormOpts(eps, norm == "l2", bool(interleaved), 0, 0, offset)
+    (q, op.q), (k, op.k) = _laid_out(q), _laid_out(k)
+    if q_weight is not None:
+        q_weight = _together(q_weight)
+    if k_weight is not None:
+        k_weight = _together(k_weight)
+    weight = k_weight if q_weight is None else q_weight
+    if weight is not None and weight.dtype == torch.bfloat16:
+        op.weight_dtype = VLA_BF16
     if cos is not None:
-        op.rot, op.places = 2 * cos.shape[1], cos.shape[0]
-    weight = q_weight if q_weight is not None else k_weight
-    op.weight_dtype = VLA_BF16 if weight is not None and weight.dtype == torch.bfloat16 else VLA_F32
+        cos, sin = _together(cos), _together(sin)
+        op.places, half = cos.shape
+        op.rot = 2 * half
     if positions is not None:
-        op.positions = kept[6].data_ptr()
-    op.q, op.k = _strides(q), _strides(k)
-    return kept, op
+        positions = positions.contiguous()
+        op.positions = positions.data_ptr()
+    return (q, k, q_weight, k_weight, cos, sin, positions), op
 
 
 def _p(x):
@@ -95,11 +110,13 @@ def _forward(q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, i
     handle, context, outside = binding._on_stream(torch, dev, stream)
     with context:
         kept, op = _call(torch, q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, interleaved)
-        q_out, k_out = (torch.empty(x.shape, dtype=q.dtype, device=dev) for x in (q, k))
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
         if outside is not None:
             q_out.record_stream(outside)
             k_out.record_stream(outside)
-        rc = lib.vla_qk_norm_rope(*(_p(x) for x in kept[:6]), _p(q_out), _p(k_out), B, T, H_q, H_k, d, io, ctypes.byref(op), handle)
+        rc = lib.vla_qk_norm_rope(_p(kept[0]), _p(kept[1]), _p(kept[2]), _p(kept[3]), _p(kept[4]), _p(kept[5]), q_out.data_ptr(),
+                                  k_out.data_ptr(), B, T, H_q, H_k, d, io, ctypes.byref(op), handle)
     if rc != 0:
         raise VlaError(rc, binding.status_string(rc), "vla_qk_norm_rope")
     return q_out, k_out
@@ -119,8 +136,9 @@ def qk_norm_rope_backward(q, k, q_weight, k_weight, cos, sin, dq_out, dk_out, *,
     handle, context, outside = binding._on_stream(torch, dev, stream)
     with context:
         kept, op = _call(torch, q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, interleaved)
-        dq_out, dk_out, dq, dk = _rows(dq_out), _rows(dk_out), _like(torch, q), _like(torch, k)
-        op.q_out, op.k_out, op.dq, op.dk = (_strides(x) for x in (dq_out, dk_out, dq, dk))
+        (dq_out, op.q_out), (dk_out, op.k_out) = _laid_out(dq_out), _laid_out(dk_out)
+        dq, dk = _like(torch, q), _like(torch, k)
+        op.dq, op.dk = _strides(dq), _strides(dk)
         dw = [None if w is None else torch.empty((d,), dtype=torch.float32, device=dev) for w in (q_weight, k_weight)]
         need = lib.vla_qk_norm_rope_workspace_bytes(d) if q_weight is not None or k_weight is not None else 0
         ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
