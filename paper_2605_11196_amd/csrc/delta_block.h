@@ -349,6 +349,9 @@ __device__ __forceinline__ void invert_tile(f4 x, float* m, typename Ops<IO>::Im
   Ops<IO>::put(out, c, g, mine);
 }
 
+// Jobs in turn, the long ones first: from the second round on the waves take them in reverse, so that the first ones have the fewest.
+__device__ __forceinline__ int job_of(int round, int wave, int waves) { return round * waves + (round == 0 ? wave : waves - 1 - wave); }
+
 // The matrices between the tokens of a block, tile by tile on different waves, as left operands of the products that follow:
 //   inverse  (I + M)^-1 of the diagonal tiles,  below  -M of the tiles below,  att  A (with ATT)
 // Products are transposed, so that a lane has four tokens j of row i.  REVERSE: rows are the block's tokens with the last one first, M =
@@ -358,8 +361,11 @@ __device__ __forceinline__ void token_matrices(const u4* sK, const u4* sQ, const
                                                typename Ops<IO>::Image* below, AttImage* att, float (*scratch)[16 * 20], float scale, int wave, int c, int g) {
   using O = Ops<IO>;
   constexpr int TILES = kTiles * (kTiles + 1) / 2;
-  for (int job = wave; job < (ATT ? 2 : 1) * TILES; job += WAVES) {
+  constexpr int JOBS = (ATT ? 2 : 1) * TILES;
+  for (int round = 0; round * WAVES < JOBS; ++round) {
     // the diagonal tiles of k k^T first: their inverses take longest
+    const int job = job_of(round, wave, WAVES);
+    if (job >= JOBS) continue;
     const bool keys = job < TILES;
     int p = keys ? job : job - TILES, i, j;
     if (p < kTiles) {

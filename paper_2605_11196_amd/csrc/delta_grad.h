@@ -154,10 +154,10 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
       }
     }
     // ---- matrices between tokens
-    // 0, 1: Z (0,0) and (1,1), twice the work of the others; 2-4: X (0,0), (1,0), (1,1); 5-7: X^T of the same; 8: Z (1,0), 9: Z (0,1), which the
-    // waves after those of 0 and 1 take as their second
-    for (int job = (wave + (WAVES == 8 ? 6 : 0)) % WAVES; job < 10; job += WAVES) {
-      const int order = WAVES == 8 ? (job < 2 ? 2 + job : (job < 6 ? 4 + job - 2 : (job < 8 ? job - 6 : job))) : job;
+    // 0, 1: Z (0,0) and (1,1), twice the work of the others; 2-4: X (0,0), (1,0), (1,1); 5-7: X^T of the same; 8: Z (1,0), 9: Z (0,1)
+    for (int round = 0; round * WAVES < 10; ++round) {
+      const int order = job_of(round, wave, WAVES);
+      if (order >= 10) continue;
       const int kind = order < 2 ? 4 : (order < 5 ? 0 : (order < 8 ? 1 : order - 6));
       const int tile = order < 2 ? 2 * order : (order < 8 ? (order - 2) % 3 : 1);
       const int i = tile > 0 ? 1 : 0, j = tile > 1 ? 1 : 0;       // row tile i, column tile j of X and Y
