@@ -131,26 +131,32 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
     stage(t0);
     __syncthreads();
 
-    // ---- dbeta and v . dV of a token for each 16 lanes
+    // ---- dbeta and v . dV of a token for each 16 lanes; every load is under way before the first is used (one after the other they took
+    // a third of the kernel)
     for (int i = threadIdx.x / 16; i < kTok; i += THREADS / 16) {
-      const int t = t0 + i;
-      float wr = 0.0f, wv = 0.0f;
-      if (t < end) {
-        const float* W = a.rows + (row0 + t) * DV;
-        const float* R = a.R + (row0 + t) * DV;
-        const IO* values = reinterpret_cast<const IO*>(v + t * v_step);
+      const int t = min(t0 + i, end - 1), x = threadIdx.x % 16;
+      const float* W = a.rows + (row0 + t) * DV + x;
+      const float* R = a.R + (row0 + t) * DV + x;
+      const IO* values = reinterpret_cast<const IO*>(v + t * v_step) + x;
+      float w[DV / 16], r[DV / 16];
+      IO y[DV / 16];
 #pragma unroll
-        for (int x = 0; x < DV; x += 16) {
-          const int at = x + threadIdx.x % 16;
-          wr = fmaf(W[at], R[at], wr);
-          wv = fmaf(W[at], widen(values[at]), wv);
-        }
+      for (int n = 0; n < DV / 16; ++n) {
+        w[n] = W[16 * n];
+        r[n] = R[16 * n];
+        y[n] = values[16 * n];
+      }
+      float wr = 0.0f, wv = 0.0f;
+#pragma unroll
+      for (int n = 0; n < DV / 16; ++n) {
+        wr = fmaf(w[n], r[n], wr);
+        wv = fmaf(w[n], widen(y[n]), wv);
       }
       wr = row_sum16(wr);
       wv = row_sum16(wv);
-      if (threadIdx.x % 16 == 0) {
-        if (t < last) a.dbeta[row0 + t] = wr;
-        change[t - first] = -gates.beta[i] * wv;
+      if (x == 0) {
+        if (t0 + i < last) a.dbeta[row0 + t0 + i] = t0 + i < end ? wr : 0.0f;
+        change[t0 + i - first] = t0 + i < end ? -gates.beta[i] * wv : 0.0f;
       }
     }
     // ---- matrices between tokens
