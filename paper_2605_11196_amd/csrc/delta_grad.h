@@ -128,33 +128,39 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
   for (int t0 = first; t0 < end; t0 += kTok) {
     asm volatile("" : "+v"(c), "+v"(g));
     if (!AHEAD) request(t0);
-    stage(t0);
-    __syncthreads();
-
-    // ---- dbeta and v . dV of a token for each 16 lanes; every load is under way before the first is used (one after the other they took
-    // a third of the kernel)
-    for (int i = threadIdx.x / 16; i < kTok; i += THREADS / 16) {
+    // the values of W, R and v that the sums of a token take, with the rows: asked for after them they took a third of the kernel
+    struct {
+      float w[DV / 16], r[DV / 16];
+      IO y[DV / 16];
+    } dots;
+    auto request_dots = [&](int i) {
       const int t = min(t0 + i, end - 1), x = threadIdx.x % 16;
       const float* W = a.rows + (row0 + t) * DV + x;
       const float* R = a.R + (row0 + t) * DV + x;
       const IO* values = reinterpret_cast<const IO*>(v + t * v_step) + x;
-      float w[DV / 16], r[DV / 16];
-      IO y[DV / 16];
 #pragma unroll
       for (int n = 0; n < DV / 16; ++n) {
-        w[n] = W[16 * n];
-        r[n] = R[16 * n];
-        y[n] = values[16 * n];
+        dots.w[n] = W[16 * n];
+        dots.r[n] = R[16 * n];
+        dots.y[n] = values[16 * n];
       }
+    };
+    request_dots(threadIdx.x / 16);
+    stage(t0);
+    __syncthreads();
+
+    // ---- dbeta and v . dV of a token for each 16 lanes
+    for (int i = threadIdx.x / 16; i < kTok; i += THREADS / 16) {
+      if (i >= THREADS / 16) request_dots(i);
       float wr = 0.0f, wv = 0.0f;
 #pragma unroll
       for (int n = 0; n < DV / 16; ++n) {
-        wr = fmaf(w[n], r[n], wr);
-        wv = fmaf(w[n], widen(y[n]), wv);
+        wr = fmaf(dots.w[n], dots.r[n], wr);
+        wv = fmaf(dots.w[n], widen(dots.y[n]), wv);
       }
       wr = row_sum16(wr);
       wv = row_sum16(wv);
-      if (x == 0) {
+      if (threadIdx.x % 16 == 0) {
         if (t0 + i < last) a.dbeta[row0 + t0 + i] = t0 + i < end ? wr : 0.0f;
         change[t0 + i - first] = t0 + i < end ? -gates.beta[i] * wv : 0.0f;
       }
