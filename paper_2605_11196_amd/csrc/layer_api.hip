@@ -128,6 +128,7 @@ Segments delta_segments(long long heads, int T, int d_k, int d_v, int requested)
   }
   if (n > blocks) n = blocks;
   if (n > 256) n = 256;
+  if (n > 0x7fffffff / heads) n = 0x7fffffff / heads;   // workgroups
   if (n <= 1) return s;
   const int each = static_cast<int>((blocks + n - 1) / n);
   s.n = (blocks + each - 1) / each;
@@ -307,6 +308,7 @@ int vla_delta_backward(const void* q, const void* k, const void* v, const float*
     if (!rows_near(*r, es)) return VLA_ERR_UNSUPPORTED;
   }
   const long long heads = static_cast<long long>(B) * H_v;
+  if (heads * kept_states(T) > 0x7fffffffLL) return VLA_ERR_UNSUPPORTED;   // workgroups
   const BackwardParts parts = backward_parts(heads, T, d_k, d_v, H_v != H_k, op.segments);
   const size_t nS = static_cast<size_t>(heads) * d_v * d_k * 4, nG = static_cast<size_t>(heads) * T * 4;
   const size_t saved = vla_delta_saved_bytes(B, H_v, T, d_k, d_v, io_dtype);

@@ -159,13 +159,16 @@ def _autograd():
                 o, S_T, saved = gated_delta_forward(q, k, v, g, beta, S0, scale=scale, lengths=lengths, save_for_backward=True)
                 ctx.save_for_backward(q, k, v, g, beta, saved, lengths)
                 ctx.scale, ctx.has_state = scale, S0 is not None
+                ctx.set_materialize_grads(False)
                 return o, S_T
 
             @staticmethod
             @torch.autograd.function.once_differentiable
             def backward(ctx, do, dS_T):
                 q, k, v, g, beta, saved, lengths = ctx.saved_tensors
-                grads = gated_delta_backward(q, k, v, g, beta, saved, do, dS_T.contiguous(), scale=ctx.scale, lengths=lengths)
+                do = torch.zeros_like(v) if do is None else do
+                dS_T = None if dS_T is None else dS_T.contiguous()
+                grads = gated_delta_backward(q, k, v, g, beta, saved, do, dS_T, scale=ctx.scale, lengths=lengths)
                 return (*grads[:5], grads[5] if ctx.has_state else None, None, None)
 
         _function = GatedDelta

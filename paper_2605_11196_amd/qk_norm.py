@@ -166,12 +166,15 @@ def _autograd():
             def forward(ctx, q, k, q_weight, k_weight, cos, sin, positions, how):
                 ctx.save_for_backward(q, k, q_weight, k_weight, cos, sin, positions)
                 ctx.how = how
+                ctx.set_materialize_grads(False)
                 return _forward(q, k, q_weight, k_weight, cos, sin, positions, how["offset"], how["eps"], how["norm"], how["interleaved"], None)
 
             @staticmethod
             @torch.autograd.function.once_differentiable
             def backward(ctx, dq_out, dk_out):
                 q, k, q_weight, k_weight, cos, sin, positions = ctx.saved_tensors
+                dq_out = torch.zeros_like(q) if dq_out is None else dq_out
+                dk_out = torch.zeros_like(k) if dk_out is None else dk_out
                 dq, dk, dwq, dwk = qk_norm_rope_backward(q, k, q_weight, k_weight, cos, sin, dq_out, dk_out, positions=positions, **ctx.how)
                 cast = lambda g, w: g if g is None else g.to(w.dtype)
                 return dq, dk, cast(dwq, q_weight), cast(dwk, k_weight), None, None, None, None
