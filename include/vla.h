@@ -334,12 +334,12 @@ void vla_norm_default_opts(vla_norm_opts* opts);
 int vla_qk_norm_rope(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos, const float* sin,
                      void* q_out, void* k_out, int B, int T, int H_q, int H_k, int d, int io_dtype, const vla_norm_opts* opts,
                      void* stream);
-/* Its gradients: dq, dk, and those of the weights (float32 [d], summed over all rows in a fixed order; NULL: not wanted).  The
- * workspace is needed where one of the latter is wanted. */
+/* Its gradients: dq, dk, and those of the weights (opts->weight_dtype [d], summed over all rows in float32 in a fixed order; NULL: not
+ * wanted).  The workspace is needed where one of the latter is wanted. */
 size_t vla_qk_norm_rope_workspace_bytes(int d);
 int vla_qk_norm_rope_backward(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos,
-                              const float* sin, const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight,
-                              float* dk_weight, int B, int T, int H_q, int H_k, int d, int io_dtype, const vla_norm_opts* opts,
+                              const float* sin, const void* dq_out, const void* dk_out, void* dq, void* dk, void* dq_weight,
+                              void* dk_weight, int B, int T, int H_q, int H_k, int d, int io_dtype, const vla_norm_opts* opts,
                               void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus

@@ -439,8 +439,8 @@ int vla_qk_norm_rope(const void* q, const void* k, const void* q_weight, const v
 }
 
 int vla_qk_norm_rope_backward(const void* q, const void* k, const void* q_weight, const void* k_weight, const float* cos,
-                              const float* sin, const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight,
-                              float* dk_weight, int B, int T, int H_q, int H_k, int d, int io_dtype, const vla_norm_opts* opts,
+                              const float* sin, const void* dq_out, const void* dk_out, void* dq, void* dk, void* dq_weight,
+                              void* dk_weight, int B, int T, int H_q, int H_k, int d, int io_dtype, const vla_norm_opts* opts,
                               void* workspace, size_t workspace_bytes, void* stream) {
   vla_norm_opts op;
   vla::NormArgs a;
@@ -464,7 +464,7 @@ int vla_qk_norm_rope_backward(const void* q, const void* k, const void* q_weight
                      {a.positions, static_cast<size_t>(B) * T * 4, false},
                      {dq_out, reach(a.ys[0], B, H_q, T, d, es), false}, {dk_out, reach(a.ys[1], B, H_k, T, d, es), false},
                      {dq, reach(a.dxs[0], B, H_q, T, d, es), true}, {dk, reach(a.dxs[1], B, H_k, T, d, es), true},
-                     {dq_weight, static_cast<size_t>(d) * 4, true}, {dk_weight, static_cast<size_t>(d) * 4, true},
+                     {dq_weight, d * ws, true}, {dk_weight, d * ws, true},
                      {sums ? workspace : nullptr, need, true}};
   if (!disjoint(r, 14, nullptr, nullptr)) return VLA_ERR_INVALID_ARG;
   a.dy[0] = dq_out; a.dy[1] = dk_out; a.dx[0] = dq; a.dx[1] = dk;

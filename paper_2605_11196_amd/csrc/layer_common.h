@@ -22,7 +22,7 @@ struct NormArgs {
   const void* dy[2];       // backward
   void* dx[2];
   float* dw_part;          // [workgroups][2][d]
-  float* dw[2];            // [d] or nullptr
+  void* dw[2];             // [d], of the weights' type, or nullptr
   Rows xs[2], ys[2], dxs[2];
   int H[2];
   int B, T, rot, places, offset;

@@ -224,8 +224,9 @@ __global__ void __launch_bounds__(kThreads) dw_kernel(NormArgs a, int parts) {
   if (row == 0) {
     float all = 0.0f;
     for (int j = 0; j < 16; ++j) all += sums[threadIdx.x][j];
-    float* dw = a.dw[col / D];
-    if (dw != nullptr) dw[col % D] = all;
+    void* dw = a.dw[col / D];
+    if (dw != nullptr && a.w_bf16) io_store(static_cast<uint16_t*>(dw) + col % D, all);
+    else if (dw != nullptr) static_cast<float*>(dw)[col % D] = all;
   }
 }
 

@@ -52,6 +52,36 @@ def _inputs(q, k, v, g, beta, scale, lengths, segments=0):
     return (q, k, v, g, beta, lengths), op
 
 
+def _forward(torch, kept, op, S0, save, stream):
+    """kept, op: of _inputs(), the inputs checked.  (o, S_T, what the backward pass needs or None)."""
+    q, k, v, g, beta, _ = kept
+    B, H_k, T, dk = q.shape
+    H_v, dv, dev, io = v.shape[1], v.shape[3], q.device, _io(torch, q)
+    lib = binding.load_library()
+    handle, context, outside = binding._on_stream(torch, dev, stream)
+    with context:
+        o = _like(torch, v)
+        if not o.is_contiguous():
+            op.o = _strides(o)
+        S_T = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
+        saved = None
+        if save:
+            op.saved_bytes = lib.vla_delta_saved_bytes(B, H_v, T, dk, dv, io)
+            saved = torch.empty((max(op.saved_bytes, 16),), dtype=torch.uint8, device=dev)
+            op.saved = saved.data_ptr()
+        need = lib.vla_delta_workspace_bytes(B, H_k, H_v, T, dk, dv, io, ctypes.byref(op), 0)
+        ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
+        if outside is not None:
+            for t in (o, S_T, saved):
+                if t is not None:
+                    t.record_stream(outside)
+        rc = lib.vla_delta_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), _p(S0), o.data_ptr(), S_T.data_ptr(), B,
+                                   H_k, H_v, T, dk, dv, io, ctypes.byref(op), _p(ws), need, handle)
+    if rc != 0:
+        raise VlaError(rc, binding.status_string(rc), "vla_delta_forward")
+    return o, S_T, saved
+
+
 def gated_delta_forward(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, save_for_backward=False, segments=0, stream=None):
     """S' = exp(g_t) S;  S <- S' + beta_t (v_t - S' k_t) k_t^T;  o_t = scale S q_t  for every value head.
 
@@ -64,30 +94,9 @@ def gated_delta_forward(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, 
     import torch
 
     _check(torch, q, k, v, g, beta, S0, "S0", lengths, 1)
-    io, (B, H_k, T, dk), H_v, dv, dev = _io(torch, q), q.shape, v.shape[1], v.shape[-1], q.device
-    lib = binding.load_library()
-    handle, context, outside = binding._on_stream(torch, dev, stream)
-    with context:
+    with binding._on_stream(torch, q.device, stream)[1]:
         kept, op = _inputs(q, k, v, g, beta, scale, lengths, segments)
-        o = _like(torch, v)
-        if not o.is_contiguous():
-            op.o = _strides(o)
-        S_T = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
-        saved = None
-        if save_for_backward:
-            op.saved_bytes = lib.vla_delta_saved_bytes(B, H_v, T, dk, dv, io)
-            saved = torch.empty((max(op.saved_bytes, 16),), dtype=torch.uint8, device=dev)
-            op.saved = saved.data_ptr()
-        need = lib.vla_delta_workspace_bytes(B, H_k, H_v, T, dk, dv, io, ctypes.byref(op), 0)
-        ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
-        if outside is not None:
-            for t in (o, S_T, saved):
-                if t is not None:
-                    t.record_stream(outside)
-        rc = lib.vla_delta_forward(*(_p(x) for x in kept[:5]), _p(S0), _p(o), _p(S_T), B, H_k, H_v, T, dk, dv, io, ctypes.byref(op),
-                                   _p(ws), need, handle)
-    if rc != 0:
-        raise VlaError(rc, binding.status_string(rc), "vla_delta_forward")
+    o, S_T, saved = _forward(torch, kept, op, S0, save_for_backward, stream)
     return (o, S_T, saved) if save_for_backward else (o, S_T)
 
 
@@ -113,19 +122,14 @@ def gated_delta_decode_step(q, k, v, g, beta, S, *, scale=None, stream=None):
     return o
 
 
-def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, lengths=None, segments=0, stream=None):
-    """The gradients (dq, dk, dv, dg, dbeta, dS0) of gated_delta_forward's inputs, given those of o and S_T (None: zero), the same inputs
-    and what it saved.  dg, dbeta and dS0 are float32."""
-    import torch
-
-    _check(torch, q, k, v, g, beta, dS_T, "dS_T", lengths, 1)
-    if do.shape != v.shape or do.dtype != v.dtype or do.device != v.device:
-        raise ValueError("do must match v in shape, dtype and device")
-    io, (B, H_k, T, dk), H_v, dv, dev = _io(torch, q), q.shape, v.shape[1], v.shape[-1], q.device
+def _backward(torch, kept, op, saved, do, dS_T, stream):
+    """The gradients, with kept and op of the forward pass (strides of o and of outputs are set here)."""
+    q, k, v, g, beta, _ = kept
+    B, H_k, T, dk = q.shape
+    H_v, dv, dev, io = v.shape[1], v.shape[3], q.device, _io(torch, q)
     lib = binding.load_library()
     handle, context, outside = binding._on_stream(torch, dev, stream)
     with context:
-        kept, op = _inputs(q, k, v, g, beta, scale, lengths, segments)
         do, op.o = _laid_out(do)
         dq, dk_, dv_ = _like(torch, q), _like(torch, k), _like(torch, v)
         dg, dbeta = (torch.empty((B, H_v, T), dtype=torch.float32, device=dev) for _ in range(2))
@@ -138,11 +142,25 @@ def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, 
         if outside is not None:
             for t in outputs:
                 t.record_stream(outside)
-        rc = lib.vla_delta_backward(*(_p(x) for x in kept[:5]), _p(do), _p(dS_T), *(_p(x) for x in outputs), B, H_k, H_v, T, dk, dv, io,
+        rc = lib.vla_delta_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), do.data_ptr(), _p(dS_T), dq.data_ptr(),
+                                    dk_.data_ptr(), dv_.data_ptr(), dg.data_ptr(), dbeta.data_ptr(), dS0.data_ptr(), B, H_k, H_v, T, dk, dv, io,
                                     ctypes.byref(op), _p(ws), need, handle)
     if rc != 0:
         raise VlaError(rc, binding.status_string(rc), "vla_delta_backward")
     return outputs
+
+
+def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, lengths=None, segments=0, stream=None):
+    """The gradients (dq, dk, dv, dg, dbeta, dS0) of gated_delta_forward's inputs, given those of o and S_T (None: zero), the same inputs
+    and what it saved.  dg, dbeta and dS0 are float32."""
+    import torch
+
+    _check(torch, q, k, v, g, beta, dS_T, "dS_T", lengths, 1)
+    if do.shape != v.shape or do.dtype != v.dtype or do.device != v.device:
+        raise ValueError("do must match v in shape, dtype and device")
+    with binding._on_stream(torch, q.device, stream)[1]:
+        kept, op = _inputs(q, k, v, g, beta, scale, lengths, segments)
+    return _backward(torch, kept, op, saved, do, dS_T, stream)
 
 
 _function = None
@@ -156,19 +174,21 @@ def _autograd():
         class GatedDelta(torch.autograd.Function):
             @staticmethod
             def forward(ctx, q, k, v, g, beta, S0, scale, lengths):
-                o, S_T, saved = gated_delta_forward(q, k, v, g, beta, S0, scale=scale, lengths=lengths, save_for_backward=True)
-                ctx.save_for_backward(q, k, v, g, beta, saved, lengths)
-                ctx.scale, ctx.has_state = scale, S0 is not None
+                kept, op = _inputs(q, k, v, g, beta, scale, lengths)
+                o, S_T, saved = _forward(torch, kept, op, S0, True, None)
+                ctx.save_for_backward(*kept, saved)      # the inputs as the kernels read them
+                ctx.op, ctx.has_state = op, S0 is not None
                 ctx.set_materialize_grads(False)
                 return o, S_T
 
             @staticmethod
             @torch.autograd.function.once_differentiable
             def backward(ctx, do, dS_T):
-                q, k, v, g, beta, saved, lengths = ctx.saved_tensors
-                do = torch.zeros_like(v) if do is None else do
+                *kept, saved = ctx.saved_tensors
+                do = torch.zeros_like(kept[2]) if do is None else do
                 dS_T = None if dS_T is None else dS_T.contiguous()
-                grads = gated_delta_backward(q, k, v, g, beta, saved, do, dS_T, scale=ctx.scale, lengths=lengths)
+                op = VlaDeltaOpts.from_buffer_copy(ctx.op)
+                grads = _backward(torch, kept, op, saved, do, dS_T, None)
                 return (*grads[:5], grads[5] if ctx.has_state else None, None, None)
 
         _function = GatedDelta
@@ -179,8 +199,11 @@ def gated_delta(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, stream=N
     """gated_delta_forward as a differentiable function: (o, S_T), with gradients for q, k, v, g, beta and S0 (on the current stream)."""
     import torch
 
-    if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in (q, k, v, g, beta, S0)):
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or g.requires_grad or beta.requires_grad
+                                    or S0 is not None and S0.requires_grad):
         if stream is not None:
             raise ValueError("with gradients the work goes to the current stream: leave stream at None")
-        return _autograd().apply(q, k, v, g, beta, S0, scale, lengths)
+        _check(torch, q, k, v, g, beta, S0, "S0", lengths, 1)
+        with binding._on_device(torch, q.device):
+            return _autograd().apply(q, k, v, g, beta, S0, scale, lengths)
     return gated_delta_forward(q, k, v, g, beta, S0, scale=scale, lengths=lengths, stream=stream)

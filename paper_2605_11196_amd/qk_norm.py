@@ -101,56 +101,65 @@ def _p(x):
     return None if x is None else x.data_ptr()
 
 
-def _forward(q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, interleaved, stream):
-    import torch
-
-    _check(torch, q, k, q_weight, k_weight, cos, sin, positions, norm)
-    io, (B, H_q, T, d), H_k, dev = _io(torch, q), q.shape, k.shape[1], q.device
-    lib = binding.load_library()
+def _forward(torch, kept, op, stream):
+    """kept, op: of _call(), the inputs checked.  (q, k) after the norm and the rotation."""
+    q, k = kept[0], kept[1]
+    B, H_q, T, d = q.shape
+    dev = q.device
     handle, context, outside = binding._on_stream(torch, dev, stream)
     with context:
-        kept, op = _call(torch, q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, interleaved)
         q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
         if outside is not None:
             q_out.record_stream(outside)
             k_out.record_stream(outside)
-        rc = lib.vla_qk_norm_rope(_p(kept[0]), _p(kept[1]), _p(kept[2]), _p(kept[3]), _p(kept[4]), _p(kept[5]), q_out.data_ptr(),
-                                  k_out.data_ptr(), B, T, H_q, H_k, d, io, ctypes.byref(op), handle)
+        rc = binding.load_library().vla_qk_norm_rope(
+            q.data_ptr(), k.data_ptr(), _p(kept[2]), _p(kept[3]), _p(kept[4]), _p(kept[5]), q_out.data_ptr(), k_out.data_ptr(), B, T, H_q,
+            k.shape[1], d, _io(torch, q), ctypes.byref(op), handle)
     if rc != 0:
         raise VlaError(rc, binding.status_string(rc), "vla_qk_norm_rope")
     return q_out, k_out
 
 
+def _backward(torch, kept, op, dq_out, dk_out, stream):
+    """The gradients (dq, dk, dq_weight, dk_weight), with kept and op of the forward pass."""
+    q, k, q_weight, k_weight = kept[:4]
+    B, H_q, T, d = q.shape
+    dev = q.device
+    lib = binding.load_library()
+    handle, context, outside = binding._on_stream(torch, dev, stream)
+    with context:
+        (dq_out, op.q_out), (dk_out, op.k_out) = _laid_out(dq_out), _laid_out(dk_out)
+        dq, dk = _like(torch, q), _like(torch, k)
+        op.dq, op.dk = _strides(dq), _strides(dk)
+        dwq = None if q_weight is None else torch.empty_like(q_weight)
+        dwk = None if k_weight is None else torch.empty_like(k_weight)
+        need = lib.vla_qk_norm_rope_workspace_bytes(d) if q_weight is not None or k_weight is not None else 0
+        ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
+        if outside is not None:
+            for t in (dq, dk, dwq, dwk):
+                if t is not None:
+                    t.record_stream(outside)
+        rc = lib.vla_qk_norm_rope_backward(
+            q.data_ptr(), k.data_ptr(), _p(q_weight), _p(k_weight), _p(kept[4]), _p(kept[5]), dq_out.data_ptr(), dk_out.data_ptr(),
+            dq.data_ptr(), dk.data_ptr(), _p(dwq), _p(dwk), B, T, H_q, k.shape[1], d, _io(torch, q), ctypes.byref(op), _p(ws), need, handle)
+    if rc != 0:
+        raise VlaError(rc, binding.status_string(rc), "vla_qk_norm_rope_backward")
+    return dq, dk, dwq, dwk
+
+
 def qk_norm_rope_backward(q, k, q_weight, k_weight, cos, sin, dq_out, dk_out, *, positions=None, offset=0, eps=1e-6, norm="rms",
                           interleaved=False, stream=None):
-    """The gradients of qk_norm_rope's q, k, q_weight and k_weight (the last two float32, None where there is no weight), given
-    those of its outputs."""
+    """The gradients of qk_norm_rope's q, k, q_weight and k_weight (None where there is no weight; summed in float32 and of the weights'
+    type), given those of its outputs."""
     import torch
 
     _check(torch, q, k, q_weight, k_weight, cos, sin, positions, norm)
     if any(y.shape != x.shape or y.dtype != x.dtype or y.device != x.device for x, y in ((q, dq_out), (k, dk_out))):
         raise ValueError("dq_out and dk_out must match q and k in shape, dtype and device")
-    io, (B, H_q, T, d), H_k, dev = _io(torch, q), q.shape, k.shape[1], q.device
-    lib = binding.load_library()
-    handle, context, outside = binding._on_stream(torch, dev, stream)
-    with context:
-        kept, op = _call(torch, q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, interleaved)
-        (dq_out, op.q_out), (dk_out, op.k_out) = _laid_out(dq_out), _laid_out(dk_out)
-        dq, dk = _like(torch, q), _like(torch, k)
-        op.dq, op.dk = _strides(dq), _strides(dk)
-        dw = [None if w is None else torch.empty((d,), dtype=torch.float32, device=dev) for w in (q_weight, k_weight)]
-        need = lib.vla_qk_norm_rope_workspace_bytes(d) if q_weight is not None or k_weight is not None else 0
-        ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
-        if outside is not None:
-            for t in (dq, dk, *dw):
-                if t is not None:
-                    t.record_stream(outside)
-        rc = lib.vla_qk_norm_rope_backward(*(_p(x) for x in kept[:6]), _p(dq_out), _p(dk_out), _p(dq), _p(dk), _p(dw[0]), _p(dw[1]), B, T,
-                                           H_q, H_k, d, io, ctypes.byref(op), _p(ws), need, handle)
-    if rc != 0:
-        raise VlaError(rc, binding.status_string(rc), "vla_qk_norm_rope_backward")
-    return dq, dk, dw[0], dw[1]
+    with binding._on_stream(torch, q.device, stream)[1]:
+        kept, op = _call(torch, q, k, q_weight, k_weight, cos, sin, positions, int(offset), float(eps), norm, interleaved)
+    return _backward(torch, kept, op, dq_out, dk_out, stream)
 
 
 _function = None
@@ -164,20 +173,20 @@ def _autograd():
         class QkNormRope(torch.autograd.Function):
             @staticmethod
             def forward(ctx, q, k, q_weight, k_weight, cos, sin, positions, how):
-                ctx.save_for_backward(q, k, q_weight, k_weight, cos, sin, positions)
-                ctx.how = how
+                kept, op = _call(torch, q, k, q_weight, k_weight, cos, sin, positions, *how)
+                ctx.save_for_backward(*kept)     # the inputs as the kernels read them
+                ctx.op = op
                 ctx.set_materialize_grads(False)
-                return _forward(q, k, q_weight, k_weight, cos, sin, positions, how["offset"], how["eps"], how["norm"], how["interleaved"], None)
+                return _forward(torch, kept, op, None)
 
             @staticmethod
             @torch.autograd.function.once_differentiable
             def backward(ctx, dq_out, dk_out):
-                q, k, q_weight, k_weight, cos, sin, positions = ctx.saved_tensors
-                dq_out = torch.zeros_like(q) if dq_out is None else dq_out
-                dk_out = torch.zeros_like(k) if dk_out is None else dk_out
-                dq, dk, dwq, dwk = qk_norm_rope_backward(q, k, q_weight, k_weight, cos, sin, dq_out, dk_out, positions=positions, **ctx.how)
-                cast = lambda g, w: g if g is None else g.to(w.dtype)
-                return dq, dk, cast(dwq, q_weight), cast(dwk, k_weight), None, None, None, None
+                kept = ctx.saved_tensors
+                dq_out = torch.zeros_like(kept[0]) if dq_out is None else dq_out
+                dk_out = torch.zeros_like(kept[1]) if dk_out is None else dk_out
+                op = VlaNormOpts.from_buffer_copy(ctx.op)
+                return (*_backward(torch, kept, op, dq_out, dk_out, None), None, None, None, None)
 
         _function = QkNormRope
     return _function
@@ -195,10 +204,15 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, cos=None, sin=None, *, posi
     """
     import torch
 
-    offset, eps = int(offset), float(eps)
-    if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in (q, k, q_weight, k_weight)):
+    how = (int(offset), float(eps), norm, interleaved)
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or q_weight is not None and q_weight.requires_grad
+                                    or k_weight is not None and k_weight.requires_grad):
         if stream is not None:
             raise ValueError("with gradients the work goes to the current stream: leave stream at None")
-        how = dict(offset=offset, eps=eps, norm=norm, interleaved=interleaved)
-        return _autograd().apply(q, k, q_weight, k_weight, cos, sin, positions, how)
-    return _forward(q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, interleaved, stream)
+        _check(torch, q, k, q_weight, k_weight, cos, sin, positions, norm)
+        with binding._on_device(torch, q.device):
+            return _autograd().apply(q, k, q_weight, k_weight, cos, sin, positions, how)
+    _check(torch, q, k, q_weight, k_weight, cos, sin, positions, norm)
+    with binding._on_device(torch, q.device) if stream is None else binding._on_stream(torch, q.device, stream)[1]:
+        kept, op = _call(torch, q, k, q_weight, k_weight, cos, sin, positions, *how)
+    return _forward(torch, kept, op, stream)
