@@ -114,7 +114,9 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
       const Gates& gt = gates[turn];
       turn ^= 1;
       __syncthreads();
+      __builtin_amdgcn_s_setprio(2);   // as in the forward kernel
       token_matrices<IO, RK, KT / 2, WAVES, true, true>(sK, sQ, gt, inverse, below, att, scratch, a.scale, wave, c, g);
+      __builtin_amdgcn_s_setprio(0);
 
       // ---- P = K dS^T
       f4 P[kTiles] = {zero, zero};
@@ -133,6 +135,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
       // ---- W, the gradient of v, the state's gradient
       const auto gate4 = [&](const float* from, int tile) { return *reinterpret_cast<const f4*>(from + 16 * tile + 4 * g); };
       static_assert(kTiles == 2, "one pair of token tiles");
+      __builtin_amdgcn_s_setprio(1);
       const bool values = !MAP || wave * 16 < DV;      // the columns of the map have no dO
       const float decay = gt.end;
       typename O::Raw d[kTiles];
@@ -187,6 +190,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
         }
         S[kt] = x;
       }
+      __builtin_amdgcn_s_setprio(0);
       next_gates(t0 - kTok, gates[turn]);
       request_gates(t0 - 2 * kTok);
       __syncthreads();
