@@ -1,5 +1,6 @@
 """The gated delta rule on torch tensors (vla_delta_forward, vla_delta_decode_step and vla_delta_backward of include/vla.h)."""
 import ctypes
+import functools
 
 from . import binding
 from .binding import VlaDeltaOpts, VlaError, VlaStrides
@@ -52,31 +53,38 @@ def _inputs(q, k, v, g, beta, scale, lengths, segments=0):
     return (q, k, v, g, beta, lengths), op
 
 
-def _forward(torch, kept, op, S0, save, stream):
-    """kept, op: of _inputs(), the inputs checked.  (o, S_T, what the backward pass needs or None)."""
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(B, H_k, H_v, T, dk, dv, io, segments, backward):
+    """vla_delta_workspace_bytes, which depends on nothing else."""
+    op = VlaDeltaOpts()
+    op.segments = segments
+    return binding.load_library().vla_delta_workspace_bytes(B, H_k, H_v, T, dk, dv, io, ctypes.byref(op), backward)
+
+
+def _forward(torch, kept, op, S0, save, handle, outside):
+    """kept, op: of _inputs(), the inputs checked; handle, outside: of binding._on_stream(), in whose context this runs.
+    (o, S_T, what the backward pass needs or None)."""
     q, k, v, g, beta, _ = kept
     B, H_k, T, dk = q.shape
     H_v, dv, dev, io = v.shape[1], v.shape[3], q.device, _io(torch, q)
     lib = binding.load_library()
-    handle, context, outside = binding._on_stream(torch, dev, stream)
-    with context:
-        o = _like(torch, v)
-        if not o.is_contiguous():
-            op.o = _strides(o)
-        S_T = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
-        saved = None
-        if save:
-            op.saved_bytes = lib.vla_delta_saved_bytes(B, H_v, T, dk, dv, io)
-            saved = torch.empty((max(op.saved_bytes, 16),), dtype=torch.uint8, device=dev)
-            op.saved = saved.data_ptr()
-        need = lib.vla_delta_workspace_bytes(B, H_k, H_v, T, dk, dv, io, ctypes.byref(op), 0)
-        ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
-        if outside is not None:
-            for t in (o, S_T, saved):
-                if t is not None:
-                    t.record_stream(outside)
-        rc = lib.vla_delta_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), _p(S0), o.data_ptr(), S_T.data_ptr(), B,
-                                   H_k, H_v, T, dk, dv, io, ctypes.byref(op), _p(ws), need, handle)
+    o = _like(torch, v)
+    if not o.is_contiguous():
+        op.o = _strides(o)
+    S_T = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
+    saved = None
+    if save:
+        op.saved_bytes = lib.vla_delta_saved_bytes(B, H_v, T, dk, dv, io)
+        saved = torch.empty((max(op.saved_bytes, 16),), dtype=torch.uint8, device=dev)
+        op.saved = saved.data_ptr()
+    need = _workspace_bytes(B, H_k, H_v, T, dk, dv, io, op.segments, 0)
+    ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
+    if outside is not None:
+        for t in (o, S_T, saved):
+            if t is not None:
+                t.record_stream(outside)
+    rc = lib.vla_delta_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), _p(S0), o.data_ptr(), S_T.data_ptr(), B, H_k,
+                               H_v, T, dk, dv, io, ctypes.byref(op), _p(ws), need, handle)
     if rc != 0:
         raise VlaError(rc, binding.status_string(rc), "vla_delta_forward")
     return o, S_T, saved
@@ -94,9 +102,11 @@ def gated_delta_forward(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, 
     import torch
 
     _check(torch, q, k, v, g, beta, S0, "S0", lengths, 1)
-    with binding._on_stream(torch, q.device, stream)[1]:
+    binding.load_library()
+    handle, context, outside = binding._on_stream(torch, q.device, stream)
+    with context:
         kept, op = _inputs(q, k, v, g, beta, scale, lengths, segments)
-    o, S_T, saved = _forward(torch, kept, op, S0, save_for_backward, stream)
+        o, S_T, saved = _forward(torch, kept, op, S0, save_for_backward, handle, outside)
     return (o, S_T, saved) if save_for_backward else (o, S_T)
 
 
@@ -136,7 +146,7 @@ def _backward(torch, kept, op, saved, do, dS_T, stream):
         dS0 = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
         op.dq, op.dk, op.dv = _strides(dq), _strides(dk_), _strides(dv_)
         op.saved, op.saved_bytes = saved.data_ptr(), saved.numel()
-        need = lib.vla_delta_workspace_bytes(B, H_k, H_v, T, dk, dv, io, ctypes.byref(op), 1)
+        need = _workspace_bytes(B, H_k, H_v, T, dk, dv, io, op.segments, 1)
         ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
         outputs = (dq, dk_, dv_, dg, dbeta, dS0)
         if outside is not None:
@@ -174,8 +184,10 @@ def _autograd():
         class GatedDelta(torch.autograd.Function):
             @staticmethod
             def forward(ctx, q, k, v, g, beta, S0, scale, lengths):
-                kept, op = _inputs(q, k, v, g, beta, scale, lengths)
-                o, S_T, saved = _forward(torch, kept, op, S0, True, None)
+                handle, context, outside = binding._on_stream(torch, q.device, None)
+                with context:
+                    kept, op = _inputs(q, k, v, g, beta, scale, lengths)
+                    o, S_T, saved = _forward(torch, kept, op, S0, True, handle, outside)
                 ctx.save_for_backward(*kept, saved)      # the inputs as the kernels read them
                 ctx.op, ctx.has_state = op, S0 is not None
                 ctx.set_materialize_grads(False)
@@ -204,6 +216,5 @@ def gated_delta(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, stream=N
         if stream is not None:
             raise ValueError("with gradients the work goes to the current stream: leave stream at None")
         _check(torch, q, k, v, g, beta, S0, "S0", lengths, 1)
-        with binding._on_device(torch, q.device):
-            return _autograd().apply(q, k, v, g, beta, S0, scale, lengths)
+        return _autograd().apply(q, k, v, g, beta, S0, scale, lengths)
     return gated_delta_forward(q, k, v, g, beta, S0, scale=scale, lengths=lengths, stream=stream)

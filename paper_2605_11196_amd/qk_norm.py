@@ -101,21 +101,19 @@ def _p(x):
     return None if x is None else x.data_ptr()
 
 
-def _forward(torch, kept, op, stream):
-    """kept, op: of _call(), the inputs checked.  (q, k) after the norm and the rotation."""
+def _forward(torch, kept, op, handle, outside):
+    """kept, op: of _call(), the inputs checked; handle, outside: of binding._on_stream(), in whose context this runs.  (q, k) after the
+    norm and the rotation."""
     q, k = kept[0], kept[1]
     B, H_q, T, d = q.shape
-    dev = q.device
-    handle, context, outside = binding._on_stream(torch, dev, stream)
-    with context:
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-        if outside is not None:
-            q_out.record_stream(outside)
-            k_out.record_stream(outside)
-        rc = binding.load_library().vla_qk_norm_rope(
-            q.data_ptr(), k.data_ptr(), _p(kept[2]), _p(kept[3]), _p(kept[4]), _p(kept[5]), q_out.data_ptr(), k_out.data_ptr(), B, T, H_q,
-            k.shape[1], d, _io(torch, q), ctypes.byref(op), handle)
+    q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+    if outside is not None:
+        q_out.record_stream(outside)
+        k_out.record_stream(outside)
+    rc = binding.load_library().vla_qk_norm_rope(
+        q.data_ptr(), k.data_ptr(), _p(kept[2]), _p(kept[3]), _p(kept[4]), _p(kept[5]), q_out.data_ptr(), k_out.data_ptr(), B, T, H_q, k.shape[1],
+        d, _io(torch, q), ctypes.byref(op), handle)
     if rc != 0:
         raise VlaError(rc, binding.status_string(rc), "vla_qk_norm_rope")
     return q_out, k_out
@@ -173,11 +171,13 @@ def _autograd():
         class QkNormRope(torch.autograd.Function):
             @staticmethod
             def forward(ctx, q, k, q_weight, k_weight, cos, sin, positions, how):
-                kept, op = _call(torch, q, k, q_weight, k_weight, cos, sin, positions, *how)
-                ctx.save_for_backward(*kept)     # the inputs as the kernels read them
-                ctx.op = op
-                ctx.set_materialize_grads(False)
-                return _forward(torch, kept, op, None)
+                handle, context, outside = binding._on_stream(torch, q.device, None)
+                with context:
+                    kept, op = _call(torch, q, k, q_weight, k_weight, cos, sin, positions, *how)
+                    ctx.save_for_backward(*kept)     # the inputs as the kernels read them
+                    ctx.op = op
+                    ctx.set_materialize_grads(False)
+                    return _forward(torch, kept, op, handle, outside)
 
             @staticmethod
             @torch.autograd.function.once_differentiable
@@ -210,9 +210,9 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, cos=None, sin=None, *, posi
         if stream is not None:
             raise ValueError("with gradients the work goes to the current stream: leave stream at None")
         _check(torch, q, k, q_weight, k_weight, cos, sin, positions, norm)
-        with binding._on_device(torch, q.device):
-            return _autograd().apply(q, k, q_weight, k_weight, cos, sin, positions, how)
+        return _autograd().apply(q, k, q_weight, k_weight, cos, sin, positions, how)
     _check(torch, q, k, q_weight, k_weight, cos, sin, positions, norm)
-    with binding._on_device(torch, q.device) if stream is None else binding._on_stream(torch, q.device, stream)[1]:
+    handle, context, outside = binding._on_stream(torch, q.device, stream)
+    with context:
         kept, op = _call(torch, q, k, q_weight, k_weight, cos, sin, positions, *how)
-    return _forward(torch, kept, op, stream)
+        return _forward(torch, kept, op, handle, outside)
