@@ -8,7 +8,8 @@
 // for 96 columns, 12 of them at work), eight columns a lane, chosen so that a pair lies in one lane: with halves apart,
 // four columns at the lane's place in each half; so no value crosses lanes but the sum of squares (DPP).  A group of lanes stays
 // with one token and goes through its heads, which keeps the position, its cosines and sines and the weights on
-// registers.  The sums are float32.
+// registers.  The sums are float32.  524288 rows of 64 in bf16 25 us (5.3 TB/s), 2.6 million rows of 128 with gradients
+// 0.25 + 0.43 ms (5.3 and 4.7 TB/s).
 #include "layer_common.h"
 #include "vla_mfma_util.h"
 
