@@ -285,6 +285,8 @@ size_t vla_delta_saved_bytes(int B, int H_v, int T, int d_k, int d_v, int io_dty
  * Sums, decays and the state are float32 whatever io_dtype; products of the state with q, k and the writes are formed from parts
  * that carry all of its bits (bf16: the read-out, which is rounded to bf16, from 16 of them).  q, k, v, o, S0 and S_T are
  * 16-byte aligned.  Running [0, T1) and then [T1, T) with the carried S_T gives the same result as one call up to rounding.
+ * Tokens go through the matrix unit 16 at a time: an infinite or NaN value reaches, besides all that follows it, the outputs of up to
+ * 15 tokens before it (never those of another head or sequence).
  */
 int vla_delta_forward(const void* q, const void* k, const void* v, const float* g, const float* beta, const float* S0, void* o,
                       float* S_T, int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, const vla_delta_opts* opts,
@@ -299,7 +301,9 @@ int vla_delta_decode_step(const void* q, const void* k, const void* v, const flo
  *   dO      [B, H_v, T, d_v] io_dtype;  dS_T [B, H_v, d_v, d_k] float32 or NULL (zero)
  *   dq, dk  [B, H_k, T, d_k] io_dtype, summed over the value heads that share a key head, in a fixed order
  *   dv      [B, H_v, T, d_v] io_dtype;  dg, dbeta [B, H_v, T] float32;  dS0 [B, H_v, d_v, d_k] float32 or NULL (not wanted)
- * The same inputs and saved states give the same bits.
+ * The same inputs and saved states give the same bits.  dg is the sum of the differences dO_i . O_i - v_i . dV_i over up to 256 tokens and of
+ * <dS, S> behind them, and exact to float32's rounding of these terms: where strong decays make it far smaller than they are, what is
+ * left of their rounding (1e-7 of them) shows.
  */
 int vla_delta_backward(const void* q, const void* k, const void* v, const float* g, const float* beta, const void* dO, const float* dS_T,
                        void* dq, void* dk, void* dv, float* dg, float* dbeta, float* dS0, int B, int H_k, int H_v, int T, int d_k,

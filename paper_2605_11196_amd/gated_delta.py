@@ -37,9 +37,24 @@ def _check(torch, q, k, v, g, beta, state, state_name, lengths, tokens):
         raise ValueError(f"lengths must be an int32 tensor of shape {tuple(shape[:1])} on {dev}")
 
 
+def _scale(scale):
+    """The option's value, where 0 stands for the default."""
+    if scale is None:
+        return 0.0
+    if scale == 0:
+        raise ValueError("scale must not be 0 (None: 1 / sqrt(d_k))")
+    return scale
+
+
+def _aligned(x):
+    """x in order from a 16-byte boundary on."""
+    x = x.contiguous()
+    return x.clone() if x.data_ptr() % 16 else x
+
+
 def _inputs(q, k, v, g, beta, scale, lengths, segments=0):
     """The inputs as the kernels take them, kept until the call, and its options."""
-    op = VlaDeltaOpts(scale or 0.0)
+    op = VlaDeltaOpts(_scale(scale))
     op.segments = segments
     (q, op.q), (k, op.k), (v, op.v) = _laid_out(q), _laid_out(k), _laid_out(v)
     (g, g_strides), (beta, beta_strides) = _gate(g), _gate(beta)
@@ -120,11 +135,11 @@ def gated_delta_decode_step(q, k, v, g, beta, S, *, scale=None, stream=None):
     lib = binding.load_library()
     handle, context, outside = binding._on_stream(torch, dev, stream)
     with context:
-        q, k, v, g, beta = q.contiguous(), k.contiguous(), v.contiguous(), g.contiguous(), beta.contiguous()
+        q, k, v, g, beta = _aligned(q), _aligned(k), _aligned(v), g.contiguous(), beta.contiguous()
         o = torch.empty_like(v)
         if outside is not None:
             o.record_stream(outside)
-        op = VlaDeltaOpts(scale=scale or 0.0)
+        op = VlaDeltaOpts(_scale(scale))
         rc = lib.vla_delta_decode_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), S.data_ptr(),
                                        o.data_ptr(), B, H_k, H_v, dk, dv, io, ctypes.byref(op), handle)
     if rc != 0:

@@ -212,3 +212,48 @@ def test_time_segments(d_k, d_v, T, segments, dtype):
     whole = vla.gated_delta_forward(*inputs, segments=1)
     cut = vla.gated_delta_forward(*inputs, segments=segments)
     close(cut[1], whole[1].double(), 2 * TOL["f32"], "S_T against one segment")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("segments", [1, 3])
+def test_a_nan_reaches_back_no_further_than_its_tile(dtype, segments):
+    """Outputs up to the 16 tokens that a NaN lies in, and those of other heads and sequences, do not change at all."""
+    clean = make(2, 2, 4, 300, 64, 64, dtype, seed=21)
+    o, S = vla.gated_delta_forward(*clean, segments=segments)
+    for which, place in ((0, (1, 1, 150)), (1, (1, 1, 150)), (2, (1, 2, 150)), (3, (1, 2, 150)), (4, (1, 2, 150))):
+        inputs = [x.clone() for x in clean]
+        inputs[which][place] = float("nan")
+        o2, S2 = vla.gated_delta_forward(*inputs, segments=segments)
+        assert torch.equal(o2[0], o[0]) and torch.equal(o2[1, :2], o[1, :2]) and torch.equal(S2[1, :2], S[1, :2]) and torch.equal(S2[0], S[0])
+        assert torch.equal(o2[1, 2, :144], o[1, 2, :144])
+        assert o2[1, 2, 150].isnan().any()
+        if which in (2, 3, 4):
+            assert torch.equal(o2[1, 3], o[1, 3])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_start_anywhere(dtype):
+    """Contiguous tensors that do not start at a 16-byte boundary, over tokens and for one."""
+    inputs = make(2, 2, 2, 40, 32, 32, dtype, seed=22)
+    moved = []
+    for x in inputs[:3]:
+        room = torch.empty(x.numel() + 3, dtype=x.dtype, device="cuda")
+        moved.append(room[3:].view(x.shape).copy_(x))
+    o, S = vla.gated_delta_forward(*inputs)
+    o2, S2 = vla.gated_delta_forward(*moved, *inputs[3:])
+    assert torch.equal(o, o2) and torch.equal(S, S2)
+    one = [x[:, :, 0].contiguous() for x in inputs[:5]]
+    odd = []
+    for x in one[:3]:
+        room = torch.empty(x.numel() + 1, dtype=x.dtype, device="cuda")
+        odd.append(room[1:].view(x.shape).copy_(x))
+    a, b = S.clone(), S.clone()
+    assert torch.equal(vla.gated_delta_decode_step(*one, a), vla.gated_delta_decode_step(*odd, *one[3:], b)) and torch.equal(a, b)
+
+
+def test_a_scale_of_zero_is_refused():
+    q, k, v, g, beta, S0 = make(1, 1, 1, 3, 16, 16, "f32", seed=23)
+    with pytest.raises(ValueError, match="scale"):
+        vla.gated_delta_forward(q, k, v, g, beta, S0, scale=0.0)
+    with pytest.raises(ValueError, match="scale"):
+        vla.gated_delta_decode_step(*(x[:, :, 0] for x in (q, k, v, g, beta)), S0, scale=0)
