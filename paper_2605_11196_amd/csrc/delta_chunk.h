@@ -9,7 +9,8 @@
 // few heads see: the substitution (700 cycles) and the solution, a chain of some ten dependent products and splits (3000 cycles).
 //
 // MAP: the affine map of a segment instead of its outputs, S_end = S_start X + Y: Y from d_v columns that start from zero, X from d_k
-// columns without values that start from the identity.
+// columns without values that start from the identity.  The first segment needs no map: where that shortens the way (first_done), a
+// workgroup beside the maps' forms its outputs and its end.
 #pragma once
 
 #include "delta_block.h"
@@ -22,12 +23,14 @@ struct Shape {
   static constexpr int COLS = DV + (MAP ? DK : 0);
   static constexpr int WAVES = COLS / 16;
   static constexpr int THREADS = 64 * WAVES;
+  // waves of a SIMD where as many workgroups share a compute unit as four waves a SIMD allow
+  static constexpr int HELD = MAP ? (16 / WAVES * WAVES + 3) / 4 : 4;
   static constexpr int DKP = DK < 32 ? 32 : DK;               // key columns in pairs of tiles
   static constexpr int KT = DKP / 16;
 };
 
 template <typename IO, int DK, int DV, bool MAP>
-__global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_kernel(DeltaArgs a) {
+__device__ __forceinline__ void chunk_segment(const DeltaArgs& a, int head, int seg) {
   using Sh = Shape<DK, DV, MAP>;
   using O = Ops<IO>;
   constexpr int KT = Sh::KT, WAVES = Sh::WAVES, THREADS = Sh::THREADS;
@@ -44,7 +47,6 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   int c = lane % 16, g = lane / 16;
-  const int head = blockIdx.x / a.n_seg, seg = blockIdx.x % a.n_seg;
   const int b = head / a.H_v, h = head % a.H_v, hk = h / (a.H_v / a.H_k);
   const int len = __builtin_amdgcn_readfirstlane(a.lengths ? max(0, min(a.lengths[b], a.T)) : a.T);
   const int first = seg * a.seg_tokens, last = min(a.T, first + a.seg_tokens), end = min(len, last);
@@ -55,21 +57,22 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
   const long long q_step = a.qs.t * sizeof(IO), k_step = a.ks.t * sizeof(IO), v_step = a.vs.t * sizeof(IO), o_step = a.os.t * sizeof(IO);
   const float* gp = a.g + b * a.gs.b + h * a.gs.h;
   const float* bp = a.beta + b * a.bs.b + h * a.bs.h;
+  const float scale = a.scale;
   const typename O::One one = O::one(c, g);
-  const int col = wave * 16 + c;            // column of this lane
+  const auto col = [&] { return wave * 16 + c; };      // column of this lane
   const f4 zero = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
   // ---- the state: tile kt holds key columns 32 (kt / 2) + 8 g + 4 (kt % 2) + r
   f4 S[KT];
-  const float* S0 = a.S0 ? a.S0 + (static_cast<size_t>(head) * (a.seg_states ? a.n_seg : 1) + (a.seg_states ? seg : 0)) * DV * DK : nullptr;
+  const float* S0 = !MAP && a.S0 ? a.S0 + (static_cast<size_t>(head) * (a.seg_states ? a.n_seg : 1) + (a.seg_states ? seg : 0)) * DV * DK : nullptr;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
     S[kt] = zero;
-    if ((DK == Sh::DKP || dk < DK) && (!MAP || col < DV) && S0 != nullptr) S[kt] = *reinterpret_cast<const f4*>(S0 + static_cast<size_t>(col) * DK + dk);
-    if (MAP && col >= DV) {
+    if ((DK == Sh::DKP || dk < DK) && S0 != nullptr) S[kt] = *reinterpret_cast<const f4*>(S0 + static_cast<uint32_t>(col() * DK + dk));
+    if (MAP && col() >= DV) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) S[kt][r] = col - DV == dk + r ? 1.0f : 0.0f;
+      for (int r = 0; r < 4; ++r) S[kt][r] = col() - DV == dk + r ? 1.0f : 0.0f;
     }
   }
   if constexpr (Sh::DKP > DK) {             // columns that no row fills
@@ -114,7 +117,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) {
         const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-        if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col) * DK + dk) = S[kt];
+        if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<uint32_t>(col() * DK + dk)) = S[kt];
       }
     }
     const int stop = min(end, (t0 / kKeep + 1) * kKeep);
@@ -130,7 +133,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
       // The chains of dependent steps go before the products with the state, which keep the matrix unit busy by themselves: the waves of
       // the other workgroup of the compute unit take turns better (512 heads: 1.762 -> 1.718 ms).
       __builtin_amdgcn_s_setprio(2);
-      token_matrices<IO, RK, KT / 2, WAVES, false, !MAP>(sK, sQ, gt, inverse, below, att, scratch, a.scale, wave, c, g);
+      token_matrices<IO, RK, KT / 2, WAVES, false, !MAP>(sK, sQ, gt, inverse, below, att, scratch, scale, wave, c, g);
       __builtin_amdgcn_s_setprio(0);
 
       // ---- P = K S^T, Q S^T
@@ -177,7 +180,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
       if (!MAP && a.rows != nullptr) {
         const __amdgpu_buffer_rsrc_t out = rows_buffer(a.rows + (static_cast<size_t>(head) * a.T + t0) * DV, DV * 4, last - t0, DV * 4);
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) store_column(out, ((16 * i + 4 * g) * DV + col) * 4, DV * 4, R[i], static_cast<float*>(nullptr));
+        for (int i = 0; i < kTiles; ++i) store_column(out, ((16 * i + 4 * g) * DV + col()) * 4, DV * 4, R[i], static_cast<float*>(nullptr));
       }
       const typename O::B w = O::pair(R[0] * w0, R[1] * w1, one);
       if constexpr (!MAP) {
@@ -185,10 +188,10 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
         const __amdgpu_buffer_rsrc_t out = rows_buffer(o + t0 * o_step, o_step, last - t0, DV * static_cast<int>(sizeof(IO)));
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
-          f4 x = gamma[i] * a.scale * QS[i];
+          f4 x = gamma[i] * scale * QS[i];
 #pragma unroll
           for (int j = 0; j <= i; ++j) x = O::mul_tok_out(at[i + j], rb[j], x);
-          store_column(out, (16 * i + 4 * g) * static_cast<int>(o_step) + col * static_cast<int>(sizeof(IO)), static_cast<int>(o_step), x,
+          store_column(out, (16 * i + 4 * g) * static_cast<int>(o_step) + col() * static_cast<int>(sizeof(IO)), static_cast<int>(o_step), x,
                        static_cast<IO*>(nullptr));
         }
       }
@@ -211,12 +214,30 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_chunk_
   }
   float* out = nullptr;
   if (MAP) out = a.seg_map + (static_cast<size_t>(head) * a.n_seg + seg) * Sh::COLS * DK;
+  else if (a.seg_S != nullptr) out = a.seg_S + (static_cast<size_t>(head) * a.n_seg + 1) * DV * DK;
   else if (a.S_T != nullptr && seg == a.n_seg - 1) out = a.S_T + static_cast<size_t>(head) * DV * DK;
   if (out == nullptr) return;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-    if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col) * DK + dk) = S[kt];
+    if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<uint32_t>(col() * DK + dk)) = S[kt];
+  }
+}
+
+template <typename IO, int DK, int DV, bool MAP>
+__global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), (Shape<DK, DV, MAP>::HELD)) delta_chunk_kernel(DeltaArgs a) {
+  if constexpr (MAP) {      // of all segments but the last one on the way
+    const int n = a.n_seg - 1, head = blockIdx.x / n, at = blockIdx.x % n, seg = at;
+    if constexpr (delta_first_with_maps(DV)) {
+      if (at == 0 && a.first_done) {
+        if (__builtin_amdgcn_readfirstlane(threadIdx.x) < Shape<DK, DV, false>::THREADS) chunk_segment<IO, DK, DV, false>(a, head, seg);
+        return;
+      }
+    }
+    chunk_segment<IO, DK, DV, true>(a, head, seg);
+  } else {
+    const int n = a.n_seg - (a.first_done ? 1 : 0), head = blockIdx.x / n, at = blockIdx.x % n;
+    chunk_segment<IO, DK, DV, false>(a, head, at + a.n_seg - n);
   }
 }
 
@@ -226,7 +247,7 @@ hipError_t launch_chunk(const DeltaArgs& a, int io_dtype, hipStream_t stream) {
   void* params[] = {&args};
   const void* fn = io_dtype == 1 ? reinterpret_cast<const void*>(&delta_chunk_kernel<uint16_t, DK, DV, MAP>)
                                  : reinterpret_cast<const void*>(&delta_chunk_kernel<float, DK, DV, MAP>);
-  return hipLaunchKernel(fn, dim3(a.B * a.H_v * a.n_seg), dim3(Shape<DK, DV, MAP>::THREADS), params, 0, stream);
+  return hipLaunchKernel(fn, dim3(a.B * a.H_v * (a.n_seg - (MAP || a.first_done ? 1 : 0))), dim3(Shape<DK, DV, MAP>::THREADS), params, 0, stream);
 }
 
 template <int DK>

@@ -15,16 +15,19 @@ namespace vla {
 namespace {
 
 template <int DK>
-__global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, float* seg_S, int d_v, int backward) {
+__global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, int d_v, int backward) {
   constexpr int KT = DK / 16;
   __shared__ f4 state[2][KT][64];
   const int tiles = d_v / 16, head = blockIdx.x / tiles, row = 16 * (blockIdx.x % tiles);
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
   const size_t map = static_cast<size_t>(d_v + DK) * DK, one = static_cast<size_t>(d_v) * DK;
   const float* maps = a.seg_map + static_cast<size_t>(head) * a.n_seg * map;
-  float* out = seg_S + static_cast<size_t>(head) * a.n_seg * one + static_cast<size_t>(row + c) * DK + 16 * wave + 4 * g;
+  float* out = a.seg_S + static_cast<size_t>(head) * a.n_seg * one + static_cast<size_t>(row + c) * DK + 16 * wave + 4 * g;
+  const auto place = [&](int s) { return backward ? a.n_seg - 1 - s : s; };
+  const int first = a.first_done ? 1 : 0;     // the state of this one is given
   f4 own = f4{0.0f, 0.0f, 0.0f, 0.0f};
-  if (a.S0 != nullptr) own = *reinterpret_cast<const f4*>(a.S0 + head * one + static_cast<size_t>(row + c) * DK + 16 * wave + 4 * g);
+  if (first > 0) own = *reinterpret_cast<const f4*>(out + place(1) * one);
+  else if (a.S0 != nullptr) own = *reinterpret_cast<const f4*>(a.S0 + head * one + static_cast<size_t>(row + c) * DK + 16 * wave + 4 * g);
   float x[KT][4];
   f4 y;
   auto request = [&](int s) {
@@ -37,10 +40,9 @@ __global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, floa
       for (int r = 0; r < 4; ++r) x[kt][r] = X[(16 * kt + 4 * g + r) * DK];
     }
   };
-  const auto place = [&](int s) { return backward ? a.n_seg - 1 - s : s; };
-  if (a.n_seg > 1) request(place(0));
-  for (int s = 0; s + 1 < a.n_seg; ++s) {
-    *reinterpret_cast<f4*>(out + place(s) * one) = own;
+  if (first == 0) *reinterpret_cast<f4*>(out + place(0) * one) = own;
+  request(place(first));
+  for (int s = first; s + 1 < a.n_seg; ++s) {
     state[s & 1][wave][lane] = own;
     __syncthreads();
     f4 acc[2] = {y, f4{0.0f, 0.0f, 0.0f, 0.0f}};
@@ -58,26 +60,26 @@ __global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, floa
       for (int r = 0; r < 4; ++r) acc[r & 1] = mfma16(now[kt][r], b[r], acc[r & 1]);
     }
     own = acc[0] + acc[1];
+    *reinterpret_cast<f4*>(out + place(s + 1) * one) = own;
   }
-  *reinterpret_cast<f4*>(out + place(a.n_seg - 1) * one) = own;
 }
 
 template <int DK>
-hipError_t launch(const DeltaArgs& a, float* seg_S, int d_v, int backward, hipStream_t stream) {
+hipError_t launch(const DeltaArgs& a, int d_v, int backward, hipStream_t stream) {
   DeltaArgs args = a;
-  void* params[] = {&args, &seg_S, &d_v, &backward};
+  void* params[] = {&args, &d_v, &backward};
   return hipLaunchKernel(reinterpret_cast<const void*>(&delta_combine_kernel<DK>), dim3(a.B * a.H_v * (d_v / 16)), dim3(4 * DK), params, 0, stream);
 }
 
 }  // namespace
 
-hipError_t launch_delta_combine(const DeltaArgs& a, float* seg_S, int d_k, int d_v, bool backward, hipStream_t stream) {
+hipError_t launch_delta_combine(const DeltaArgs& a, int d_k, int d_v, bool backward, hipStream_t stream) {
   switch (d_k) {
-    case 16: return launch<16>(a, seg_S, d_v, backward, stream);
-    case 32: return launch<32>(a, seg_S, d_v, backward, stream);
-    case 64: return launch<64>(a, seg_S, d_v, backward, stream);
-    case 96: return launch<96>(a, seg_S, d_v, backward, stream);
-    case 128: return launch<128>(a, seg_S, d_v, backward, stream);
+    case 16: return launch<16>(a, d_v, backward, stream);
+    case 32: return launch<32>(a, d_v, backward, stream);
+    case 64: return launch<64>(a, d_v, backward, stream);
+    case 96: return launch<96>(a, d_v, backward, stream);
+    case 128: return launch<128>(a, d_v, backward, stream);
     default: return hipErrorInvalidValue;
   }
 }

@@ -17,7 +17,7 @@ namespace vla {
 namespace delta {
 
 template <typename IO, int DK, int DV, bool MAP>
-__global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_reverse_kernel(DeltaArgs a) {
+__device__ __forceinline__ void reverse_segment(const DeltaArgs& a, int head, int seg) {
   using Sh = Shape<DK, DV, MAP>;
   using O = Ops<IO>;
   constexpr int KT = Sh::KT, WAVES = Sh::WAVES, THREADS = Sh::THREADS;
@@ -33,7 +33,6 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   int c = lane % 16, g = lane / 16;
-  const int head = blockIdx.x / a.n_seg, seg = blockIdx.x % a.n_seg;
   const int b = head / a.H_v, h = head % a.H_v, hk = h / (a.H_v / a.H_k);
   const int len = __builtin_amdgcn_readfirstlane(a.lengths ? max(0, min(a.lengths[b], a.T)) : a.T);
   const int first = seg * a.seg_tokens, last = min(a.T, first + a.seg_tokens), end = min(len, last);
@@ -44,21 +43,22 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
   const long long q_step = a.qs.t * sizeof(IO), k_step = a.ks.t * sizeof(IO), o_step = a.os.t * sizeof(IO), dv_step = a.dvs.t * sizeof(IO);
   const float* gp = a.g + b * a.gs.b + h * a.gs.h;
   const float* bp = a.beta + b * a.bs.b + h * a.bs.h;
+  const float scale = a.scale;
   const typename O::One one = O::one(c, g);
-  const int col = wave * 16 + c;            // column of this lane
+  const auto col = [&] { return wave * 16 + c; };      // column of this lane
   const f4 zero = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
   // ---- the state: tile kt holds key columns 32 (kt / 2) + 8 g + 4 (kt % 2) + r
   f4 S[KT];
-  const float* S0 = a.S0 ? a.S0 + (static_cast<size_t>(head) * (a.seg_states ? a.n_seg : 1) + (a.seg_states ? seg : 0)) * DV * DK : nullptr;
+  const float* S0 = !MAP && a.S0 ? a.S0 + (static_cast<size_t>(head) * (a.seg_states ? a.n_seg : 1) + (a.seg_states ? seg : 0)) * DV * DK : nullptr;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
     S[kt] = zero;
-    if ((DK == Sh::DKP || dk < DK) && (!MAP || col < DV) && S0 != nullptr) S[kt] = *reinterpret_cast<const f4*>(S0 + static_cast<size_t>(col) * DK + dk);
-    if (MAP && col >= DV) {
+    if ((DK == Sh::DKP || dk < DK) && S0 != nullptr) S[kt] = *reinterpret_cast<const f4*>(S0 + static_cast<uint32_t>(col() * DK + dk));
+    if (MAP && col() >= DV) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) S[kt][r] = col - DV == dk + r ? 1.0f : 0.0f;
+      for (int r = 0; r < 4; ++r) S[kt][r] = col() - DV == dk + r ? 1.0f : 0.0f;
     }
   }
   if constexpr (Sh::DKP > DK) {             // columns that no row fills
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) {
         const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-        if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col) * DK + dk) = S[kt];
+        if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<uint32_t>(col() * DK + dk)) = S[kt];
       }
     }
     for (int inner = min(left, t0 % kKeep / kTok + 1); inner > 0; --inner, --left, t0 -= kTok) {
@@ -117,7 +117,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
       turn ^= 1;
       __syncthreads();
       __builtin_amdgcn_s_setprio(2);   // as in the forward kernel
-      token_matrices<IO, RK, KT / 2, WAVES, true, true>(sK, sQ, gt, inverse, below, att, scratch, a.scale, wave, c, g);
+      token_matrices<IO, RK, KT / 2, WAVES, true, true>(sK, sQ, gt, inverse, below, att, scratch, scale, wave, c, g);
       __builtin_amdgcn_s_setprio(0);
 
       // ---- P = K dS^T
@@ -169,8 +169,8 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
           const int t = kTok - 1 - (16 * i + 4 * g);
-          store_column(rows, (t * DV + col) * 4, -DV * 4, W[i], static_cast<float*>(nullptr));
-          store_column(out, t * static_cast<int>(dv_step) + col * static_cast<int>(sizeof(IO)), -static_cast<int>(dv_step), W[i] * gate4(gt.beta, i),
+          store_column(rows, (t * DV + col()) * 4, -DV * 4, W[i], static_cast<float*>(nullptr));
+          store_column(out, t * static_cast<int>(dv_step) + col() * static_cast<int>(sizeof(IO)), -static_cast<int>(dv_step), W[i] * gate4(gt.beta, i),
                        static_cast<IO*>(nullptr));
         }
       }
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
       for (int i = 0; i < kTiles; ++i) {
         const f4 gamma = gate4(gt.gamma, i);
         W[i] *= -gamma * gate4(gt.beta, i);
-        e[i] = O::value(d[i]) * (gamma * a.scale);
+        e[i] = O::value(d[i]) * (gamma * scale);
       }
       const typename O::B wp = O::pair(W[0], W[1], one), ep = O::pair(e[0], e[1], one);
 #pragma unroll
@@ -208,12 +208,30 @@ __global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), 4) delta_revers
   }
   float* out = nullptr;
   if (MAP) out = a.seg_map + (static_cast<size_t>(head) * a.n_seg + seg) * Sh::COLS * DK;
+  else if (a.seg_S != nullptr) out = a.seg_S + (static_cast<size_t>(head) * a.n_seg + a.n_seg - 2) * DV * DK;
   else if (a.S_T != nullptr && seg == 0) out = a.S_T + static_cast<size_t>(head) * DV * DK;
   if (out == nullptr) return;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
-    if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<size_t>(col) * DK + dk) = S[kt];
+    if (DK == Sh::DKP || dk < DK) *reinterpret_cast<f4*>(out + static_cast<uint32_t>(col() * DK + dk)) = S[kt];
+  }
+}
+
+template <typename IO, int DK, int DV, bool MAP>
+__global__ void __launch_bounds__((Shape<DK, DV, MAP>::THREADS), (Shape<DK, DV, MAP>::HELD)) delta_reverse_kernel(DeltaArgs a) {
+  if constexpr (MAP) {      // of all segments but the last one on the way
+    const int n = a.n_seg - 1, head = blockIdx.x / n, at = blockIdx.x % n, seg = a.n_seg - 1 - at;
+    if constexpr (delta_first_with_maps(DV)) {
+      if (at == 0 && a.first_done) {
+        if (__builtin_amdgcn_readfirstlane(threadIdx.x) < Shape<DK, DV, false>::THREADS) reverse_segment<IO, DK, DV, false>(a, head, seg);
+        return;
+      }
+    }
+    reverse_segment<IO, DK, DV, true>(a, head, seg);
+  } else {
+    const int n = a.n_seg - (a.first_done ? 1 : 0), head = blockIdx.x / n, at = blockIdx.x % n;
+    reverse_segment<IO, DK, DV, false>(a, head, at);
   }
 }
 
@@ -223,7 +241,7 @@ hipError_t launch_reverse(const DeltaArgs& a, int io_dtype, hipStream_t stream) 
   void* params[] = {&args};
   const void* fn = io_dtype == 1 ? reinterpret_cast<const void*>(&delta_reverse_kernel<uint16_t, DK, DV, MAP>)
                                  : reinterpret_cast<const void*>(&delta_reverse_kernel<float, DK, DV, MAP>);
-  return hipLaunchKernel(fn, dim3(a.B * a.H_v * a.n_seg), dim3(Shape<DK, DV, MAP>::THREADS), params, 0, stream);
+  return hipLaunchKernel(fn, dim3(a.B * a.H_v * (a.n_seg - (MAP || a.first_done ? 1 : 0))), dim3(Shape<DK, DV, MAP>::THREADS), params, 0, stream);
 }
 
 template <int DK>

@@ -106,25 +106,35 @@ bool gate_rows(const vla_strides& s, long long H, long long T, vla::Rows* out) {
 }
 
 // Time segments of a sequence.  Few heads leave most of the card idle; in segments the sequence goes through twice (maps, then outputs:
-// 2.5 times the work).  The maps' workgroups of (d_v + d_k) / 16 waves decide how many segments the card holds at once; with small heads
-// twice as many still gain.  Forward, one segment against the rule's (us, bf16 but where said): 64 heads of 128, 4096 tokens, 4: 467, 295
-// (2: 519, 8: 304); 128 heads, 2: 476, 550 (the rule: none); 16 heads of 128, 32768 tokens, 16: 3770, 559; 128 heads of 64, 4096 tokens, 8:
-// 381, 226; 256 heads, 4: 387, 420 (none); 39 heads of 128 x 64, float32, 1537 tokens, 6: 352, 175; 8 heads of 64, 512 tokens, 4: 52, 36;
-// 256 tokens, 2: 28, 33 (none).
+// 2.5 times the work).  `held`: the maps' workgroups of (d_v + d_k) / 16 waves that the card holds at once for each head.
+// Where that is 2 to 16 the first segment goes with the maps of the others (first), which makes their number held + 1: with more the
+// segments get hardly shorter, and one of them takes longer than a map.  Otherwise as many as the card holds, with small heads twice as
+// many still gain.  Forward, microseconds, bf16 but where said:
+//   first: 64 heads of 128, 4096 tokens: 1 segment 475, 5 248 (all maps, 4: 293); 128 heads, 3: 382 (1: 479); 96 heads, 3: 367 (1: 480); 16 heads,
+//   32768 tokens, 17: 540 (16: 561); 128 heads of 64, 4096 tokens, 5: 190 (8: 217); 256 heads, 3: 303 (1: 371); 39 heads of 128 x 64, float32,
+//   1537 tokens, 7: 145 (6: 171)
+//   else: 4 heads of 128, 32768 tokens, 64: 267 (first, 65: 275); 16 heads of 64, 4096 tokens, 32: 67 (33: 73); 8 heads, 512 tokens, 4: 34 (1: 50);
+//   256 tokens, 2: 32 (1: 27, the rule); 32 heads of 128 x 16, 16: 154 (197 with the first beside the maps)
 struct Segments {
   int n, tokens;
+  bool first;
   size_t map_bytes, bytes;   // of the maps, of both arrays
 };
 Segments delta_segments(long long heads, int T, int d_k, int d_v, int requested) {
-  Segments s{1, T, 0, 0};
+  Segments s{1, T, false, 0, 0};
   const int blocks = (T + 31) / 32;
+  const bool can = vla::delta_first_with_maps(d_v);
   long long n = requested;
   if (requested == 0) {
     const int waves = (d_v + d_k) / 16;
-    const long long slots = 256 * (waves < 16 ? 16 / waves : 1);
-    n = (waves <= 8 ? 2 : 1) * slots / heads;
-    if (n > blocks / 4) n = blocks / 4;
-    if (blocks < 16 || n < (heads * n <= slots ? 3 : 6)) n = 1;
+    const long long slots = 256 * (waves < 16 ? 16 / waves : 1), held = slots / heads;
+    if (can && held >= 2 && held <= 16 && held + 1 <= blocks / 4) {
+      n = held + 1;
+    } else {
+      n = (waves <= 8 ? 2 : 1) * held;
+      if (n > blocks / 4) n = blocks / 4;
+      if (blocks < 16 || n < (heads * n <= slots ? 3 : 6)) n = 1;
+    }
   }
   if (n > blocks) n = blocks;
   if (n > 256) n = 256;
@@ -133,6 +143,7 @@ Segments delta_segments(long long heads, int T, int d_k, int d_v, int requested)
   const int each = static_cast<int>((blocks + n - 1) / n);
   s.n = (blocks + each - 1) / each;
   s.tokens = 32 * each;
+  s.first = can && s.n >= 3 && s.n <= 17;
   s.map_bytes = static_cast<size_t>(heads) * s.n * (d_v + d_k) * d_k * 4;
   s.bytes = s.map_bytes + static_cast<size_t>(heads) * s.n * d_v * d_k * 4;
   return s;
@@ -262,14 +273,14 @@ int vla_delta_forward(const void* q, const void* k, const void* v, const float* 
   if (seg.n == 1 || workspace == nullptr || workspace_bytes < seg.bytes) return launched(launch_blocks(a, d_k, d_v, io_dtype, false, s));
   a.n_seg = seg.n;
   a.seg_tokens = seg.tokens;
+  a.first_done = seg.first;
   a.seg_map = static_cast<float*>(workspace);
-  float* states = reinterpret_cast<float*>(static_cast<char*>(workspace) + seg.map_bytes);
-  vla::DeltaArgs maps = a;
-  maps.S0 = nullptr;
-  hipError_t err = launch_blocks(maps, d_k, d_v, io_dtype, true, s);
-  if (err == hipSuccess) err = vla::launch_delta_combine(a, states, d_k, d_v, false, s);
+  a.seg_S = reinterpret_cast<float*>(static_cast<char*>(workspace) + seg.map_bytes);
+  hipError_t err = launch_blocks(a, d_k, d_v, io_dtype, true, s);
+  if (err == hipSuccess) err = vla::launch_delta_combine(a, d_k, d_v, false, s);
   if (err != hipSuccess) return launched(err);
-  a.S0 = states;
+  a.S0 = a.seg_S;
+  a.seg_S = nullptr;
   a.seg_states = true;
   return launched(launch_blocks(a, d_k, d_v, io_dtype, false, s));
 }
@@ -334,16 +345,17 @@ int vla_delta_backward(const void* q, const void* k, const void* v, const float*
   a.n_kept = kept_states(T);
   a.n_seg = parts.seg.n;
   a.seg_tokens = parts.seg.tokens;
+  a.first_done = parts.seg.first;
   // W, dv, the state's gradient at the places that are kept
   vla::DeltaArgs chain = a;
   hipError_t err = hipSuccess;
   if (a.n_seg > 1) {
     chain.seg_map = at(parts.seg_map);
-    vla::DeltaArgs maps = chain;
-    maps.S0 = nullptr;
-    err = launch_reverse(maps, d_k, d_v, io_dtype, true, s);
-    if (err == hipSuccess) err = vla::launch_delta_combine(chain, at(parts.seg_S), d_k, d_v, true, s);
-    chain.S0 = at(parts.seg_S);
+    chain.seg_S = at(parts.seg_S);
+    err = launch_reverse(chain, d_k, d_v, io_dtype, true, s);
+    if (err == hipSuccess) err = vla::launch_delta_combine(chain, d_k, d_v, true, s);
+    chain.S0 = chain.seg_S;
+    chain.seg_S = nullptr;
     chain.seg_states = true;
   }
   if (err == hipSuccess) err = launch_reverse(chain, d_k, d_v, io_dtype, false, s);

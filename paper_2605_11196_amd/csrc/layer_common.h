@@ -66,11 +66,17 @@ struct DeltaArgs {
   float* dbeta;
   // time segments
   int n_seg, seg_tokens;
+  bool first_done;         // the first segment on the way goes with the maps
   bool seg_states;         // S0 holds a state for each segment: [B * H_v][n_seg][d_v][d_k]
   float* seg_map;          // [B * H_v][n_seg][d_v + d_k][d_k]: the segments' affine maps, Y then X
+  float* seg_S;            // with the maps: [B * H_v][n_seg][d_v][d_k], the states that the segments start from
 };
 // Token by token, the rows of the state on registers (delta_step.hip): single tokens and short sequences.
 hipError_t launch_delta_step(const DeltaArgs& a, int d_k, int d_v, int io_dtype, hipStream_t stream);
+
+// Whether the first of several time segments can go with the maps of the others.  With fewer waves for its outputs it would take longer than they
+// (32 heads of 128 x 16, 4096 tokens, 16 segments 154 -> 196 us).
+constexpr bool delta_first_with_maps(int d_v) { return d_v >= 64; }
 
 // In blocks of 32 tokens (delta_chunk.h); map: the affine maps of the segments instead of outputs.
 hipError_t launch_delta_chunk_16(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
@@ -80,8 +86,8 @@ hipError_t launch_delta_chunk_96(const DeltaArgs& a, int d_v, int io_dtype, bool
 hipError_t launch_delta_chunk_128(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
 
 // seg_S[h][0] = S0[h], seg_S[h][s + 1] = seg_S[h][s] X + Y of segment s (delta_combine.hip)
-// (backward: seg_S[h][n_seg - 1] = S0[h], seg_S[h][s - 1] = seg_S[h][s] X + Y of segment s)
-hipError_t launch_delta_combine(const DeltaArgs& a, float* seg_S, int d_k, int d_v, bool backward, hipStream_t stream);
+// (backward: seg_S[h][n_seg - 1] = S0[h], seg_S[h][s - 1] = seg_S[h][s] X + Y of segment s); with first_done from the second one on, which is there
+hipError_t launch_delta_combine(const DeltaArgs& a, int d_k, int d_v, bool backward, hipStream_t stream);
 
 // The chain of the state's gradient from the last block to the first (delta_reverse.h): S0 is the gradient of S_T and S_T that of S0.
 hipError_t launch_delta_reverse_16(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
