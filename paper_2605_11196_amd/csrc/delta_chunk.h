@@ -49,7 +49,7 @@ __device__ __forceinline__ void chunk_segment(const DeltaArgs& a, int head, int 
   int c = lane % 16, g = lane / 16;
   const int b = head / a.H_v, h = head % a.H_v, hk = h / (a.H_v / a.H_k);
   const int len = __builtin_amdgcn_readfirstlane(a.lengths ? max(0, min(a.lengths[b], a.T)) : a.T);
-  const int first = seg * a.seg_tokens, last = min(a.T, first + a.seg_tokens), end = min(len, last);
+  const int first = seg * a.seg_tokens, last = seg == a.n_seg - 1 ? a.T : first + a.seg_tokens, end = min(len, last);
   const char* q = reinterpret_cast<const char*>(static_cast<const IO*>(a.q) + b * a.qs.b + hk * a.qs.h);
   const char* k = reinterpret_cast<const char*>(static_cast<const IO*>(a.k) + b * a.ks.b + hk * a.ks.h);
   const char* v = reinterpret_cast<const char*>(static_cast<const IO*>(a.v) + b * a.vs.b + h * a.vs.h);
