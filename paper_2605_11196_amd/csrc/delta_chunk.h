@@ -64,7 +64,8 @@ __device__ __forceinline__ void chunk_segment(const DeltaArgs& a, int head, int 
 
   // ---- the state: tile kt holds key columns 32 (kt / 2) + 8 g + 4 (kt % 2) + r
   f4 S[KT];
-  const float* S0 = !MAP && a.S0 ? a.S0 + (static_cast<size_t>(head) * (a.seg_states ? a.n_seg : 1) + (a.seg_states ? seg : 0)) * DV * DK : nullptr;
+  const size_t slot = static_cast<size_t>(head) * a.n_slots + seg - (a.n_seg - a.n_slots);
+  const float* S0 = !MAP && a.S0 ? a.S0 + (a.seg_states ? slot : static_cast<size_t>(head)) * DV * DK : nullptr;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     const int dk = 32 * (kt / 2) + 8 * g + 4 * (kt % 2);
@@ -213,8 +214,8 @@ __device__ __forceinline__ void chunk_segment(const DeltaArgs& a, int head, int 
     }
   }
   float* out = nullptr;
-  if (MAP) out = a.seg_map + (static_cast<size_t>(head) * a.n_seg + seg) * Sh::COLS * DK;
-  else if (a.seg_S != nullptr) out = a.seg_S + (static_cast<size_t>(head) * a.n_seg + 1) * DV * DK;
+  if (MAP) out = a.seg_map + slot * Sh::COLS * DK;
+  else if (a.seg_S != nullptr) out = a.seg_S + (slot + 1) * DV * DK;
   else if (a.S_T != nullptr && seg == a.n_seg - 1) out = a.S_T + static_cast<size_t>(head) * DV * DK;
   if (out == nullptr) return;
 #pragma unroll

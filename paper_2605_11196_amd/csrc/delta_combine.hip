@@ -21,10 +21,10 @@ __global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, int 
   const int tiles = d_v / 16, head = blockIdx.x / tiles, row = 16 * (blockIdx.x % tiles);
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
   const size_t map = static_cast<size_t>(d_v + DK) * DK, one = static_cast<size_t>(d_v) * DK;
-  const float* maps = a.seg_map + static_cast<size_t>(head) * a.n_seg * map;
-  float* out = a.seg_S + static_cast<size_t>(head) * a.n_seg * one + static_cast<size_t>(row + c) * DK + 16 * wave + 4 * g;
-  const auto place = [&](int s) { return backward ? a.n_seg - 1 - s : s; };
+  const float* maps = a.seg_map + static_cast<size_t>(head) * a.n_slots * map;
+  float* out = a.seg_S + static_cast<size_t>(head) * a.n_slots * one + static_cast<size_t>(row + c) * DK + 16 * wave + 4 * g;
   const int first = a.first_done ? 1 : 0;     // the state of this one is given
+  const auto place = [&](int s) { return backward ? a.n_seg - 1 - s : s - (a.n_seg - a.n_slots); };
   f4 own = f4{0.0f, 0.0f, 0.0f, 0.0f};
   if (first > 0) own = *reinterpret_cast<const f4*>(out + place(1) * one);
   else if (a.S0 != nullptr) own = *reinterpret_cast<const f4*>(a.S0 + head * one + static_cast<size_t>(row + c) * DK + 16 * wave + 4 * g);

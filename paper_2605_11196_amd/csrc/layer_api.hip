@@ -116,12 +116,12 @@ bool gate_rows(const vla_strides& s, long long H, long long T, vla::Rows* out) {
 //   else: 4 heads of 128, 32768 tokens, 64: 267 (first, 65: 275); 16 heads of 64, 4096 tokens, 32: 67 (33: 73); 8 heads, 512 tokens, 4: 34 (1: 50);
 //   256 tokens, 2: 32 (1: 27, the rule); 32 heads of 128 x 16, 16: 154 (197 with the first beside the maps)
 struct Segments {
-  int n, tokens;
+  int n, tokens, slots;
   bool first;
   size_t map_bytes, bytes;   // of the maps, of both arrays
 };
 Segments delta_segments(long long heads, int T, int d_k, int d_v, int requested) {
-  Segments s{1, T, false, 0, 0};
+  Segments s{1, T, 1, false, 0, 0};
   const int blocks = (T + 31) / 32;
   const bool can = vla::delta_first_with_maps(d_v);
   long long n = requested;
@@ -144,8 +144,9 @@ Segments delta_segments(long long heads, int T, int d_k, int d_v, int requested)
   s.n = (blocks + each - 1) / each;
   s.tokens = 32 * each;
   s.first = can && s.n >= 3 && s.n <= 17;
-  s.map_bytes = static_cast<size_t>(heads) * s.n * (d_v + d_k) * d_k * 4;
-  s.bytes = s.map_bytes + static_cast<size_t>(heads) * s.n * d_v * d_k * 4;
+  s.slots = s.n - (s.first ? 1 : 0);
+  s.map_bytes = static_cast<size_t>(heads) * s.slots * (d_v + d_k) * d_k * 4;
+  s.bytes = s.map_bytes + static_cast<size_t>(heads) * s.slots * d_v * d_k * 4;
   return s;
 }
 
@@ -274,6 +275,7 @@ int vla_delta_forward(const void* q, const void* k, const void* v, const float* 
   a.n_seg = seg.n;
   a.seg_tokens = seg.tokens;
   a.first_done = seg.first;
+  a.n_slots = seg.slots;
   a.seg_map = static_cast<float*>(workspace);
   a.seg_S = reinterpret_cast<float*>(static_cast<char*>(workspace) + seg.map_bytes);
   hipError_t err = launch_blocks(a, d_k, d_v, io_dtype, true, s);
@@ -346,6 +348,7 @@ int vla_delta_backward(const void* q, const void* k, const void* v, const float*
   a.n_seg = parts.seg.n;
   a.seg_tokens = parts.seg.tokens;
   a.first_done = parts.seg.first;
+  a.n_slots = parts.seg.slots;
   // W, dv, the state's gradient at the places that are kept
   vla::DeltaArgs chain = a;
   hipError_t err = hipSuccess;

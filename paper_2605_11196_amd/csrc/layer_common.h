@@ -67,9 +67,10 @@ struct DeltaArgs {
   // time segments
   int n_seg, seg_tokens;
   bool first_done;         // the first segment on the way goes with the maps
-  bool seg_states;         // S0 holds a state for each segment: [B * H_v][n_seg][d_v][d_k]
-  float* seg_map;          // [B * H_v][n_seg][d_v + d_k][d_k]: the segments' affine maps, Y then X
-  float* seg_S;            // with the maps: [B * H_v][n_seg][d_v][d_k], the states that the segments start from
+  bool seg_states;         // S0 holds a state for each segment: [B * H_v][n_slots][d_v][d_k]
+  int n_slots;             // places of the arrays for each head: one for each segment but a first one that goes with the maps
+  float* seg_map;          // [B * H_v][n_slots][d_v + d_k][d_k]: the segments' affine maps, Y then X
+  float* seg_S;            // with the maps: [B * H_v][n_slots][d_v][d_k], the states that the segments start from
 };
 // Token by token, the rows of the state on registers (delta_step.hip): single tokens and short sequences.
 hipError_t launch_delta_step(const DeltaArgs& a, int d_k, int d_v, int io_dtype, hipStream_t stream);
@@ -85,8 +86,8 @@ hipError_t launch_delta_chunk_64(const DeltaArgs& a, int d_v, int io_dtype, bool
 hipError_t launch_delta_chunk_96(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
 hipError_t launch_delta_chunk_128(const DeltaArgs& a, int d_v, int io_dtype, bool map, hipStream_t stream);
 
-// seg_S[h][0] = S0[h], seg_S[h][s + 1] = seg_S[h][s] X + Y of segment s (delta_combine.hip)
-// (backward: seg_S[h][n_seg - 1] = S0[h], seg_S[h][s - 1] = seg_S[h][s] X + Y of segment s); with first_done from the second one on, which is there
+// The states from segment to segment, S <- S X + Y, from S0 on, or with first_done from that of the second segment on, which is there
+// (delta_combine.hip; backward: from the last segment on).
 hipError_t launch_delta_combine(const DeltaArgs& a, int d_k, int d_v, bool backward, hipStream_t stream);
 
 // The chain of the state's gradient from the last block to the first (delta_reverse.h): S0 is the gradient of S_T and S_T that of S0.
