@@ -4,7 +4,7 @@ import functools
 
 from . import binding
 from .binding import VlaDeltaOpts, VlaError, VlaStrides
-from .qk_norm import _io, _laid_out, _like, _p, _steps, _strides
+from .qk_norm import _io, _keep_plan, _kind, _laid_out, _like, _p, _steps, _strides, _together
 
 
 def _gate(x):
@@ -46,14 +46,25 @@ def _scale(scale):
     return scale
 
 
-def _aligned(x):
-    """x in order from a 16-byte boundary on."""
-    x = x.contiguous()
-    return x.clone() if x.data_ptr() % 16 else x
+# Options of calls whose tensors go to the kernels as they are, by the shapes, layouts and types of these: a call like an earlier one is
+# neither checked nor laid out again (4 of 16 us).
+_plans = {}
 
 
-def _inputs(q, k, v, g, beta, scale, lengths, segments=0):
+def _key(q, k, v, g, beta, S0, lengths, scale, segments=0):
+    return (q.shape, q.stride(), q.dtype, q.device, k.shape, k.stride(), k.dtype, k.device, v.shape, v.stride(), v.dtype, v.device, g.shape,
+            g.stride(), g.dtype, g.device, beta.shape, beta.stride(), beta.dtype, beta.device, _kind(S0), _kind(lengths), scale, segments)
+
+
+def _inputs(key, q, k, v, g, beta, scale, lengths, segments=0):
     """The inputs as the kernels take them, kept until the call, and its options."""
+    given = q, k, v, g, beta, lengths
+    plan = _plans.get(key)
+    if plan is not None and not (q.data_ptr() | k.data_ptr() | v.data_ptr()) & 15:
+        op = VlaDeltaOpts.from_buffer_copy(plan)
+        if lengths is not None:
+            op.lengths = lengths.data_ptr()
+        return given, op
     op = VlaDeltaOpts(_scale(scale))
     op.segments = segments
     (q, op.q), (k, op.k), (v, op.v) = _laid_out(q), _laid_out(k), _laid_out(v)
@@ -64,8 +75,12 @@ def _inputs(q, k, v, g, beta, scale, lengths, segments=0):
         op.beta = beta_strides
     if lengths is not None:
         lengths = lengths.contiguous()
+    kept = q, k, v, g, beta, lengths
+    if plan is None:
+        _keep_plan(_plans, key, kept, given, op)
+    if lengths is not None:
         op.lengths = lengths.data_ptr()
-    return (q, k, v, g, beta, lengths), op
+    return kept, op
 
 
 @functools.lru_cache(maxsize=1024)
@@ -116,11 +131,14 @@ def gated_delta_forward(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, 
     """
     import torch
 
-    _check(torch, q, k, v, g, beta, S0, "S0", lengths, 1)
+    scale = None if scale is None else float(scale)
+    key = _key(q, k, v, g, beta, S0, lengths, scale, segments)
+    if key not in _plans:
+        _check(torch, q, k, v, g, beta, S0, "S0", lengths, 1)
     binding.load_library()
     handle, context, outside = binding._on_stream(torch, q.device, stream)
     with context:
-        kept, op = _inputs(q, k, v, g, beta, scale, lengths, segments)
+        kept, op = _inputs(key, q, k, v, g, beta, scale, lengths, segments)
         o, S_T, saved = _forward(torch, kept, op, S0, save_for_backward, handle, outside)
     return (o, S_T, saved) if save_for_backward else (o, S_T)
 
@@ -130,18 +148,27 @@ def gated_delta_decode_step(q, k, v, g, beta, S, *, scale=None, stream=None):
     place.  Returns o [B,H_v,d_v]."""
     import torch
 
-    _check(torch, q, k, v, g, beta, S, "S", None, 0)
-    io, (B, H_k, dk), H_v, dv, dev = _io(torch, q), q.shape, v.shape[1], v.shape[-1], q.device
-    lib = binding.load_library()
-    handle, context, outside = binding._on_stream(torch, dev, stream)
+    scale = None if scale is None else float(scale)
+    key = _key(q, k, v, g, beta, S, None, scale)
+    plan = _plans.get(key)
+    if plan is None:
+        _check(torch, q, k, v, g, beta, S, "S", None, 0)
+    handle, context, outside = binding._on_stream(torch, q.device, stream)
     with context:
-        q, k, v, g, beta = _aligned(q), _aligned(k), _aligned(v), g.contiguous(), beta.contiguous()
+        if plan is None or (q.data_ptr() | k.data_ptr() | v.data_ptr()) & 15:
+            given = q, k, v, g, beta
+            q, k, v, g, beta = kept = _together(q), _together(k), _together(v), g.contiguous(), beta.contiguous()
+            op = VlaDeltaOpts(_scale(scale))
+            if plan is None:
+                _keep_plan(_plans, key, kept, given, op)
+        else:
+            op = VlaDeltaOpts.from_buffer_copy(plan)
+        (B, H_k, dk), (_, H_v, dv) = q.shape, v.shape
         o = torch.empty_like(v)
         if outside is not None:
             o.record_stream(outside)
-        op = VlaDeltaOpts(_scale(scale))
-        rc = lib.vla_delta_decode_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), S.data_ptr(),
-                                       o.data_ptr(), B, H_k, H_v, dk, dv, io, ctypes.byref(op), handle)
+        rc = binding.load_library().vla_delta_decode_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), S.data_ptr(),
+                                                          o.data_ptr(), B, H_k, H_v, dk, dv, _io(torch, q), ctypes.byref(op), handle)
     if rc != 0:
         raise VlaError(rc, binding.status_string(rc), "vla_delta_decode_step")
     return o
@@ -180,11 +207,14 @@ def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, 
     and what it saved.  dg, dbeta and dS0 are float32."""
     import torch
 
-    _check(torch, q, k, v, g, beta, dS_T, "dS_T", lengths, 1)
+    scale = None if scale is None else float(scale)
+    key = _key(q, k, v, g, beta, dS_T, lengths, scale, segments)
+    if key not in _plans:
+        _check(torch, q, k, v, g, beta, dS_T, "dS_T", lengths, 1)
     if do.shape != v.shape or do.dtype != v.dtype or do.device != v.device:
         raise ValueError("do must match v in shape, dtype and device")
     with binding._on_stream(torch, q.device, stream)[1]:
-        kept, op = _inputs(q, k, v, g, beta, scale, lengths, segments)
+        kept, op = _inputs(key, q, k, v, g, beta, scale, lengths, segments)
     return _backward(torch, kept, op, saved, do, dS_T, stream)
 
 
@@ -198,10 +228,10 @@ def _autograd():
 
         class GatedDelta(torch.autograd.Function):
             @staticmethod
-            def forward(ctx, q, k, v, g, beta, S0, scale, lengths):
+            def forward(ctx, q, k, v, g, beta, S0, key, scale, lengths):
                 handle, context, outside = binding._on_stream(torch, q.device, None)
                 with context:
-                    kept, op = _inputs(q, k, v, g, beta, scale, lengths)
+                    kept, op = _inputs(key, q, k, v, g, beta, scale, lengths)
                     o, S_T, saved = _forward(torch, kept, op, S0, True, handle, outside)
                 ctx.save_for_backward(*kept, saved)      # the inputs as the kernels read them
                 ctx.op, ctx.has_state = op, S0 is not None
@@ -216,7 +246,7 @@ def _autograd():
                 dS_T = None if dS_T is None else dS_T.contiguous()
                 op = VlaDeltaOpts.from_buffer_copy(ctx.op)
                 grads = _backward(torch, kept, op, saved, do, dS_T, None)
-                return (*grads[:5], grads[5] if ctx.has_state else None, None, None)
+                return (*grads[:5], grads[5] if ctx.has_state else None, None, None, None)
 
         _function = GatedDelta
     return _function
@@ -230,6 +260,9 @@ def gated_delta(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, stream=N
                                     or S0 is not None and S0.requires_grad):
         if stream is not None:
             raise ValueError("with gradients the work goes to the current stream: leave stream at None")
-        _check(torch, q, k, v, g, beta, S0, "S0", lengths, 1)
-        return _autograd().apply(q, k, v, g, beta, S0, scale, lengths)
+        scale = None if scale is None else float(scale)
+        key = _key(q, k, v, g, beta, S0, lengths, scale)
+        if key not in _plans:
+            _check(torch, q, k, v, g, beta, S0, "S0", lengths, 1)
+        return _autograd().apply(q, k, v, g, beta, S0, key, scale, lengths)
     return gated_delta_forward(q, k, v, g, beta, S0, scale=scale, lengths=lengths, stream=stream)
