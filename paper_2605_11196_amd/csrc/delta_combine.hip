@@ -7,7 +7,8 @@
 // columns of the product on the FP32 matrix instruction, from the rows that the waves leave in LDS.  The product is transposed: a
 // result tile (columns of S along its rows) is the right operand of the next product as it stands.  X of the next segment is
 // requested before the present product.  Bound by the latency of a step, about 2 us at d_k = 128 (64 matrix
-// instructions on each SIMD, the exchange through LDS and a barrier): 16 heads of 128 x 128, 16 segments 34 us.
+// instructions on each SIMD, the exchange through LDS and a barrier): 16 heads of 128 x 128, 15 steps 32 us; 64 heads, 3 steps 17.5 us (25.6
+// with the workgroups of a head on different L2 caches).
 #include "layer_common.h"
 #include "vla_mfma_util.h"
 
@@ -18,7 +19,9 @@ template <int DK>
 __global__ void __launch_bounds__(4 * DK) delta_combine_kernel(DeltaArgs a, int d_v, int backward) {
   constexpr int KT = DK / 16;
   __shared__ f4 state[2][KT][64];
-  const int tiles = d_v / 16, head = blockIdx.x / tiles, row = 16 * (blockIdx.x % tiles);
+  // the workgroups of a head on one of the eight L2 caches, which take workgroups in turn: they all read X
+  const int tiles = d_v / 16, turns = a.B * a.H_v / 8 * 8 * tiles, at = blockIdx.x;
+  const int head = at < turns ? at / (8 * tiles) * 8 + at % 8 : at / tiles, row = 16 * (at < turns ? at / 8 % tiles : at % tiles);
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 16, g = lane / 16;
   const size_t map = static_cast<size_t>(d_v + DK) * DK, one = static_cast<size_t>(d_v) * DK;
   const float* maps = a.seg_map + static_cast<size_t>(head) * a.n_slots * map;
