@@ -6,7 +6,7 @@
 // and then everything is as in the forward kernel (delta_chunk.h): a wave has 16 columns of what has d_v columns.  W is kept in float32,
 // and dS at the end of every 256 tokens, for the kernel that forms the other gradients (delta_grad.h).
 //
-// Bound like the forward kernel: 64 heads of 128, 4096 tokens in four segments 175 us (and 200 us for their maps).
+// Bound like the forward kernel: 64 heads of 128, 4096 tokens in five segments 150 us, and 168 us for the maps.
 //
 // MAP: the affine map of a segment, dS_start = dS_end X + Y.
 #pragma once
