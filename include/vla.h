@@ -1,7 +1,7 @@
 /*
  * vla.h -- C ABI of the MI355X (gfx950) Variational Linear Attention forward library.
  *
- * One operation: the causal per-head VLA forward recurrence (paper Section 3.3,
+ * The operation it is named for: the causal per-head VLA forward recurrence (paper Section 3.3,
  * eq. (sm), eq. (s-update), numerator of eq. (output); Algorithm 1).  For every
  * (batch b, head h) independently, starting from S = S0[b,h], A = A0[b,h], for
  * t = 1..T:

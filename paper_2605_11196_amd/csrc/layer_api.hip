@@ -106,21 +106,26 @@ bool gate_rows(const vla_strides& s, long long H, long long T, vla::Rows* out) {
 }
 
 // Time segments of a sequence.  Few heads leave most of the card idle; in segments the sequence goes through twice (maps, then outputs:
-// 2.5 times the work).  `held`: the maps' workgroups of (d_v + d_k) / 16 waves that the card holds at once for each head.
-// Where that is 2 to 16 the first segment goes with the maps of the others (first), which makes their number held + 1: with more the
-// segments get hardly shorter, and one of them takes longer than a map.  Otherwise as many as the card holds, with small heads twice as
-// many still gain.  Forward, microseconds, bf16 but where said:
-//   first: 64 heads of 128, 4096 tokens: 1 segment 475, 5 248 (all maps, 4: 293); 128 heads, 3: 382 (1: 479); 96 heads, 3: 367 (1: 480); 16 heads,
-//   32768 tokens, 17: 540 (16: 561); 128 heads of 64, 4096 tokens, 5: 190 (8: 217); 256 heads, 3: 303 (1: 371); 39 heads of 128 x 64, float32,
-//   1537 tokens, 7: 145 (6: 171)
-//   else: 4 heads of 128, 32768 tokens, 64: 267 (first, 65: 275); 16 heads of 64, 4096 tokens, 32: 67 (33: 73); 8 heads, 512 tokens, 4: 34 (1: 50);
-//   256 tokens, 2: 32 (1: 27, the rule); 32 heads of 128 x 16, 16: 154 (197 with the first beside the maps)
+// 2.6 times the work of a block, one after the other).  `held`: the maps' workgroups of (d_v + d_k) / 16 waves that the card holds at
+// once for each head.  The first of 3 to 17 segments goes with the maps of the others (first), which allows held + 1 of them: with more they get hardly
+// shorter, and the first one takes longer than a map.  Where that is not done (d_v < 64) twice as many still gain with small heads.
+// The number of segments, of 1, 2, 3, 4, 6, 8 ... blocks or as many as the card holds, is the one of least time by a model that is fitted to measurements
+// of 1 to 33 segments for 4 to 256 heads of 16 to 128 columns and 192 to 4096 tokens (microseconds): a block by the rounds in which its waves
+// form the six matrices between tokens and by its products; a map by its waves; a step from one segment to the next d_k / 60; d_k / 8 for the
+// launches.  Its choices are up to 10 % behind the best one (128 heads of 64 x 128, float32, 512 tokens: 102, 93).
+// Forward, microseconds, bf16 but where said, 1 segment and the rule's:
+//   4 heads of 64: 256 tokens 27, 22 (8 segments); 1024 tokens 94, 34 (16).  The same in float32 41, 24 and 151, 41
+//   4 heads of 128: 256 tokens 36, 36 (none; 4: 38); 384 tokens 51, 43 (6); 1024 tokens 124, 61 (11); 32 heads, 1024 tokens 124, 68 (8)
+//   128 heads of 128: 768 tokens 95, 95 (none; 3: 100); 1536 tokens 184, 162 (3); 4096 tokens 479, 382 (3)
+//   64 heads of 128, 4096 tokens: 475, 248 (5; all maps, 4: 293); 16 heads, 32768 tokens, 17: 540 (16: 561); one head 266 (64; 32: 325, 128: 328)
+//   128 heads of 64, 4096 tokens: 370, 190 (5); 256 heads: 512 tokens 50, 50 (none; 3: 58); 4096 tokens 371, 303 (3)
+//   39 heads of 128 x 64, float32, 1537 tokens: 338, 140 (7; all maps, 6: 171)
 struct Segments {
   int n, tokens, slots;
   bool first;
   size_t map_bytes, bytes;   // of the maps, of both arrays
 };
-Segments delta_segments(long long heads, int T, int d_k, int d_v, int requested) {
+Segments delta_segments(long long heads, int T, int d_k, int d_v, int io_dtype, int requested) {
   Segments s{1, T, 1, false, 0, 0};
   const int blocks = (T + 31) / 32;
   const bool can = vla::delta_first_with_maps(d_v);
@@ -128,12 +133,32 @@ Segments delta_segments(long long heads, int T, int d_k, int d_v, int requested)
   if (requested == 0) {
     const int waves = (d_v + d_k) / 16;
     const long long slots = 256 * (waves < 16 ? 16 / waves : 1), held = slots / heads;
-    if (can && held >= 2 && held <= 16 && held + 1 <= blocks / 4) {
-      n = held + 1;
-    } else {
-      n = (waves <= 8 ? 2 : 1) * held;
-      if (n > blocks / 4) n = blocks / 4;
-      if (blocks < 16 || n < (heads * n <= slots ? 3 : 6)) n = 1;
+    const long long most = can ? (held <= 16 ? held + 1 : held) : (waves <= 8 ? 2 : 1) * held;
+    const bool f32 = io_dtype == VLA_F32;
+    const int rounds = (6 + d_v / 16 - 1) / (d_v / 16);       // of the matrices between tokens on d_v / 16 waves
+    const float block = f32 ? (0.6f + 0.002f * d_k) * rounds + (1.2f + 0.032f * d_k) * (d_v > 64 ? 1.6f : 1.0f)
+                            : 1.4f + 0.45f * rounds + 1.1e-4f * d_k * d_k + (d_v > 64 ? 1.4f - 0.011f * d_k : 0.0f);
+    const float both = block + 2.0f + (f32 ? 0.6f : 0.18f) * waves;
+    float least = 0.97f * (block * blocks + 7.0f);
+    n = 1;
+    const auto consider = [&](long long each) {      // blocks of a segment
+      const long long m = (blocks + each - 1) / each;
+      if (m < 2 || m > most || m > 256) return;
+      const long long maps = heads * (m - (can ? 1 : 0));
+      const float crowd = 2 * maps < slots || waves > 8 ? 1.0f : (1.0f + 0.8f / waves) * (f32 ? 1.25f : 1.0f);
+      const float time = both * each * crowd * (maps > slots ? 2.1f : 1.0f) + d_k / 60.0f * m + d_k / 8.0f +
+                         (2 * maps >= slots ? 4.0f : -3.0f);
+      if (time < least) {
+        least = time;
+        n = m;
+      }
+    };
+    if (held >= 2 && blocks >= (f32 ? 6 : 8)) {
+      for (long long each = 1; each < blocks; each *= 2) {
+        consider(each);
+        consider(each + (each + 1) / 2);
+      }
+      consider((blocks + most - 1) / most);
     }
   }
   if (n > blocks) n = blocks;
@@ -159,9 +184,9 @@ struct BackwardParts {
   Segments seg;
   size_t kept, rows, dk, dq, seg_map, seg_S, bytes;   // offsets
 };
-BackwardParts backward_parts(long long heads, int T, int d_k, int d_v, bool shared, int requested) {
+BackwardParts backward_parts(long long heads, int T, int d_k, int d_v, int io_dtype, bool shared, int requested) {
   BackwardParts p{};
-  p.seg = delta_segments(heads, T, d_k, d_v, requested);
+  p.seg = delta_segments(heads, T, d_k, d_v, io_dtype, requested);
   p.kept = 0;
   p.rows = p.kept + kept_bytes(heads, T, d_k, d_v);
   p.dk = p.rows + row_bytes(heads, T, d_v);
@@ -216,8 +241,8 @@ size_t vla_delta_workspace_bytes(int B, int H_k, int H_v, int T, int d_k, int d_
   const vla_delta_opts op = delta_opts(opts, d_k);
   if (check_delta(B, H_k, H_v, T, d_k, d_v, io_dtype, op) != VLA_OK) return 0;
   const long long heads = static_cast<long long>(B) * H_v;
-  if (!backward) return delta_segments(heads, T, d_k, d_v, op.segments).bytes;
-  return backward_parts(heads, T, d_k, d_v, H_v != H_k, op.segments).bytes;
+  if (!backward) return delta_segments(heads, T, d_k, d_v, io_dtype, op.segments).bytes;
+  return backward_parts(heads, T, d_k, d_v, io_dtype, H_v != H_k, op.segments).bytes;
 }
 
 size_t vla_delta_saved_bytes(int B, int H_v, int T, int d_k, int d_v, int io_dtype) {
@@ -270,7 +295,7 @@ int vla_delta_forward(const void* q, const void* k, const void* v, const float* 
     a.rows = reinterpret_cast<float*>(static_cast<char*>(op.saved) + kept_bytes(static_cast<long long>(B) * H_v, T, d_k, d_v));
   }
   if (T < 16 && op.saved == nullptr) return launched(vla::launch_delta_step(a, d_k, d_v, io_dtype, s));
-  Segments seg = delta_segments(static_cast<long long>(B) * H_v, T, d_k, d_v, op.segments);
+  Segments seg = delta_segments(static_cast<long long>(B) * H_v, T, d_k, d_v, io_dtype, op.segments);
   if (seg.n == 1 || workspace == nullptr || workspace_bytes < seg.bytes) return launched(launch_blocks(a, d_k, d_v, io_dtype, false, s));
   a.n_seg = seg.n;
   a.seg_tokens = seg.tokens;
@@ -322,7 +347,7 @@ int vla_delta_backward(const void* q, const void* k, const void* v, const float*
   }
   const long long heads = static_cast<long long>(B) * H_v;
   if (heads * kept_states(T) > 0x7fffffffLL) return VLA_ERR_UNSUPPORTED;   // workgroups
-  const BackwardParts parts = backward_parts(heads, T, d_k, d_v, H_v != H_k, op.segments);
+  const BackwardParts parts = backward_parts(heads, T, d_k, d_v, io_dtype, H_v != H_k, op.segments);
   const size_t nS = static_cast<size_t>(heads) * d_v * d_k * 4, nG = static_cast<size_t>(heads) * T * 4;
   const size_t saved = vla_delta_saved_bytes(B, H_v, T, d_k, d_v, io_dtype);
   const Range r[] = {{q, reach(a.qs, B, H_k, T, d_k, es), false}, {k, reach(a.ks, B, H_k, T, d_k, es), false},
