@@ -174,29 +174,28 @@ def gated_delta_decode_step(q, k, v, g, beta, S, *, scale=None, stream=None):
     return o
 
 
-def _backward(torch, kept, op, saved, do, dS_T, stream):
-    """The gradients, with kept and op of the forward pass (strides of o and of outputs are set here)."""
+def _backward(torch, kept, op, saved, do, dS_T, handle, outside):
+    """kept, op, handle, outside: as for _forward().  The gradients."""
     q, k, v, g, beta, _ = kept
     B, H_k, T, dk = q.shape
     H_v, dv, dev, io = v.shape[1], v.shape[3], q.device, _io(torch, q)
     lib = binding.load_library()
-    handle, context, outside = binding._on_stream(torch, dev, stream)
-    with context:
-        do, op.o = _laid_out(do)
-        dq, dk_, dv_ = _like(torch, q), _like(torch, k), _like(torch, v)
-        dg, dbeta = (torch.empty((B, H_v, T), dtype=torch.float32, device=dev) for _ in range(2))
-        dS0 = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
-        op.dq, op.dk, op.dv = _strides(dq), _strides(dk_), _strides(dv_)
-        op.saved, op.saved_bytes = saved.data_ptr(), saved.numel()
-        need = _workspace_bytes(B, H_k, H_v, T, dk, dv, io, op.segments, 1)
-        ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
-        outputs = (dq, dk_, dv_, dg, dbeta, dS0)
-        if outside is not None:
-            for t in outputs:
-                t.record_stream(outside)
-        rc = lib.vla_delta_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), do.data_ptr(), _p(dS_T), dq.data_ptr(),
-                                    dk_.data_ptr(), dv_.data_ptr(), dg.data_ptr(), dbeta.data_ptr(), dS0.data_ptr(), B, H_k, H_v, T, dk, dv, io,
-                                    ctypes.byref(op), _p(ws), need, handle)
+    do, op.o = _laid_out(do)
+    dq, dk_, dv_ = _like(torch, q), _like(torch, k), _like(torch, v)
+    dg, dbeta = (torch.empty((B, H_v, T), dtype=torch.float32, device=dev) for _ in range(2))
+    dS0 = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
+    op.dq, op.dk, op.dv = _strides(dq), _strides(dk_), _strides(dv_)
+    saved = _together(saved)
+    op.saved, op.saved_bytes = saved.data_ptr(), saved.numel()
+    need = _workspace_bytes(B, H_k, H_v, T, dk, dv, io, op.segments, 1)
+    ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
+    outputs = (dq, dk_, dv_, dg, dbeta, dS0)
+    if outside is not None:
+        for t in outputs:
+            t.record_stream(outside)
+    rc = lib.vla_delta_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), do.data_ptr(), _p(dS_T), dq.data_ptr(),
+                                dk_.data_ptr(), dv_.data_ptr(), dg.data_ptr(), dbeta.data_ptr(), dS0.data_ptr(), B, H_k, H_v, T, dk, dv, io,
+                                ctypes.byref(op), _p(ws), need, handle)
     if rc != 0:
         raise VlaError(rc, binding.status_string(rc), "vla_delta_backward")
     return outputs
@@ -213,9 +212,10 @@ def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, 
         _check(torch, q, k, v, g, beta, dS_T, "dS_T", lengths, 1)
     if do.shape != v.shape or do.dtype != v.dtype or do.device != v.device:
         raise ValueError("do must match v in shape, dtype and device")
-    with binding._on_stream(torch, q.device, stream)[1]:
+    handle, context, outside = binding._on_stream(torch, q.device, stream)
+    with context:
         kept, op = _inputs(key, q, k, v, g, beta, scale, lengths, segments)
-    return _backward(torch, kept, op, saved, do, dS_T, stream)
+        return _backward(torch, kept, op, saved, do, dS_T, handle, outside)
 
 
 _function = None
@@ -234,18 +234,18 @@ def _autograd():
                     kept, op = _inputs(key, q, k, v, g, beta, scale, lengths)
                     o, S_T, saved = _forward(torch, kept, op, S0, True, handle, outside)
                 ctx.save_for_backward(*kept, saved)      # the inputs as the kernels read them
-                ctx.op, ctx.has_state = op, S0 is not None
+                ctx.scale, ctx.has_state = scale, S0 is not None
                 ctx.set_materialize_grads(False)
                 return o, S_T
 
             @staticmethod
             @torch.autograd.function.once_differentiable
             def backward(ctx, do, dS_T):
-                *kept, saved = ctx.saved_tensors
-                do = torch.zeros_like(kept[2]) if do is None else do
+                # hooks (offload, checkpoints) may give other tensors than the saved ones: addresses and strides are those of these
+                q, k, v, g, beta, lengths, saved = ctx.saved_tensors
+                do = torch.zeros_like(v) if do is None else do
                 dS_T = None if dS_T is None else dS_T.contiguous()
-                op = VlaDeltaOpts.from_buffer_copy(ctx.op)
-                grads = _backward(torch, kept, op, saved, do, dS_T, None)
+                grads = gated_delta_backward(q, k, v, g, beta, saved, do, dS_T, scale=ctx.scale, lengths=lengths)
                 return (*grads[:5], grads[5] if ctx.has_state else None, None, None, None)
 
         _function = GatedDelta

@@ -1,0 +1,162 @@
+"""What the autograd functions of the operators around the recurrence hand to the library (CPU only: calls that would launch kernels are
+recorded, with their options as they are at the call).
+
+Saved tensors may come back as other ones: hooks that offload or pack them give copies with other strides at other addresses, and a
+checkpointed layer forms them again.  The library knows addresses and strides but no sizes, so the two have to be those of the tensors that the backward
+pass holds."""
+import contextlib
+import ctypes
+import importlib
+
+import pytest
+import torch
+from torch.utils.checkpoint import checkpoint
+
+import paper_2605_11196_amd as vla
+from paper_2605_11196_amd import binding
+from paper_2605_11196_amd.binding import VlaDeltaOpts, VlaNormOpts, VlaStrides
+
+gated_delta, qk_norm = (importlib.import_module("paper_2605_11196_amd." + n) for n in ("gated_delta", "qk_norm"))
+
+LAUNCHES = {"vla_delta_forward": (VlaDeltaOpts, 15), "vla_delta_decode_step": (VlaDeltaOpts, 13), "vla_delta_backward": (VlaDeltaOpts, 20),
+            "vla_qk_norm_rope": (VlaNormOpts, 14), "vla_qk_norm_rope_backward": (VlaNormOpts, 18)}   # options, their place among the arguments
+
+
+class Recorder:
+    """The library, with what it would launch as entries (name, arguments, options) of `calls`."""
+
+    def __init__(self):
+        self.lib, self.calls = binding.load_library(), []
+
+    def __getattr__(self, name):
+        if name not in LAUNCHES:
+            return getattr(self.lib, name)
+        kind, place = LAUNCHES[name]
+
+        def launch(*args):
+            self.calls.append((name, args, kind.from_buffer_copy(args[place]._obj)))
+            return 0
+
+        return launch
+
+    def last(self, name):
+        return next(c for c in reversed(self.calls) if c[0] == name)
+
+
+@pytest.fixture
+def recorder(monkeypatch):
+    r = Recorder()
+    monkeypatch.setattr(binding, "load_library", lambda: r)
+    monkeypatch.setattr(binding, "_on_stream", lambda torch, dev, stream: (0, contextlib.nullcontext(), None))
+    for module in (gated_delta, qk_norm):
+        monkeypatch.setattr(module, "_check", lambda *a: None)   # refuses tensors that are not on the GPU
+        monkeypatch.setattr(module, "_plans", {})
+    return r
+
+
+def dense(x):
+    return x.clone(memory_format=torch.contiguous_format)
+
+
+def turned(x):
+    """Tokens before heads, whatever the order was."""
+    return x.transpose(1, 2).clone(memory_format=torch.contiguous_format).transpose(1, 2) if x.dim() >= 3 else x.clone()
+
+
+def off_by_one(x):
+    """Not at a 16-byte boundary."""
+    room = torch.empty(x.numel() + 1, dtype=x.dtype)
+    return room[1:].view(x.shape).copy_(x)
+
+
+class Hooks:
+    """Saved tensors come back as copies, which stay here."""
+
+    def __init__(self, layout):
+        self.layout, self.copies = layout, []
+
+    def unpack(self, x):
+        self.copies.append(self.layout(x))
+        return self.copies[-1]
+
+    def __enter__(self):
+        self.context = torch.autograd.graph.saved_tensors_hooks(lambda x: x, self.unpack)
+        return self.context.__enter__()
+
+    def __exit__(self, *args):
+        return self.context.__exit__(*args)
+
+
+def read(address, strides, shape, dtype, contiguous):
+    """The tensor that the library would read."""
+    steps = (strides.b, strides.h, strides.t)[:len(shape[:3])]
+    if not any(steps):
+        steps = contiguous[:len(steps)]
+    reach = sum(s * (n - 1) for s, n in zip(steps, shape)) + (shape[3] if len(shape) > 3 else 1)
+    kind = {torch.float32: ctypes.c_float, torch.bfloat16: ctypes.c_int16, torch.int32: ctypes.c_int32}[dtype]
+    flat = torch.frombuffer((kind * reach).from_address(address), dtype=dtype)
+    return flat.as_strided(shape, (*steps, 1)[:len(shape)])
+
+
+def holds(address, strides, copies, want):
+    """Whether one of `copies` starts at the address, covers what the strides reach and reads as `want`."""
+    shape, contiguous = tuple(want.shape), want.contiguous().stride()
+    steps = (strides.b, strides.h, strides.t)
+    steps = steps if any(steps) else contiguous[:3]
+    reach = sum(s * (n - 1) for s, n in zip(steps, shape)) + (shape[3] if len(shape) > 3 else 1)
+    for x in copies:
+        end = x.untyped_storage().data_ptr() + x.untyped_storage().nbytes()
+        if x.data_ptr() == address and address + reach * want.element_size() <= end:
+            return torch.equal(read(address, strides, shape, want.dtype, contiguous), want)
+    return False
+
+
+def fused(B, T, H_k, H_v, d, seed=0):
+    """Leaves: rows of a projection and of its gates; q, k, v, g, beta as their slices, and S0."""
+    gen = torch.Generator().manual_seed(seed)
+    rows = torch.randn((B, T, (2 * H_k + H_v) * d), generator=gen).requires_grad_()
+    gates = torch.randn((B, T, 2 * H_v), generator=gen).requires_grad_()
+    q, k, v = rows.view(B, T, -1, d).transpose(1, 2).split((H_k, H_k, H_v), 1)
+    g, beta = gates.transpose(1, 2).split(H_v, 1)
+    return (rows, gates), (q, k, v, g, beta), torch.randn((B, H_v, d, d), generator=gen)
+
+
+@pytest.mark.parametrize("layout", [dense, turned, off_by_one])
+def test_the_delta_rules_gradients_read_the_unpacked_tensors(recorder, layout):
+    B, T, H_k, H_v, d = 3, 40, 2, 4, 32
+    leaves, inputs, S0 = fused(B, T, H_k, H_v, d)
+    lengths = torch.tensor([5, 40, 17], dtype=torch.int32)
+    for _ in range(2):      # the second time as a call like an earlier one
+        hooks = Hooks(layout)
+        with hooks:
+            o, S = vla.gated_delta(*inputs, S0.requires_grad_(), lengths=lengths)
+        (o.sum() + S.sum()).backward(inputs=(*leaves, S0))
+        name, args, op = recorder.calls[-1]
+        copies = hooks.copies
+        assert name == "vla_delta_backward" and len(copies) >= 7
+        own = {x.data_ptr() for x in copies}
+        for i, x in enumerate(inputs):
+            name = ("q", "k", "v", "g", "beta")[i]
+            if layout is off_by_one and i < 3:
+                assert args[i] not in own and args[i] % 16 == 0 and not any((getattr(op, name).b, getattr(op, name).h, getattr(op, name).t)), name
+            else:
+                assert holds(args[i], getattr(op, name), copies, x.detach()), name
+        assert holds(op.lengths, VlaStrides(), copies, lengths)
+        assert op.saved in own or layout is off_by_one
+        assert [args[i] for i in range(13, 19)] == [B, H_k, H_v, T, d, d]
+        del o, S
+
+
+def test_a_checkpointed_delta_rule_reads_the_lengths_that_are_formed_again(recorder):
+    leaves, inputs, _ = fused(2, 20, 1, 2, 16)
+    made = []
+
+    def layer(q, k, v, g, beta):
+        made.append(torch.tensor([7, 20], dtype=torch.int32))
+        return vla.gated_delta(q, k, v, g, beta, lengths=made[-1])[0]
+
+    o = checkpoint(layer, *inputs, use_reentrant=False)
+    first = recorder.last("vla_delta_forward")[2].lengths
+    o.sum().backward()
+    assert len(made) == 2 and first == made[0].data_ptr()
+    assert recorder.last("vla_delta_backward")[2].lengths == made[1].data_ptr()
