@@ -154,28 +154,26 @@ def _forward(torch, kept, op, handle, outside):
     return q_out, k_out
 
 
-def _backward(torch, kept, op, dq_out, dk_out, stream):
-    """The gradients (dq, dk, dq_weight, dk_weight), with kept and op of the forward pass."""
+def _backward(torch, kept, op, dq_out, dk_out, handle, outside):
+    """kept, op, handle, outside: as for _forward().  The gradients (dq, dk, dq_weight, dk_weight)."""
     q, k, q_weight, k_weight = kept[:4]
     B, H_q, T, d = q.shape
     dev = q.device
     lib = binding.load_library()
-    handle, context, outside = binding._on_stream(torch, dev, stream)
-    with context:
-        (dq_out, op.q_out), (dk_out, op.k_out) = _laid_out(dq_out), _laid_out(dk_out)
-        dq, dk = _like(torch, q), _like(torch, k)
-        op.dq, op.dk = _strides(dq), _strides(dk)
-        dwq = None if q_weight is None else torch.empty_like(q_weight)
-        dwk = None if k_weight is None else torch.empty_like(k_weight)
-        need = lib.vla_qk_norm_rope_workspace_bytes(d) if q_weight is not None or k_weight is not None else 0
-        ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
-        if outside is not None:
-            for t in (dq, dk, dwq, dwk):
-                if t is not None:
-                    t.record_stream(outside)
-        rc = lib.vla_qk_norm_rope_backward(
-            q.data_ptr(), k.data_ptr(), _p(q_weight), _p(k_weight), _p(kept[4]), _p(kept[5]), dq_out.data_ptr(), dk_out.data_ptr(),
-            dq.data_ptr(), dk.data_ptr(), _p(dwq), _p(dwk), B, T, H_q, k.shape[1], d, _io(torch, q), ctypes.byref(op), _p(ws), need, handle)
+    (dq_out, op.q_out), (dk_out, op.k_out) = _laid_out(dq_out), _laid_out(dk_out)
+    dq, dk = _like(torch, q), _like(torch, k)
+    op.dq, op.dk = _strides(dq), _strides(dk)
+    dwq = None if q_weight is None else torch.empty_like(q_weight)
+    dwk = None if k_weight is None else torch.empty_like(k_weight)
+    need = lib.vla_qk_norm_rope_workspace_bytes(d) if q_weight is not None or k_weight is not None else 0
+    ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
+    if outside is not None:
+        for t in (dq, dk, dwq, dwk):
+            if t is not None:
+                t.record_stream(outside)
+    rc = lib.vla_qk_norm_rope_backward(
+        q.data_ptr(), k.data_ptr(), _p(q_weight), _p(k_weight), _p(kept[4]), _p(kept[5]), dq_out.data_ptr(), dk_out.data_ptr(),
+        dq.data_ptr(), dk.data_ptr(), _p(dwq), _p(dwk), B, T, H_q, k.shape[1], d, _io(torch, q), ctypes.byref(op), _p(ws), need, handle)
     if rc != 0:
         raise VlaError(rc, binding.status_string(rc), "vla_qk_norm_rope_backward")
     return dq, dk, dwq, dwk
@@ -193,9 +191,10 @@ def qk_norm_rope_backward(q, k, q_weight, k_weight, cos, sin, dq_out, dk_out, *,
         _check(torch, q, k, q_weight, k_weight, cos, sin, positions, norm)
     if any(y.shape != x.shape or y.dtype != x.dtype or y.device != x.device for x, y in ((q, dq_out), (k, dk_out))):
         raise ValueError("dq_out and dk_out must match q and k in shape, dtype and device")
-    with binding._on_stream(torch, q.device, stream)[1]:
+    handle, context, outside = binding._on_stream(torch, q.device, stream)
+    with context:
         kept, op = _call(torch, key, q, k, q_weight, k_weight, cos, sin, positions, *how)
-    return _backward(torch, kept, op, dq_out, dk_out, stream)
+        return _backward(torch, kept, op, dq_out, dk_out, handle, outside)
 
 
 _function = None
@@ -213,18 +212,21 @@ def _autograd():
                 with context:
                     kept, op = _call(torch, key, q, k, q_weight, k_weight, cos, sin, positions, *how)
                     ctx.save_for_backward(*kept)     # the inputs as the kernels read them
-                    ctx.op = op
+                    ctx.how = how
                     ctx.set_materialize_grads(False)
                     return _forward(torch, kept, op, handle, outside)
 
             @staticmethod
             @torch.autograd.function.once_differentiable
             def backward(ctx, dq_out, dk_out):
-                kept = ctx.saved_tensors
-                dq_out = torch.zeros_like(kept[0]) if dq_out is None else dq_out
-                dk_out = torch.zeros_like(kept[1]) if dk_out is None else dk_out
-                op = VlaNormOpts.from_buffer_copy(ctx.op)
-                return (*_backward(torch, kept, op, dq_out, dk_out, None), None, None, None, None, None)
+                # hooks (offload, checkpoints) may give other tensors than the saved ones: addresses and strides are those of these
+                q, k, q_weight, k_weight, cos, sin, positions = ctx.saved_tensors
+                dq_out = torch.zeros_like(q) if dq_out is None else dq_out
+                dk_out = torch.zeros_like(k) if dk_out is None else dk_out
+                offset, eps, norm, interleaved = ctx.how
+                grads = qk_norm_rope_backward(q, k, q_weight, k_weight, cos, sin, dq_out, dk_out, positions=positions, offset=offset, eps=eps,
+                                              norm=norm, interleaved=interleaved)
+                return (*grads, None, None, None, None, None)
 
         _function = QkNormRope
     return _function

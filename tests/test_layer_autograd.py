@@ -160,3 +160,48 @@ def test_a_checkpointed_delta_rule_reads_the_lengths_that_are_formed_again(recor
     o.sum().backward()
     assert len(made) == 2 and first == made[0].data_ptr()
     assert recorder.last("vla_delta_backward")[2].lengths == made[1].data_ptr()
+
+
+@pytest.mark.parametrize("layout", [dense, turned, off_by_one])
+@pytest.mark.parametrize("rotated", [False, True])
+def test_the_norms_gradients_read_the_unpacked_tensors(recorder, layout, rotated):
+    B, T, H_q, H_k, d = 3, 11, 4, 2, 32
+    rows = torch.randn((B, T, (H_q + H_k) * d)).requires_grad_()
+    q, k = rows.view(B, T, -1, d).transpose(1, 2).split((H_q, H_k), 1)
+    weights = [torch.rand(d).requires_grad_() for _ in range(2)]
+    tables = [torch.rand(20, 8) for _ in range(2)] if rotated else [None, None]
+    positions = torch.randint(0, 20, (1, T), dtype=torch.int32).expand(B, T) if rotated else None
+    for _ in range(2):      # the second time as a call like an earlier one
+        hooks = Hooks(layout)
+        with hooks:
+            out = vla.qk_norm_rope(q, k, *weights, *tables, positions=positions, eps=1e-5, norm="l2", interleaved=True, offset=2)
+        (out[0].sum() + out[1].sum()).backward(inputs=(rows, *weights))
+        name, args, op = recorder.calls[-1]
+        assert name == "vla_qk_norm_rope_backward"
+        own = {x.data_ptr() for x in hooks.copies}
+        for i, (x, n) in enumerate(((q, "q"), (k, "k"))):
+            if layout is off_by_one:
+                assert args[i] not in own and args[i] % 16 == 0
+            else:
+                assert holds(args[i], getattr(op, n), hooks.copies, x.detach()), n
+        for i, x in enumerate((*weights, *tables)):
+            assert (args[2 + i] is None) if x is None else (args[2 + i] % 16 == 0 if layout is off_by_one else args[2 + i] in own)
+        if rotated:
+            assert holds(op.positions, VlaStrides(), hooks.copies, positions.contiguous())
+        assert (op.l2, op.interleaved, op.offset, op.rot, op.places) == (1, 1, 2, 16 if rotated else 0, 20 if rotated else 0)
+        assert abs(op.eps - 1e-5) < 1e-11 and [args[i] for i in range(12, 16)] == [B, T, H_q, H_k]
+
+
+def test_a_checkpointed_norm_reads_the_positions_that_are_formed_again(recorder):
+    q, k, tables = torch.randn(2, 3, 5, 16).requires_grad_(), torch.randn(2, 1, 5, 16), [torch.rand(20, 8) for _ in range(2)]
+    made = []
+
+    def layer(q):
+        made.append(torch.arange(10, dtype=torch.int32).view(2, 5))
+        return vla.qk_norm_rope(q, k, None, None, *tables, positions=made[-1])[0]
+
+    y = checkpoint(layer, q, use_reentrant=False)
+    first = recorder.last("vla_qk_norm_rope")[2].positions
+    y.sum().backward()
+    assert len(made) == 2 and first == made[0].data_ptr()
+    assert recorder.last("vla_qk_norm_rope_backward")[2].positions == made[1].data_ptr()

@@ -84,3 +84,48 @@ def test_a_checkpointed_delta_rule(dtype):
     torch.full((64,), 3, device="cuda", dtype=torch.int32)      # takes the place of the first lengths
     got = torch.autograd.grad(out, leaves, (do, dS))
     assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def norm_inputs(B, T, H_q, H_k, d, dtype, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    rows = randn(gen, B, T, (H_q + H_k) * d).to(DT[dtype])
+    leaves = [x.requires_grad_() for x in (rows, 1 + 0.1 * randn(gen, d), 1 + 0.1 * randn(gen, d))]
+    angle = torch.arange(64, device="cuda").unsqueeze(1) * 100.0 ** (-torch.arange(d // 4, device="cuda") * 4.0 / d)
+    return leaves, (angle.cos(), angle.sin()), [randn(gen, B, H, T, d).to(DT[dtype]) for H in (H_q, H_k)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hook", ["pageable", "pinned", "dense", "turned", "off_by_one"])
+def test_the_norm_under_saved_tensor_hooks(hook, dtype):
+    B, T, H_q, H_k, d = 3, 21, 4, 2, 64
+    leaves, tables, dy = norm_inputs(B, T, H_q, H_k, d, dtype, seed=3)
+    positions = torch.randint(0, 64, (1, T), device="cuda", dtype=torch.int32)
+
+    def grads():
+        q, k = leaves[0].view(B, T, -1, d).transpose(1, 2).split((H_q, H_k), 1)
+        out = vla.qk_norm_rope(q, k, *leaves[1:], *tables, positions=positions.expand(B, T), norm="l2")
+        return torch.autograd.grad(out, leaves, dy)
+
+    want = grads()
+    with hooks(hook):
+        got = grads()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_checkpointed_norm(dtype):
+    B, T, H_q, H_k, d = 2, 16, 3, 1, 32
+    leaves, tables, dy = norm_inputs(B, T, H_q, H_k, d, dtype, seed=4)
+    start = torch.tensor([[5], [40]]).cuda()
+
+    def layer(rows, *weights):
+        q, k = rows.view(B, T, -1, d).transpose(1, 2).split((H_q, H_k), 1)
+        positions = (start + torch.arange(T, device="cuda")).int()
+        return vla.qk_norm_rope(q, k, *weights, *tables, positions=positions, interleaved=True)
+
+    want = torch.autograd.grad(layer(*leaves), leaves, dy)
+    out = checkpoint(layer, *leaves, use_reentrant=False)
+    torch.full((128,), 7, device="cuda", dtype=torch.int32)     # takes the place of the first positions
+    got = torch.autograd.grad(out, leaves, dy)
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
