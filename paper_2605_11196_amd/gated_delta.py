@@ -212,6 +212,8 @@ def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, 
         _check(torch, q, k, v, g, beta, dS_T, "dS_T", lengths, 1)
     if do.shape != v.shape or do.dtype != v.dtype or do.device != v.device:
         raise ValueError("do must match v in shape, dtype and device")
+    if saved.dtype != torch.uint8 or saved.dim() != 1 or not saved.is_contiguous() or saved.device != q.device:
+        raise ValueError(f"saved must be what gated_delta_forward returned: a contiguous uint8 tensor on {q.device}")
     handle, context, outside = binding._on_stream(torch, q.device, stream)
     with context:
         kept, op = _inputs(key, q, k, v, g, beta, scale, lengths, segments)

@@ -205,3 +205,15 @@ def test_a_checkpointed_norm_reads_the_positions_that_are_formed_again(recorder)
     y.sum().backward()
     assert len(made) == 2 and first == made[0].data_ptr()
     assert recorder.last("vla_qk_norm_rope_backward")[2].positions == made[1].data_ptr()
+
+
+@pytest.mark.parametrize("change", [lambda x: x.float(), lambda x: x.to("meta"), lambda x: x.repeat_interleave(2)[::2], lambda x: x.view(16, -1)])
+def test_what_was_saved_is_looked_at(recorder, change):
+    """An address of another device or a tensor with gaps would be read all the same: the library sees an address and a size."""
+    _, inputs, _ = fused(1, 20, 1, 1, 32)
+    inputs = [x.detach() for x in inputs]
+    saved = torch.zeros(binding.load_library().vla_delta_saved_bytes(1, 1, 20, 32, 32, 0), dtype=torch.uint8)
+    with pytest.raises(ValueError, match="saved"):
+        vla.gated_delta_backward(*inputs, change(saved), inputs[2])
+    vla.gated_delta_backward(*inputs, saved, inputs[2])
+    assert recorder.last("vla_delta_backward")[2].saved == saved.data_ptr()
