@@ -37,6 +37,11 @@ def _check(torch, q, k, v, g, beta, state, state_name, lengths, tokens):
         raise ValueError(f"lengths must be an int32 tensor of shape {tuple(shape[:1])} on {dev}")
 
 
+def _aligned(S):
+    """A contiguous state (or None) at a 16-byte boundary."""
+    return S.clone() if S is not None and S.data_ptr() & 15 else S
+
+
 def _scale(scale):
     """The option's value, where 0 stands for the default."""
     if scale is None:
@@ -98,6 +103,7 @@ def _forward(torch, kept, op, S0, save, handle, outside):
     B, H_k, T, dk = q.shape
     H_v, dv, dev, io = v.shape[1], v.shape[3], q.device, _io(torch, q)
     lib = binding.load_library()
+    S0 = _aligned(S0)
     o = _like(torch, v)
     if not o.is_contiguous():
         op.o = _strides(o)
@@ -180,7 +186,7 @@ def _backward(torch, kept, op, saved, do, dS_T, handle, outside):
     B, H_k, T, dk = q.shape
     H_v, dv, dev, io = v.shape[1], v.shape[3], q.device, _io(torch, q)
     lib = binding.load_library()
-    do, op.o = _laid_out(do)
+    (do, op.o), dS_T = _laid_out(do), _aligned(dS_T)
     dq, dk_, dv_ = _like(torch, q), _like(torch, k), _like(torch, v)
     dg, dbeta = (torch.empty((B, H_v, T), dtype=torch.float32, device=dev) for _ in range(2))
     dS0 = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)

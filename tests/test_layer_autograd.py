@@ -217,3 +217,17 @@ def test_what_was_saved_is_looked_at(recorder, change):
         vla.gated_delta_backward(*inputs, change(saved), inputs[2])
     vla.gated_delta_backward(*inputs, saved, inputs[2])
     assert recorder.last("vla_delta_backward")[2].saved == saved.data_ptr()
+
+
+def test_states_and_their_gradients_may_start_anywhere(recorder):
+    """A state cut out of a larger buffer, and the gradient that torch.cat gives back: contiguous, not at a 16-byte boundary."""
+    _, inputs, S0 = fused(1, 20, 1, 1, 16)
+    inputs = [x.detach() for x in inputs]
+    S0 = off_by_one(S0).requires_grad_()
+    assert S0.data_ptr() % 16 and S0.is_contiguous()
+    o, S = vla.gated_delta(*inputs, S0)
+    address = recorder.last("vla_delta_forward")[1][5]
+    assert address % 16 == 0 and address != S0.data_ptr()
+    torch.cat((torch.ones(1), S.flatten())).sum().backward()
+    address = recorder.last("vla_delta_backward")[1][6]
+    assert address % 16 == 0 and address

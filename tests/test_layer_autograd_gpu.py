@@ -129,3 +129,15 @@ def test_a_checkpointed_norm(dtype):
     torch.full((128,), 7, device="cuda", dtype=torch.int32)     # takes the place of the first positions
     got = torch.autograd.grad(out, leaves, dy)
     assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_a_state_that_starts_anywhere():
+    """Cut out of a larger buffer; its gradient comes back from torch.cat, not at a 16-byte boundary either."""
+    leaves, do, dS = projection(2, 40, 1, 2, 32, "f32", seed=5)
+    inputs = sliced(*leaves[:2], 1, 2, 32)
+    want = torch.autograd.grad(vla.gated_delta(*inputs, leaves[2]), leaves, (do, dS), retain_graph=True)
+    S0 = off_by_one(leaves[2].detach()).requires_grad_()
+    o, S = vla.gated_delta(*inputs, S0)
+    joined = torch.cat((torch.zeros(1, device="cuda"), S.flatten(), o.flatten()))
+    got = torch.autograd.grad(joined, (*leaves[:2], S0), torch.cat((torch.zeros(1, device="cuda"), dS.flatten(), do.flatten())))
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
