@@ -4,7 +4,7 @@ import functools
 
 from . import binding
 from .binding import VlaDeltaOpts, VlaError, VlaStrides
-from .qk_norm import _io, _keep_plan, _kind, _laid_out, _like, _p, _steps, _strides, _together
+from .qk_norm import _fits, _io, _keep_plan, _kind, _laid_out, _like, _p, _steps, _strides, _together
 
 
 def _gate(x):
@@ -18,6 +18,7 @@ def _gate(x):
 def _check(torch, q, k, v, g, beta, state, state_name, lengths, tokens):
     """Shapes of a call over tokens (tokens 1) or of one token (0); state: the given state or gradient of it, or None."""
     dev, dtype, shape, v_shape = q.device, q.dtype, q.shape, v.shape
+    _fits("sizes", *shape, *v_shape)
     if not (q.is_cuda and k.is_cuda and v.is_cuda):
         raise ValueError("q, k, v must be GPU tensors (no CPU path exists)")
     if k.dtype != dtype or v.dtype != dtype or k.device != dev or v.device != dev:
@@ -71,6 +72,7 @@ def _inputs(key, q, k, v, g, beta, scale, lengths, segments=0):
             op.lengths = lengths.data_ptr()
         return given, op
     op = VlaDeltaOpts(_scale(scale))
+    _fits("segments", segments)
     op.segments = segments
     (q, op.q), (k, op.k), (v, op.v) = _laid_out(q), _laid_out(k), _laid_out(v)
     (g, g_strides), (beta, beta_strides) = _gate(g), _gate(beta)

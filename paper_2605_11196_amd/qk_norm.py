@@ -13,6 +13,13 @@ def _io(torch, x):
     raise ValueError(f"unsupported dtype {x.dtype}")
 
 
+def _fits(what, *numbers):
+    """ctypes cuts what an int of the library does not hold."""
+    for n in numbers:
+        if not -2 ** 31 <= n < 2 ** 31:
+            raise ValueError(f"{what} must fit 32 bits, not {n}")
+
+
 def _steps(x):
     """The strides of the first three dimensions; 0 where a dimension has one entry and its stride says nothing."""
     return [step if n > 1 else 0 for step, n in zip(x.stride(), x.shape[:3])]
@@ -47,6 +54,7 @@ def _like(torch, x):
 
 def _check(torch, q, k, q_weight, k_weight, cos, sin, positions, norm):
     dev, dtype, shape, k_shape = q.device, q.dtype, q.shape, k.shape
+    _fits("sizes", *shape, *k_shape)
     if not (q.is_cuda and k.is_cuda):
         raise ValueError("q and k must be GPU tensors (no CPU path exists)")
     if k.dtype != dtype or len(shape) != 4 or len(k_shape) != 4 or shape[0] != k_shape[0] or shape[2:] != k_shape[2:] or k.device != dev:
@@ -63,6 +71,7 @@ def _check(torch, q, k, q_weight, k_weight, cos, sin, positions, norm):
         raise ValueError("cos and sin come together")
     if cos is not None:
         table = cos.shape
+        _fits("sizes", *table)
         if (cos.dtype != torch.float32 or sin.dtype != torch.float32 or len(table) != 2 or sin.shape != table or cos.device != dev
                 or sin.device != dev or not 0 < 2 * table[1] <= d or table[0] < 1):
             raise ValueError(f"cos and sin must be float32 tensors [positions, rot / 2] on {dev}")
@@ -101,6 +110,7 @@ def _key(q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, inter
 def _call(torch, key, q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, interleaved):
     """What both directions share: the tensors as the kernels take them, which have to live until the call, and the options."""
     given = q, k, q_weight, k_weight, cos, sin, positions
+    _fits("offset", offset)
     plan = _plans.get(key)
     if plan is not None and not (q.data_ptr() | k.data_ptr() | (_p(q_weight) or 0) | (_p(k_weight) or 0) | (_p(cos) or 0) | (_p(sin) or 0)) & 15:
         op = VlaNormOpts.from_buffer_copy(plan)

@@ -231,3 +231,33 @@ def test_states_and_their_gradients_may_start_anywhere(recorder):
     torch.cat((torch.ones(1), S.flatten())).sum().backward()
     address = recorder.last("vla_delta_backward")[1][6]
     assert address % 16 == 0 and address
+
+
+@pytest.mark.parametrize("number", [2 ** 31, 2 ** 32 + 3, -2 ** 40])
+def test_numbers_that_32_bits_do_not_hold_are_refused(recorder, number):
+    """ctypes would cut them: position 3 in the place of 2^32 + 3."""
+    _, inputs, _ = fused(1, 20, 1, 1, 32)
+    q, k, v, g, beta = (x.detach() for x in inputs)
+    tables = [torch.rand(64, 16) for _ in range(2)]
+    saved = torch.zeros(binding.load_library().vla_delta_saved_bytes(1, 1, 20, 32, 32, 0), dtype=torch.uint8)
+    for call in (lambda: vla.qk_norm_rope(q, k, None, None, *tables, offset=number),
+                 lambda: vla.qk_norm_rope_backward(q, k, None, None, *tables, q, k, offset=number),
+                 lambda: vla.gated_delta_forward(q, k, v, g, beta, segments=number),
+                 lambda: vla.gated_delta_backward(q, k, v, g, beta, saved, v, segments=number)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    vla.qk_norm_rope(q, k, None, None, *tables, offset=2 ** 31 - 1)
+    assert recorder.calls[-1][2].offset == 2 ** 31 - 1
+
+
+def test_sizes_that_32_bits_do_not_hold_are_refused():
+    """2^32 + 5 tokens would be taken for 5."""
+    x = torch.empty((1, 1, 2 ** 32 + 5, 16), device="meta")
+    gate = torch.empty((1, 1, 2 ** 32 + 5), device="meta")
+    with pytest.raises(ValueError, match="32 bits"):
+        vla.qk_norm_rope(x, x)
+    with pytest.raises(ValueError, match="32 bits"):
+        vla.gated_delta_forward(x, x, x, gate, gate)
+    one = torch.empty((2 ** 31, 1, 16), device="meta")
+    with pytest.raises(ValueError, match="32 bits"):
+        vla.gated_delta_decode_step(one, one, one, one[..., 0], one[..., 0], torch.empty((2 ** 31, 1, 16, 16), device="meta"))
