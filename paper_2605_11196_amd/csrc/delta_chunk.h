@@ -179,14 +179,14 @@ __device__ __forceinline__ void chunk_segment(const DeltaArgs& a, int head, int 
       R[1] = O::mul_tok(inv[1], O::tokens(O::mul_tok(under, rb[0], O::value(vr[1]) - gamma[1] * P[1]), one), zero);
       if (!MAP) rb[1] = O::tokens(R[1], one);
       if (!MAP && a.rows != nullptr) {
-        const __amdgpu_buffer_rsrc_t out = rows_buffer(a.rows + (static_cast<size_t>(head) * a.T + t0) * DV, DV * 4, last - t0, DV * 4);
+        const __amdgpu_buffer_rsrc_t out = rows_buffer(a.rows + (static_cast<size_t>(head) * a.T + t0) * DV, DV * 4, end - t0, DV * 4);
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) store_column(out, ((16 * i + 4 * g) * DV + col()) * 4, DV * 4, R[i], static_cast<float*>(nullptr));
       }
       const typename O::B w = O::pair(R[0] * w0, R[1] * w1, one);
       if constexpr (!MAP) {
         const decltype(O::image(att[0], c, g)) at[3] = {O::image(att[0], c, g), O::image(att[1], c, g), O::image(att[2], c, g)};
-        const __amdgpu_buffer_rsrc_t out = rows_buffer(o + t0 * o_step, o_step, last - t0, DV * static_cast<int>(sizeof(IO)));
+        const __amdgpu_buffer_rsrc_t out = rows_buffer(o + t0 * o_step, o_step, end - t0, DV * static_cast<int>(sizeof(IO)));
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
           f4 x = gamma[i] * scale * QS[i];
@@ -206,10 +206,10 @@ __device__ __forceinline__ void chunk_segment(const DeltaArgs& a, int head, int 
     }
   }
 
-  // ---- outputs of tokens past the end of the sequence, the state
+  // ---- outputs of tokens past the end of the sequence (the block that it ends in stores none for them: they would be NaN beside an infinite
+  // state), the state
   if constexpr (!MAP) {
-    const int done = first < end ? first + (end - first + kTok - 1) / kTok * kTok : first;
-    for (int t = done + wave; t < last; t += WAVES) {
+    for (int t = max(first, end) + wave; t < last; t += WAVES) {
       for (int i = lane; i < DV; i += 64) io_store(reinterpret_cast<IO*>(o + t * o_step) + i, 0.0f);
     }
   }

@@ -245,9 +245,9 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
       for (int j = 0; j < kTiles; ++j) dK[i] = O::mul_tok_raw(O::image(Z[2 * i + j], c, g), kr[j], dK[i]);
     }
     {
-      const __amdgpu_buffer_rsrc_t part = rows_buffer(a.dk_part + (row0 + t0) * DK, DK * 4, last - t0, DK * 4);
-      const __amdgpu_buffer_rsrc_t qpart = rows_buffer(a.dq_part + (row0 + t0) * DK, DK * 4, shared ? last - t0 : 0, DK * 4);
-      const __amdgpu_buffer_rsrc_t out = rows_buffer(dq + t0 * a.dqs.t * sizeof(IO), a.dqs.t * sizeof(IO), shared ? 0 : last - t0, DK * static_cast<int>(sizeof(IO)));
+      const __amdgpu_buffer_rsrc_t part = rows_buffer(a.dk_part + (row0 + t0) * DK, DK * 4, end - t0, DK * 4);
+      const __amdgpu_buffer_rsrc_t qpart = rows_buffer(a.dq_part + (row0 + t0) * DK, DK * 4, shared ? end - t0 : 0, DK * 4);
+      const __amdgpu_buffer_rsrc_t out = rows_buffer(dq + t0 * a.dqs.t * sizeof(IO), a.dqs.t * sizeof(IO), shared ? 0 : end - t0, DK * static_cast<int>(sizeof(IO)));
       const int step = static_cast<int>(a.dqs.t * sizeof(IO));
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
@@ -310,8 +310,8 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) dK[i] = O::mul_split_out(O::template rows_split<TW, RV>(sR, i, s, c, g), x, dK[i]);
     }
-    const __amdgpu_buffer_rsrc_t part = rows_buffer(a.dk_part + (row0 + t0) * DK, DK * 4, last - t0, DK * 4);
-    const __amdgpu_buffer_rsrc_t out = rows_buffer(dk + t0 * a.dks.t * sizeof(IO), a.dks.t * sizeof(IO), last - t0, DK * static_cast<int>(sizeof(IO)));
+    const __amdgpu_buffer_rsrc_t part = rows_buffer(a.dk_part + (row0 + t0) * DK, DK * 4, end - t0, DK * 4);
+    const __amdgpu_buffer_rsrc_t out = rows_buffer(dk + t0 * a.dks.t * sizeof(IO), a.dks.t * sizeof(IO), end - t0, DK * static_cast<int>(sizeof(IO)));
     const int step = static_cast<int>(a.dks.t * sizeof(IO));
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
@@ -364,8 +364,7 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
     }
   }
   // ---- tokens past the end of the sequence
-  const int done = first < end ? start + kTok : first;
-  for (int t = done + static_cast<int>(threadIdx.x) / 16; t < last; t += THREADS / 16) {
+  for (int t = max(first, end) + static_cast<int>(threadIdx.x) / 16; t < last; t += THREADS / 16) {
     for (int x = threadIdx.x % 16; x < DK; x += 16) {
       if (shared) {
         a.dq_part[(row0 + t) * DK + x] = 0.0f;

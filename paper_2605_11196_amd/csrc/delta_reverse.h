@@ -165,8 +165,8 @@ __device__ __forceinline__ void reverse_segment(const DeltaArgs& a, int head, in
         if (i + 1 < kTiles) wb[i] = O::tokens(W[i], one);
       }
       if constexpr (!MAP) {
-        const __amdgpu_buffer_rsrc_t rows = rows_buffer(a.rows + (static_cast<size_t>(head) * a.T + t0) * DV, DV * 4, last - t0, DV * 4);
-        const __amdgpu_buffer_rsrc_t out = rows_buffer(dv + t0 * dv_step, dv_step, last - t0, DV * static_cast<int>(sizeof(IO)));
+        const __amdgpu_buffer_rsrc_t rows = rows_buffer(a.rows + (static_cast<size_t>(head) * a.T + t0) * DV, DV * 4, end - t0, DV * 4);
+        const __amdgpu_buffer_rsrc_t out = rows_buffer(dv + t0 * dv_step, dv_step, end - t0, DV * static_cast<int>(sizeof(IO)));
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
           const int t = kTok - 1 - (16 * i + 4 * g);
@@ -202,8 +202,7 @@ __device__ __forceinline__ void reverse_segment(const DeltaArgs& a, int head, in
 
   // ---- gradients of tokens past the end of the sequence, of the state
   if constexpr (!MAP) {
-    const int done = first + blocks * kTok;
-    for (int t = done + wave; t < last; t += WAVES) {
+    for (int t = max(first, end) + wave; t < last; t += WAVES) {
       for (int i = lane; i < DV; i += 64) io_store(reinterpret_cast<IO*>(dv + t * dv_step) + i, 0.0f);
     }
   }
