@@ -182,8 +182,8 @@ def gated_delta_decode_step(q, k, v, g, beta, S, *, scale=None, stream=None):
     return o
 
 
-def _backward(torch, kept, op, saved, do, dS_T, handle, outside):
-    """kept, op, handle, outside: as for _forward().  The gradients."""
+def _backward(torch, kept, op, saved, do, dS_T, state, handle, outside):
+    """kept, op, handle, outside: as for _forward().  The gradients, with state also that of S0."""
     q, k, v, g, beta, _ = kept
     B, H_k, T, dk = q.shape
     H_v, dv, dev, io = v.shape[1], v.shape[3], q.device, _io(torch, q)
@@ -191,7 +191,7 @@ def _backward(torch, kept, op, saved, do, dS_T, handle, outside):
     (do, op.o), dS_T = _laid_out(do), _aligned(dS_T)
     dq, dk_, dv_ = _like(torch, q), _like(torch, k), _like(torch, v)
     dg, dbeta = (torch.empty((B, H_v, T), dtype=torch.float32, device=dev) for _ in range(2))
-    dS0 = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev)
+    dS0 = torch.empty((B, H_v, dv, dk), dtype=torch.float32, device=dev) if state else None
     op.dq, op.dk, op.dv = _strides(dq), _strides(dk_), _strides(dv_)
     saved = _together(saved)
     op.saved, op.saved_bytes = saved.data_ptr(), saved.numel()
@@ -199,22 +199,18 @@ def _backward(torch, kept, op, saved, do, dS_T, handle, outside):
     ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
     outputs = (dq, dk_, dv_, dg, dbeta, dS0)
     if outside is not None:
-        for t in outputs:
+        for t in outputs[:6 if state else 5]:
             t.record_stream(outside)
     rc = lib.vla_delta_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), do.data_ptr(), _p(dS_T), dq.data_ptr(),
-                                dk_.data_ptr(), dv_.data_ptr(), dg.data_ptr(), dbeta.data_ptr(), dS0.data_ptr(), B, H_k, H_v, T, dk, dv, io,
+                                dk_.data_ptr(), dv_.data_ptr(), dg.data_ptr(), dbeta.data_ptr(), _p(dS0), B, H_k, H_v, T, dk, dv, io,
                                 ctypes.byref(op), _p(ws), need, handle)
     if rc != 0:
         raise VlaError(rc, binding.status_string(rc), "vla_delta_backward")
     return outputs
 
 
-def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, lengths=None, segments=0, stream=None):
-    """The gradients (dq, dk, dv, dg, dbeta, dS0) of gated_delta_forward's inputs, given those of o and S_T (None: zero), the same inputs
-    and what it saved.  dg, dbeta and dS0 are float32."""
-    import torch
-
-    scale = None if scale is None else float(scale)
+def _gradients(torch, q, k, v, g, beta, saved, do, dS_T, scale, lengths, segments, state, stream):
+    """gated_delta_backward on these tensors; state: as for _backward()."""
     key = _key(q, k, v, g, beta, dS_T, lengths, scale, segments)
     if key not in _plans:
         _check(torch, q, k, v, g, beta, dS_T, "dS_T", lengths, 1)
@@ -225,7 +221,16 @@ def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, 
     handle, context, outside = binding._on_stream(torch, q.device, stream)
     with context:
         kept, op = _inputs(key, q, k, v, g, beta, scale, lengths, segments)
-        return _backward(torch, kept, op, saved, do, dS_T, handle, outside)
+        return _backward(torch, kept, op, saved, do, dS_T, state, handle, outside)
+
+
+def gated_delta_backward(q, k, v, g, beta, saved, do, dS_T=None, *, scale=None, lengths=None, segments=0, stream=None):
+    """The gradients (dq, dk, dv, dg, dbeta, dS0) of gated_delta_forward's inputs, given those of o and S_T (None: zero), the same inputs
+    and what it saved.  dg, dbeta and dS0 are float32."""
+    import torch
+
+    scale = None if scale is None else float(scale)
+    return _gradients(torch, q, k, v, g, beta, saved, do, dS_T, scale, lengths, segments, True, stream)
 
 
 _function = None
@@ -244,7 +249,7 @@ def _autograd():
                     kept, op = _inputs(key, q, k, v, g, beta, scale, lengths)
                     o, S_T, saved = _forward(torch, kept, op, S0, True, handle, outside)
                 ctx.save_for_backward(*kept, saved)      # the inputs as the kernels read them
-                ctx.scale, ctx.has_state = scale, S0 is not None
+                ctx.scale = scale
                 ctx.set_materialize_grads(False)
                 return o, S_T
 
@@ -255,8 +260,8 @@ def _autograd():
                 q, k, v, g, beta, lengths, saved = ctx.saved_tensors
                 do = torch.zeros_like(v) if do is None else do
                 dS_T = None if dS_T is None else dS_T.contiguous()
-                grads = gated_delta_backward(q, k, v, g, beta, saved, do, dS_T, scale=ctx.scale, lengths=lengths)
-                return (*grads[:5], grads[5] if ctx.has_state else None, None, None, None)
+                grads = _gradients(torch, q, k, v, g, beta, saved, do, dS_T, ctx.scale, lengths, 0, ctx.needs_input_grad[5], None)
+                return (*grads, None, None, None)
 
         _function = GatedDelta
     return _function

@@ -164,8 +164,8 @@ def _forward(torch, kept, op, handle, outside):
     return q_out, k_out
 
 
-def _backward(torch, kept, op, dq_out, dk_out, handle, outside):
-    """kept, op, handle, outside: as for _forward().  The gradients (dq, dk, dq_weight, dk_weight)."""
+def _backward(torch, kept, op, dq_out, dk_out, wanted, handle, outside):
+    """kept, op, handle, outside: as for _forward().  The gradients (dq, dk, dq_weight, dk_weight), of the weights those that are wanted."""
     q, k, q_weight, k_weight = kept[:4]
     B, H_q, T, d = q.shape
     dev = q.device
@@ -173,9 +173,9 @@ def _backward(torch, kept, op, dq_out, dk_out, handle, outside):
     (dq_out, op.q_out), (dk_out, op.k_out) = _laid_out(dq_out), _laid_out(dk_out)
     dq, dk = _like(torch, q), _like(torch, k)
     op.dq, op.dk = _strides(dq), _strides(dk)
-    dwq = None if q_weight is None else torch.empty_like(q_weight)
-    dwk = None if k_weight is None else torch.empty_like(k_weight)
-    need = lib.vla_qk_norm_rope_workspace_bytes(d) if q_weight is not None or k_weight is not None else 0
+    dwq = torch.empty_like(q_weight) if wanted[0] and q_weight is not None else None
+    dwk = torch.empty_like(k_weight) if wanted[1] and k_weight is not None else None
+    need = lib.vla_qk_norm_rope_workspace_bytes(d) if dwq is not None or dwk is not None else 0
     ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
     if outside is not None:
         for t in (dq, dk, dwq, dwk):
@@ -189,6 +189,20 @@ def _backward(torch, kept, op, dq_out, dk_out, handle, outside):
     return dq, dk, dwq, dwk
 
 
+def _gradients(torch, q, k, q_weight, k_weight, cos, sin, positions, how, dq_out, dk_out, wanted, stream):
+    """qk_norm_rope_backward on these tensors; wanted: as for _backward()."""
+    key = _key(q, k, q_weight, k_weight, cos, sin, positions, *how)
+    if key not in _plans:
+        _check(torch, q, k, q_weight, k_weight, cos, sin, positions, how[2])
+    for x, y in ((q, dq_out), (k, dk_out)):
+        if y.shape != x.shape or y.dtype != x.dtype or y.device != x.device:
+            raise ValueError("dq_out and dk_out must match q and k in shape, dtype and device")
+    handle, context, outside = binding._on_stream(torch, q.device, stream)
+    with context:
+        kept, op = _call(torch, key, q, k, q_weight, k_weight, cos, sin, positions, *how)
+        return _backward(torch, kept, op, dq_out, dk_out, wanted, handle, outside)
+
+
 def qk_norm_rope_backward(q, k, q_weight, k_weight, cos, sin, dq_out, dk_out, *, positions=None, offset=0, eps=1e-6, norm="rms",
                           interleaved=False, stream=None):
     """The gradients of qk_norm_rope's q, k, q_weight and k_weight (None where there is no weight; summed in float32 and of the weights'
@@ -196,15 +210,7 @@ def qk_norm_rope_backward(q, k, q_weight, k_weight, cos, sin, dq_out, dk_out, *,
     import torch
 
     how = (int(offset), float(eps), norm, interleaved)
-    key = _key(q, k, q_weight, k_weight, cos, sin, positions, *how)
-    if key not in _plans:
-        _check(torch, q, k, q_weight, k_weight, cos, sin, positions, norm)
-    if any(y.shape != x.shape or y.dtype != x.dtype or y.device != x.device for x, y in ((q, dq_out), (k, dk_out))):
-        raise ValueError("dq_out and dk_out must match q and k in shape, dtype and device")
-    handle, context, outside = binding._on_stream(torch, q.device, stream)
-    with context:
-        kept, op = _call(torch, key, q, k, q_weight, k_weight, cos, sin, positions, *how)
-        return _backward(torch, kept, op, dq_out, dk_out, handle, outside)
+    return _gradients(torch, q, k, q_weight, k_weight, cos, sin, positions, how, dq_out, dk_out, (True, True), stream)
 
 
 _function = None
@@ -233,9 +239,7 @@ def _autograd():
                 q, k, q_weight, k_weight, cos, sin, positions = ctx.saved_tensors
                 dq_out = torch.zeros_like(q) if dq_out is None else dq_out
                 dk_out = torch.zeros_like(k) if dk_out is None else dk_out
-                offset, eps, norm, interleaved = ctx.how
-                grads = qk_norm_rope_backward(q, k, q_weight, k_weight, cos, sin, dq_out, dk_out, positions=positions, offset=offset, eps=eps,
-                                              norm=norm, interleaved=interleaved)
+                grads = _gradients(torch, q, k, q_weight, k_weight, cos, sin, positions, ctx.how, dq_out, dk_out, ctx.needs_input_grad[2:4], None)
                 return (*grads, None, None, None, None, None)
 
         _function = QkNormRope

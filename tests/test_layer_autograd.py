@@ -261,3 +261,25 @@ def test_sizes_that_32_bits_do_not_hold_are_refused():
     one = torch.empty((2 ** 31, 1, 16), device="meta")
     with pytest.raises(ValueError, match="32 bits"):
         vla.gated_delta_decode_step(one, one, one, one[..., 0], one[..., 0], torch.empty((2 ** 31, 1, 16, 16), device="meta"))
+
+
+@pytest.mark.parametrize("wanted", [(), (0,), (1,), (0, 1)])
+def test_gradients_of_frozen_weights_are_not_formed(recorder, wanted):
+    q, k = torch.randn(2, 3, 5, 16).requires_grad_(), torch.randn(2, 1, 5, 16)
+    weights = [torch.rand(16).requires_grad_(i in wanted) for i in range(2)]
+    out = vla.qk_norm_rope(q, k, *weights)
+    (out[0].sum() + out[1].sum()).backward()
+    args = recorder.last("vla_qk_norm_rope_backward")[1]
+    assert [i for i in range(2) if args[10 + i] is not None] == list(wanted)
+    assert (args[19] is not None) == bool(wanted) and (args[20] > 0) == bool(wanted)       # the workspace of the sums
+    assert [w.grad is not None for w in weights] == [i in wanted for i in range(2)]
+
+
+@pytest.mark.parametrize("state", ["none", "frozen", "learned"])
+def test_the_gradient_of_a_state_that_nothing_asks_for_is_not_formed(recorder, state):
+    _, inputs, S0 = fused(1, 20, 1, 1, 16)
+    S0 = None if state == "none" else S0.requires_grad_(state == "learned")
+    o, S = vla.gated_delta(*inputs, S0)
+    (o.sum() + S.sum()).backward()
+    assert (recorder.last("vla_delta_backward")[1][12] is not None) == (state == "learned")
+    assert S0 is None or (S0.grad is not None) == (state == "learned")
