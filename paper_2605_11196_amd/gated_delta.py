@@ -152,10 +152,14 @@ def gated_delta_forward(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, 
 
 
 def gated_delta_decode_step(q, k, v, g, beta, S, *, scale=None, stream=None):
-    """One token for every head: q, k [B,H_k,d_k], v [B,H_v,d_v], g, beta [B,H_v] float32; S [B,H_v,d_v,d_k] float32 is updated in
-    place.  Returns o [B,H_v,d_v]."""
+    """One token for every head: q, k [B,H_k,d_k], v [B,H_v,d_v], g, beta [B,H_v] float32; S [B,H_v,d_v,d_k] float32, contiguous and
+    16-byte aligned, is updated in place.  Returns o [B,H_v,d_v].  Without a gradient: for generation, under torch.no_grad() where an
+    input asks for one."""
     import torch
 
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or g.requires_grad or beta.requires_grad
+                                    or S.requires_grad):
+        raise ValueError("gated_delta_decode_step has no gradient: call it under torch.no_grad(), or gated_delta with one token")
     scale = None if scale is None else float(scale)
     key = _key(q, k, v, g, beta, S, None, scale)
     plan = _plans.get(key)
@@ -179,6 +183,8 @@ def gated_delta_decode_step(q, k, v, g, beta, S, *, scale=None, stream=None):
                                                           o.data_ptr(), B, H_k, H_v, dk, dv, _io(torch, q), ctypes.byref(op), handle)
     if rc != 0:
         raise VlaError(rc, binding.status_string(rc), "vla_delta_decode_step")
+    if not S.is_inference():
+        torch.autograd.graph.increment_version(S)     # a graph that saved S must not use what it holds now
     return o
 
 

@@ -283,3 +283,26 @@ def test_the_gradient_of_a_state_that_nothing_asks_for_is_not_formed(recorder, s
     (o.sum() + S.sum()).backward()
     assert (recorder.last("vla_delta_backward")[1][12] is not None) == (state == "learned")
     assert S0 is None or (S0.grad is not None) == (state == "learned")
+
+
+def test_a_single_token_has_no_gradient_and_says_so(recorder):
+    """The state is updated in place without a graph: inputs that ask for gradients are refused, what saved the state learns of the update."""
+    names = ("q", "k", "v", "g", "beta", "S")
+    made = lambda: dict(zip(names, [torch.randn(2, 1, 16) for _ in range(3)] + [torch.randn(2, 1) for _ in range(2)] + [torch.randn(2, 1, 16, 16)]))
+    for name in names:
+        inputs = made()
+        vla.gated_delta_decode_step(**inputs)
+        inputs[name].requires_grad_()
+        with pytest.raises(ValueError, match="no_grad"):
+            vla.gated_delta_decode_step(**inputs)
+        with torch.no_grad():
+            vla.gated_delta_decode_step(**inputs)
+    inputs = made()
+    w = torch.randn(2, 1, 16, 16).requires_grad_()
+    y = (w * inputs["S"]).sum()          # saves S
+    with torch.no_grad():
+        vla.gated_delta_decode_step(**inputs)
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.backward()
+    with torch.inference_mode():
+        vla.gated_delta_decode_step(**made())
