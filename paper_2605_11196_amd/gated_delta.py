@@ -4,7 +4,7 @@ import functools
 
 from . import binding
 from .binding import VlaDeltaOpts, VlaError, VlaStrides
-from .qk_norm import _fits, _io, _keep_plan, _kind, _laid_out, _like, _p, _steps, _strides, _together
+from .qk_norm import _fits, _io, _keep_plan, _kind, _laid_out, _like, _no_tangents, _p, _steps, _strides, _together
 
 
 def _gate(x):
@@ -157,6 +157,7 @@ def gated_delta_decode_step(q, k, v, g, beta, S, *, scale=None, stream=None):
     input asks for one."""
     import torch
 
+    _no_tangents(torch, q, k, v, g, beta, S)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or g.requires_grad or beta.requires_grad
                                     or S.requires_grad):
         raise ValueError("gated_delta_decode_step has no gradient: call it under torch.no_grad(), or gated_delta with one token")
@@ -274,9 +275,11 @@ def _autograd():
 
 
 def gated_delta(q, k, v, g, beta, S0=None, *, scale=None, lengths=None, stream=None):
-    """gated_delta_forward as a differentiable function: (o, S_T), with gradients for q, k, v, g, beta and S0 (on the current stream)."""
+    """gated_delta_forward as a differentiable function: (o, S_T), with gradients for q, k, v, g, beta and S0 (once, in reverse mode, on
+    the current stream)."""
     import torch
 
+    _no_tangents(torch, q, k, v, g, beta, S0)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or g.requires_grad or beta.requires_grad
                                     or S0 is not None and S0.requires_grad):
         if stream is not None:

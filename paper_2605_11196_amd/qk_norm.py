@@ -20,6 +20,13 @@ def _fits(what, *numbers):
             raise ValueError(f"{what} must fit 32 bits, not {n}")
 
 
+def _no_tangents(torch, *tensors):
+    """Refuses tensors of forward mode, whose tangents would be lost."""
+    ad = torch.autograd.forward_ad
+    if getattr(ad, "_current_level", -1) >= 0 and any(x is not None and ad.unpack_dual(x).tangent is not None for x in tensors):
+        raise NotImplementedError("gradients in reverse mode alone: no jvp for forward mode")
+
+
 def _steps(x):
     """The strides of the first three dimensions; 0 where a dimension has one entry and its stride says nothing."""
     return [step if n > 1 else 0 for step, n in zip(x.stride(), x.shape[:3])]
@@ -254,10 +261,11 @@ def qk_norm_rope(q, k, q_weight=None, k_weight=None, cos=None, sin=None, *, posi
     of a fused projection [B,T,H d] with tokens and heads swapped.  norm: "rms" (by the root of the mean square) or "l2" (unit length).
     q_weight, k_weight: [d] or None.  cos, sin: float32 [positions, rot / 2], the tables of the rotation of the first rot
     columns (None: no rotation).  Token t is at positions[b, t] (int32), or at offset + t.  Returns contiguous (q, k), which
-    vla_forward and gated_delta take; differentiable in q, k and the weights (on the current stream).
+    vla_forward and gated_delta take; differentiable in q, k and the weights (once, in reverse mode, on the current stream).
     """
     import torch
 
+    _no_tangents(torch, q, k, q_weight, k_weight, cos, sin)
     how = (int(offset), float(eps), norm, interleaved)
     train = torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or q_weight is not None and q_weight.requires_grad
                                          or k_weight is not None and k_weight.requires_grad)

@@ -306,3 +306,22 @@ def test_a_single_token_has_no_gradient_and_says_so(recorder):
         y.backward()
     with torch.inference_mode():
         vla.gated_delta_decode_step(**made())
+
+
+def test_forward_mode_tangents_are_refused(recorder):
+    """There are gradients in reverse alone; a tangent was dropped where no input asked for one of those."""
+    import torch.autograd.forward_ad as forward_ad
+
+    _, inputs, _ = fused(1, 4, 1, 1, 16)
+    q, k, v, g, beta = (x.detach() for x in inputs)
+    one = [x[:, :, 0] for x in (q, k, v, g, beta)]
+    with forward_ad.dual_level():
+        vla.gated_delta(q, k, v, g, beta)
+        vla.qk_norm_rope(q, k)
+        with torch.no_grad():
+            vla.gated_delta_decode_step(*one, torch.zeros(1, 1, 16, 16))
+        dual = forward_ad.make_dual(q, torch.ones_like(q))
+        for call in (lambda: vla.gated_delta(dual, k, v, g, beta), lambda: vla.qk_norm_rope(dual, k),
+                     lambda: vla.gated_delta_decode_step(dual[:, :, 0], *one[1:], torch.zeros(1, 1, 16, 16))):
+            with pytest.raises(NotImplementedError, match="jvp"):
+                call()
