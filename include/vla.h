@@ -303,7 +303,8 @@ int vla_delta_decode_step(const void* q, const void* k, const void* v, const flo
  *   dv      [B, H_v, T, d_v] io_dtype;  dg, dbeta [B, H_v, T] float32;  dS0 [B, H_v, d_v, d_k] float32 or NULL (not wanted)
  * The same inputs and saved states give the same bits.  dg is the sum of the differences dO_i . O_i - v_i . dV_i over up to 256 tokens and of
  * <dS, S> behind them, and exact to float32's rounding of these terms: where strong decays make it far smaller than they are, what is
- * left of their rounding (1e-7 of them) shows.
+ * left of their rounding (1e-7 of them) shows.  A decay that is 0 in float32 (g < -104) ends the sums: its dg is 0, and nothing behind it
+ * counts for the tokens before it.
  */
 int vla_delta_backward(const void* q, const void* k, const void* v, const float* g, const float* beta, const void* dO, const float* dS_T,
                        void* dq, void* dk, void* dv, float* dg, float* dbeta, float* dS0, int B, int H_k, int H_v, int T, int d_k,

@@ -8,6 +8,7 @@
 //   dg_t = sum over the tokens i >= t of (dO_i . O_i - v_i . dV_i), up to any later place, + <dS, S> there
 // The last line: the loss does not change when the state and all that is written later grow by a factor and all that is read shrinks by it;
 // so the gradient of a decay is <dS, S> right behind it, and between two places that differs by what the tokens read and write.  dO . O = q . dQ.
+// A decay of 0 ends the sums, with 0.
 //
 // A sweep along the tokens carries S (everything but the last term of dK), a sweep back carries dS.  Here a wave has 16 columns of what has
 // d_k columns, so that the products over d_v stay in it; states are tiles with d_v along the rows, left operands the rows of dO, R and W in
@@ -336,31 +337,46 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
     __syncthreads();
   }
 
-  // ---- the decays' gradients: sums from the end of the 256 tokens in float64
+  // ---- the decays' gradients: sums from the end of the 256 tokens in float64.  Past a decay that is 0 in float32 nothing counts: its own gradient
+  // and what lies behind it add up to 0, but their rounding would not.
   __syncthreads();
   if (wave == 0) {
     double all = 0.0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) all += static_cast<double>(whole[w]);
     constexpr int EACH = kKeep / 64;
+    constexpr float kForgets = -104.0f;      // exp of less is below half of the smallest float32 number
     double sum[EACH], tail = 0.0;
+    int cut = 0, cuts[EACH];                 // whether a token from here to the lane's last one forgets the state
 #pragma unroll
     for (int i = EACH - 1; i >= 0; --i) {
-      const int t = EACH * lane + i;
-      if (first + t < end) tail += static_cast<double>(change[t]);
+      const int t = first + EACH * lane + i;
+      if (t < end) {
+        tail += static_cast<double>(change[t - first]);
+        if (gp[t * a.gs.t] < kForgets) {
+          tail = 0.0;
+          cut = 1;
+        }
+      }
       sum[i] = tail;
+      cuts[i] = cut;
     }
-    double later = tail;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const double other = __shfl_down(later, d, 64);
-      if (lane + d < 64) later += other;
+    for (int d = 1; d < 64; d *= 2) {        // of the lanes from here on, up to the first that cuts
+      const double other = __shfl_down(tail, d, 64);
+      const int other_cut = __shfl_down(cut, d, 64);
+      if (lane + d < 64 && !cut) {
+        tail += other;
+        cut = other_cut;
+      }
     }
-    later -= tail;
+    double later = __shfl_down(tail, 1, 64);
+    if (lane == 63) later = 0.0;
+    if (__shfl_down(cut, 1, 64) == 0 || lane == 63) later += all;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       const int t = first + EACH * lane + i;
-      if (t < last) a.dg[row0 + t] = t < end ? static_cast<float>(sum[i] + later + all) : 0.0f;
+      if (t < last) a.dg[row0 + t] = t < end ? static_cast<float>(cuts[i] ? sum[i] : sum[i] + later) : 0.0f;
     }
   }
   // ---- tokens past the end of the sequence
