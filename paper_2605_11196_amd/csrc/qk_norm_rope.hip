@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a, int heads_ea
   constexpr int G = kLanes<D>, TOK = kThreads / G;
   const int lane = threadIdx.x % G;
   const bool active = 8 * lane < D;
-  const long long n = static_cast<long long>(blockIdx.x) * TOK + threadIdx.x / G;
+  const long long n = (static_cast<long long>(blockIdx.z) * gridDim.x + blockIdx.x) * TOK + threadIdx.x / G;
   if (n >= static_cast<long long>(a.B) * a.T) return;
   const int b = static_cast<int>(n / a.T), t = static_cast<int>(n % a.T);
   Lane<D, INTER> l;
@@ -245,7 +245,10 @@ hipError_t launch(const NormArgs& a, bool backward, hipStream_t stream) {
     int each = (heads + split - 1) / split;
     split = (heads + each - 1) / each;
     void* params[] = {&args, &each};
-    return hipLaunchKernel(reinterpret_cast<const void*>(&norm_kernel<D, IO, INTER>), dim3(tiles, split), dim3(kThreads), params, 0, stream);
+    // a dimension of a launch holds less than 2^32 work-items, and the runtime does not check it
+    constexpr int kMost = 1 << 23;
+    const dim3 grid(tiles < kMost ? tiles : kMost, split, (tiles + kMost - 1) / kMost);
+    return hipLaunchKernel(reinterpret_cast<const void*>(&norm_kernel<D, IO, INTER>), grid, dim3(kThreads), params, 0, stream);
   }
   int parts = tiles < kNormPartials ? tiles : kNormPartials, n_tiles = tiles;
   void* params[] = {&args, &n_tiles};
