@@ -73,6 +73,10 @@ bool tokens_apart(const vla::Rows& r, long long T, long long d) { return T <= 1 
 // the kernels address the rows of a block of 32 tokens with 31-bit byte offsets
 bool rows_near(const vla::Rows& r, size_t es) { return r.t < 0x7fffffffLL / 32 / static_cast<long long>(es); }
 
+// A launch holds less than 2^32 work-items; the runtime wraps a larger grid without an error.
+constexpr long long kMostItems = 0xffffffffLL;
+bool fits_launch(long long groups, long long threads) { return groups <= kMostItems / threads; }
+
 int launched(hipError_t err) {
   if (err == hipSuccess) return VLA_OK;
   fprintf(stderr, "libvla: kernel launch failed: %s (%d)\n", hipGetErrorString(err), static_cast<int>(err));
@@ -86,8 +90,9 @@ int check_delta(int B, int H_k, int H_v, int T, int d_k, int d_v, int io_dtype, 
   if (io_dtype != VLA_F32 && io_dtype != VLA_BF16) return VLA_ERR_INVALID_ARG;
   if (!(fabsf(o.scale) <= 3.4e38f) || o.segments < 0) return VLA_ERR_INVALID_ARG;
   if (!vla::layer_head_size(d_k) || !vla::layer_head_size(d_v)) return VLA_ERR_UNSUPPORTED;
-  // workgroups (up to 32 a head and segment) and tokens with a block of look-ahead are 32-bit indices
+  // workgroups (up to 32 a head and segment) and tokens with a block of look-ahead are 32-bit indices; a workgroup has a wave for 16 columns
   if (static_cast<long long>(B) * H_v > 0x7fffffff / 32 || T > 0x7fffff00) return VLA_ERR_UNSUPPORTED;
+  if (!fits_launch(static_cast<long long>(B) * H_v, 4 * d_v)) return VLA_ERR_UNSUPPORTED;
   return VLA_OK;
 }
 vla_delta_opts delta_opts(const vla_delta_opts* o, int d_k) {
@@ -163,7 +168,8 @@ Segments delta_segments(long long heads, int T, int d_k, int d_v, int io_dtype, 
   }
   if (n > blocks) n = blocks;
   if (n > 256) n = 256;
-  if (n > 0x7fffffff / heads) n = 0x7fffffff / heads;   // workgroups
+  if (n > kMostItems / (heads * 4 * (d_v + d_k))) n = kMostItems / (heads * 4 * (d_v + d_k));   // work-items of the maps
+  if (!fits_launch(heads * (d_v / 16), 4 * d_k)) n = 1;                                         // of the states between segments
   if (n <= 1) return s;
   const int each = static_cast<int>((blocks + n - 1) / n);
   s.n = (blocks + each - 1) / each;
@@ -294,8 +300,9 @@ int vla_delta_forward(const void* q, const void* k, const void* v, const float* 
     a.kept = static_cast<float*>(op.saved);
     a.rows = reinterpret_cast<float*>(static_cast<char*>(op.saved) + kept_bytes(static_cast<long long>(B) * H_v, T, d_k, d_v));
   }
-  if (T < 16 && op.saved == nullptr) return launched(vla::launch_delta_step(a, d_k, d_v, io_dtype, s));
-  Segments seg = delta_segments(static_cast<long long>(B) * H_v, T, d_k, d_v, io_dtype, op.segments);
+  const long long heads = static_cast<long long>(B) * H_v;
+  if (T < 16 && op.saved == nullptr && fits_launch(heads * (d_v / 16), 256)) return launched(vla::launch_delta_step(a, d_k, d_v, io_dtype, s));
+  Segments seg = delta_segments(heads, T, d_k, d_v, io_dtype, op.segments);
   if (seg.n == 1 || workspace == nullptr || workspace_bytes < seg.bytes) return launched(launch_blocks(a, d_k, d_v, io_dtype, false, s));
   a.n_seg = seg.n;
   a.seg_tokens = seg.tokens;
@@ -346,7 +353,7 @@ int vla_delta_backward(const void* q, const void* k, const void* v, const float*
     if (!rows_near(*r, es)) return VLA_ERR_UNSUPPORTED;
   }
   const long long heads = static_cast<long long>(B) * H_v;
-  if (heads * kept_states(T) > 0x7fffffffLL) return VLA_ERR_UNSUPPORTED;   // workgroups
+  if (!fits_launch(heads * kept_states(T), 4 * d_k)) return VLA_ERR_UNSUPPORTED;
   const BackwardParts parts = backward_parts(heads, T, d_k, d_v, io_dtype, H_v != H_k, op.segments);
   const size_t nS = static_cast<size_t>(heads) * d_v * d_k * 4, nG = static_cast<size_t>(heads) * T * 4;
   const size_t saved = vla_delta_saved_bytes(B, H_v, T, d_k, d_v, io_dtype);

@@ -117,7 +117,8 @@ def _key(q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, inter
 def _call(torch, key, q, k, q_weight, k_weight, cos, sin, positions, offset, eps, norm, interleaved):
     """What both directions share: the tensors as the kernels take them, which have to live until the call, and the options."""
     given = q, k, q_weight, k_weight, cos, sin, positions
-    _fits("offset", offset)
+    if not 0 <= offset < 2 ** 31:
+        _fits("offset", offset)
     plan = _plans.get(key)
     if plan is not None and not (q.data_ptr() | k.data_ptr() | (_p(q_weight) or 0) | (_p(k_weight) or 0) | (_p(cos) or 0) | (_p(sin) or 0)) & 15:
         op = VlaNormOpts.from_buffer_copy(plan)
