@@ -234,7 +234,8 @@ int vla_resolve_mode(int B, int H, int T, int d_k, int d_v, int io_dtype, const 
  * The gated delta rule (the sister recurrence: the same residual write on a state of the same layout, a decay and a write
  * strength in place of A) and the norm of queries and keys with the position rotation (what comes before either
  * recurrence).  The rules above hold for them: device pointers, nothing allocated or kept, asynchronous on `stream`, all
- * validation on the host before anything is launched, no written buffer overlapping another one of the call.
+ * validation on the host before anything is launched, no written buffer overlapping another one of the call (by the range of addresses
+ * that its strides span: slices of one buffer that alternate in memory are refused as outputs).
  */
 
 /* Element strides of a [B, H, T, d] (gates: [B, H, T]) tensor.  All zero: contiguous.  The last dimension of d elements is always
@@ -254,10 +255,11 @@ typedef struct vla_delta_opts {
   vla_strides q, k, v, o, g, beta; /* [contiguous]; dO of the backward pass has the strides of o */
   vla_strides dq, dk, dv;          /* [contiguous] of the backward pass's outputs; dg and dbeta are contiguous */
   void* saved;        /* [NULL = not wanted] device, vla_delta_saved_bytes(): what vla_delta_forward keeps for vla_delta_backward
-                         (the states that blocks of tokens start from); written by the first, read by the second */
+                         (the state at every 256th token, and d_v float32 numbers for every token and value head); written by the first, read by
+                         the second */
   size_t saved_bytes;
-  int segments;       /* [0 = the library chooses] time segments that vla_delta_forward cuts long sequences of few heads into (1: none).
-                         Sizes the workspace, so pass the same value to vla_delta_workspace_bytes() */
+  int segments;       /* [0 = the library chooses] time segments that vla_delta_forward and vla_delta_backward cut long sequences of few heads
+                         into (1: none; each call by itself).  Sizes the workspace, so pass the same value to vla_delta_workspace_bytes() */
 } vla_delta_opts;
 
 void vla_delta_default_opts(vla_delta_opts* opts);
@@ -301,7 +303,7 @@ int vla_delta_decode_step(const void* q, const void* k, const void* v, const flo
  *   dO      [B, H_v, T, d_v] io_dtype;  dS_T [B, H_v, d_v, d_k] float32 or NULL (zero)
  *   dq, dk  [B, H_k, T, d_k] io_dtype, summed over the value heads that share a key head, in a fixed order
  *   dv      [B, H_v, T, d_v] io_dtype;  dg, dbeta [B, H_v, T] float32;  dS0 [B, H_v, d_v, d_k] float32 or NULL (not wanted)
- * The same inputs and saved states give the same bits.  dg is the sum of the differences dO_i . O_i - v_i . dV_i over up to 256 tokens and of
+ * The same inputs and saved states give the same bits.  dq, dk and dv are rounded to io_dtype once (bf16: dk from 16 bits of each factor).  dg is the sum of the differences dO_i . O_i - v_i . dV_i over up to 256 tokens and of
  * <dS, S> behind them, and exact to float32's rounding of these terms: where strong decays make it far smaller than they are, what is
  * left of their rounding (1e-7 of them) shows.  A decay that is 0 in float32 (g < -104) ends the sums: its dg is 0, and nothing behind it
  * counts for the tokens before it.

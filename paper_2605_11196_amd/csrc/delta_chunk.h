@@ -4,9 +4,10 @@
 // A wave has 16 rows of S; the waves of a head share the matrices between tokens, which different waves form at once, beside the products
 // of K and Q with the state.  Three barriers a block: rows staged; matrices ready; rows no longer needed.
 //
-// Bound by the matrix and the vector unit together (56 and 51 % of the SIMD cycles; two workgroups of eight waves a compute unit, 128
-// registers): 512 heads of 128, 8192 tokens, bf16 1.72 ms = 2.5 TB/s of q, k, v and o. A workgroup alone takes 3.6 us a block, which is what
-// few heads see: the substitution (700 cycles) and the solution, a chain of some ten dependent products and splits (3000 cycles).
+// 512 heads of 128, 8192 tokens, bf16 1.72 ms = 2.5 TB/s of q, k, v and o, two workgroups of eight waves a compute unit (128 registers).  Neither unit is full: the
+// matrix unit is busy for 56 % of the SIMD cycles and other vector instructions take 51 %, which can overlap; a quarter of the matrix instructions
+// form residuals of the three terms.  A workgroup alone takes 3.6 us a block, two 6.7, and few heads see the first: the substitution (700 cycles) and
+// the solution, a chain of some ten dependent products and splits (3000 cycles).
 //
 // MAP: the affine map of a segment instead of its outputs, S_end = S_start X + Y: Y from d_v columns that start from zero, X from d_k
 // columns without values that start from the identity.  The first segment needs no map: where that shortens the way (first_done), a

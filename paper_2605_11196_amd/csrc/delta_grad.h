@@ -13,7 +13,7 @@
 // A sweep along the tokens carries S (everything but the last term of dK), a sweep back carries dS.  Here a wave has 16 columns of what has
 // d_k columns, so that the products over d_v stay in it; states are tiles with d_v along the rows, left operands the rows of dO, R and W in
 // LDS.  Twice the forward kernel's products; bound by memory and the waits for it, since both sweeps read K, Q, dO, R and W
-// (64 heads of 128, 4096 tokens, bf16: 396 us, 1.6 GB).  Nothing is added atomically.
+// (64 heads of 128, 4096 tokens, bf16: 396 us, 1.5 GB, the waves wait 54 % of their cycles).  Nothing is added atomically.
 #pragma once
 
 #include "delta_block.h"
@@ -29,7 +29,9 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
   constexpr int PK = DK / O::PER16, PV = DV / O::PER16;
   using RK = PieceRows<DKP / O::PER16>;
   using RV = PieceRows<DVP / O::PER16>;
-  constexpr int TR = O::TERMS, TW = O::TERMS > 1 ? 2 : 1;      // terms of R and of W
+  // Terms of R and of W.  W enters dK alone (dbeta and v . dV read it from memory), so 16 bits of it: the third term's 8 KB at d_v = 128 would leave one
+  // workgroup on a compute unit instead of two.
+  constexpr int TR = O::TERMS, TW = O::TERMS > 1 ? 2 : 1;
   __shared__ u4 sK[kTok * RK::STRIDE], sQ[kTok * RK::STRIDE], sD[kTok * RV::STRIDE], sR[TR * kTok * RV::STRIDE], sW[TW * kTok * RV::STRIDE];
   __shared__ typename O::Image X[3];                 // tiles (0,0), (1,0), (1,1)
   __shared__ typename O::ImageOut Xt[3], Z[4];       // X^T: (0,0), (0,1), (1,1);  Y + Y^T: (0,0), (0,1), (1,0), (1,1)
@@ -279,7 +281,8 @@ __global__ void __launch_bounds__(4 * DK, 4) delta_grad_kernel(DeltaArgs a) {
     }
   }
 
-  // ---- back along the tokens with the state's gradient
+  // ---- back along the tokens with the state's gradient, from the kept one at their end.  What is carried over up to eight blocks is for dK alone, so its
+  // updates are formed from 16 bits of their factors as well (of each 2^-17, against the 2^-9 that dK is rounded to).
   {
     f4 dS[VT];
     load_state(a.kept + (static_cast<size_t>(head) * segs + seg) * DV * DK, dS);

@@ -22,7 +22,8 @@ bool overlap(const Range& a, const Range& b) {
   const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
   return a0 < b0 + b.bytes && b0 < a0 + a.bytes;
 }
-// No written buffer may overlap another buffer of the call; `same` is the one pair that may be the same buffer.
+// No written buffer may overlap another buffer of the call, by the range of addresses that its strides span: slices of one buffer are refused
+// also where their rows alternate.  `same` is the one pair that may be the same buffer.
 bool disjoint(const Range* r, int n, const void* same0, const void* same1) {
   for (int i = 0; i < n; ++i) {
     if (!r[i].written) continue;
@@ -36,7 +37,7 @@ bool disjoint(const Range* r, int n, const void* same0, const void* same1) {
 }
 
 // The strides of a call, the contiguous ones where none are given.  False where one is negative or not a whole number of
-// 16-byte pieces, or where a written tensor's would make two of its rows the same.
+// 16-byte pieces.  (Whether rows lie in each other: rows_apart, tokens_apart.)
 bool rows_of(const vla_strides& s, long long H, long long T, long long d, int per16, vla::Rows* out) {
   *out = vla::Rows{s.b, s.h, s.t};
   if (s.b == 0 && s.h == 0 && s.t == 0) *out = vla::Rows{H * T * d, T * d, d};
@@ -117,7 +118,9 @@ bool gate_rows(const vla_strides& s, long long H, long long T, vla::Rows* out) {
 // The number of segments, of 1, 2, 3, 4, 6, 8 ... blocks or as many as the card holds, is the one of least time by a model that is fitted to measurements
 // of 1 to 33 segments for 4 to 256 heads of 16 to 128 columns and 192 to 4096 tokens (microseconds): a block by the rounds in which its waves
 // form the six matrices between tokens and by its products; a map by its waves; a step from one segment to the next d_k / 60; d_k / 8 for the
-// launches.  Its choices are up to 10 % behind the best one (128 heads of 64 x 128, float32, 512 tokens: 102, 93).
+// launches.  Against the best of up to 12 other numbers at 150 points (profiles/gated_delta_segments.txt) its choices take 1 % more in the geometric mean
+// and 4.5 % or less at nine in ten; at worst 19 % (16 heads of 32, float32, 4096 tokens: 73, 62 with 32 segments) and 15 % (256 heads of 128 x 64, bf16,
+// 4096 tokens: 709, 614 with 3).  With the backward pass, whose chain is cut alike: 0.2 %, 1.5 %, 11 %.
 // Forward, microseconds, bf16 but where said, 1 segment and the rule's:
 //   4 heads of 64: 256 tokens 27, 22 (8 segments); 1024 tokens 94, 34 (16).  The same in float32 41, 24 and 151, 41
 //   4 heads of 128: 256 tokens 36, 36 (none; 4: 38); 384 tokens 51, 43 (6); 1024 tokens 124, 61 (11); 32 heads, 1024 tokens 124, 68 (8)

@@ -54,14 +54,15 @@ struct DeltaArgs {
   int n_kept;
   // backward
   const void* dO;          // strides os
-  void* dv;
-  void* dq;                // share of a value head: [B * H_v][T][d_k] float32 where heads share a key head, else by strides
+  void* dv;                // outputs by strides
+  void* dq;
   void* dk;
   Rows dvs, dqs, dks;
   const float* kept_state; // of the forward pass: kept, rows
   const float* R;
   float* dk_part;          // [B * H_v][T][d_k]: what the sweep along the tokens gives of dk
-  float* dq_part;          // the same of dq, where heads share a key head
+                           // (with dq_part: the whole of it)
+  float* dq_part;          // [B * H_v][T][d_k]: dq of a value head where heads share a key head, or nullptr
   float* dg;               // [B * H_v][T]
   float* dbeta;
   // time segments
