@@ -349,6 +349,135 @@ int vla_qk_norm_rope_backward(const void* q, const void* k, const void* q_weight
                               void* dk_weight, int B, int T, int H_q, int H_k, int d, int io_dtype, const vla_norm_opts* opts,
                               void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * ---- Operators on rows of channels ---------------------------------------------------------------------------
+ *
+ * Tensors [B, T, n]: n channels of T tokens, the rows that a projection gives (the heads of the recurrences above side by side).  Their strides are
+ * a vla_strides whose h is 0; the rules above hold for them (16-byte pieces, written rows apart, all zero: contiguous; read rows may repeat).  n is a multiple
+ * of 8.  `lengths` as in vla_delta_opts: what lies past the end of a sequence is not read, its outputs and gradients are 0.
+ */
+
+typedef struct vla_conv_opts {
+  int silu;            /* [1] 1: y = pre / (1 + exp(-pre)); 0: y = pre */
+  int weight_dtype;    /* [VLA_F32] of weight and bias, and of their gradients */
+  const int* lengths;  /* [NULL = T] device, [B] */
+  vla_strides x, y;    /* [contiguous] of y and of dy */
+  vla_strides dx;      /* [contiguous] */
+} vla_conv_opts;
+void vla_conv_default_opts(vla_conv_opts* opts);
+
+/*
+ * vla_causal_conv -- the short causal convolution of every channel: pre_t = bias + sum_j weight[.,j] x_{t-width+1+j}, j < width.
+ *
+ *   x, y     [B, T, n] io_dtype by strides
+ *   weight   [n, width] weight_dtype, width 2, 3 or 4;  bias [n] or NULL (zero)
+ *   state    [B, width-1, n] io_dtype: the rows before token 0, oldest first, or NULL (zero)
+ *   state_T  the same, written: the rows before the token that comes next; or NULL; may be state itself
+ *
+ * Float32 sums, one rounding.  Running [0, T1) and then [T1, T) with the carried state gives the same bits as one call.
+ */
+int vla_causal_conv(const void* x, const void* weight, const void* bias, const void* state, void* y, void* state_T, int B, int T, int n,
+                    int width, int io_dtype, const vla_conv_opts* opts, void* stream);
+/* One token, x and y [B, n] (strides: b alone); the state moves on in place.  No lengths. */
+int vla_causal_conv_step(const void* x, const void* weight, const void* bias, void* state, void* y, int B, int n, int width, int io_dtype,
+                         const vla_conv_opts* opts, void* stream);
+/* Its gradients, given those of y and state_T (NULL: zero).  dweight, dbias, dstate: NULL if not wanted; the first two are summed in
+ * float32 in a fixed order and need the workspace. */
+size_t vla_causal_conv_workspace_bytes(int B, int T, int n, int width, int io_dtype);
+int vla_causal_conv_backward(const void* x, const void* weight, const void* bias, const void* state, const void* dy, const void* dstate_T,
+                             void* dx, void* dweight, void* dbias, void* dstate, int B, int T, int n, int width, int io_dtype,
+                             const vla_conv_opts* opts, void* workspace, size_t workspace_bytes, void* stream);
+
+typedef struct vla_scan_opts {
+  int softplus;               /* [1] 1: dt = log(1 + exp(delta + delta_bias)); 0: dt = delta + delta_bias */
+  int groups;                 /* [1] of channels that share B and C: n / groups neighbouring ones, a multiple of 8 */
+  const int* lengths;         /* [NULL = T] device, [B] */
+  vla_strides u, delta, z, y; /* [contiguous] of y and of dy */
+  vla_strides B, C;           /* [contiguous [B, T, groups, N]]; h: from group to group */
+  vla_strides du, ddelta, dz; /* [contiguous]; the gradients of B and C are contiguous [B, T, groups, N] */
+  void* saved;                /* [NULL = not wanted] device, vla_selective_scan_saved_bytes(): the state at every 8th token, written by
+                                 vla_selective_scan, read by vla_selective_scan_backward */
+  size_t saved_bytes;
+  int segments;               /* [0 = the library chooses] time segments that long sequences of few channels are cut into (1: none).  Sizes the
+                                 workspace, so pass the same value to vla_selective_scan_workspace_bytes() */
+} vla_scan_opts;
+void vla_scan_default_opts(vla_scan_opts* opts);
+
+/* Bytes of workspace of vla_selective_scan (backward: of vla_selective_scan_backward); 0 when it wants none and when the arguments are
+ * invalid.  A forward call with a smaller one, or none, runs every sequence from its start to its end; a backward call returns
+ * VLA_ERR_WORKSPACE. */
+size_t vla_selective_scan_workspace_bytes(int B, int T, int n, int N, int io_dtype, const vla_scan_opts* opts, int backward);
+/* Bytes of opts->saved. */
+size_t vla_selective_scan_saved_bytes(int B, int T, int n, int N, int io_dtype, const vla_scan_opts* opts);
+
+/*
+ * vla_selective_scan -- the selective state space scan.  For every batch row, channel c with its group, and state s, from h = h0:
+ *
+ *     h_t[c,s] = exp(dt_t[c] A[c,s]) h_{t-1}[c,s] + dt_t[c] u_t[c] Bm_t[s];   y_t[c] = (sum_s Cm_t[s] h_t[c,s] + D[c] u_t[c]) z_t[c] sigmoid(z_t[c])
+ *
+ *   u, delta, z, y  [B, T, n]         io_dtype by strides; z NULL: no gate
+ *   Bm, Cm          [B, T, groups, N] io_dtype by strides
+ *   A               [n, N]            float32 (finite; negative for a state that decays);  D, delta_bias [n] float32 or NULL (zero)
+ *   h0, h_T         [B, n, N]         float32; h0 NULL: zero; h_T written, or NULL; may be h0 itself
+ *   N in {8, 16, 32, 64};  T >= 0 (T == 0 copies h0 to h_T)
+ *
+ * Float32 arithmetic and states; one rounding, to io_dtype.  Running [0, T1) and then [T1, T) with the carried h_T gives the same
+ * result as one call up to rounding.
+ */
+int vla_selective_scan(const void* u, const void* delta, const float* A, const void* Bm, const void* Cm, const float* D, const void* z,
+                       const float* delta_bias, const float* h0, void* y, float* h_T, int B, int T, int n, int N, int io_dtype,
+                       const vla_scan_opts* opts, void* workspace, size_t workspace_bytes, void* stream);
+/* One token, u, delta, z, y [B, n], Bm, Cm [B, groups, N]; h [B, n, N] is updated in place.  No lengths. */
+int vla_selective_scan_step(const void* u, const void* delta, const float* A, const void* Bm, const void* Cm, const float* D, const void* z,
+                            const float* delta_bias, float* h, void* y, int B, int n, int N, int io_dtype, const vla_scan_opts* opts,
+                            void* stream);
+/*
+ * vla_selective_scan_backward -- the gradients of its inputs, given those of y and h_T (NULL: zero) and what it saved.  du, ddelta, dz
+ * (NULL without z), dBm, dCm: io_dtype, each rounded once; dA, dD, ddelta_bias, dh0: float32, the last three NULL if not wanted.  The sums over
+ * tokens, channels and sequences are float32 in a fixed order: the same inputs give the same bits.
+ */
+int vla_selective_scan_backward(const void* u, const void* delta, const float* A, const void* Bm, const void* Cm, const float* D, const void* z,
+                                const float* delta_bias, const void* dy, const float* dh_T, void* du, void* ddelta, float* dA, void* dBm,
+                                void* dCm, float* dD, void* dz, float* ddelta_bias, float* dh0, int B, int T, int n, int N, int io_dtype,
+                                const vla_scan_opts* opts, void* workspace, size_t workspace_bytes, void* stream);
+
+typedef struct vla_residual_opts {
+  float eps;              /* [1e-6] of both norms */
+  int group;              /* [0 = n] columns of a group of the norm of y (a head), a multiple of 8 that divides n */
+  int activation;         /* [0] of the gate: 0: g / (1 + exp(-g)); 1: 1 / (1 + exp(-g)) */
+  int stream_dtype;       /* [VLA_F32] of x, s and their gradients: VLA_F32 or io_dtype */
+  int weight_dtype;       /* [VLA_F32] of post_weight, scale, weight and their gradients */
+  vla_strides x, y, gate; /* [contiguous] */
+  vla_strides s, h;       /* [contiguous] of the outputs and of their gradients */
+  vla_strides dx, dy, dgate;
+} vla_residual_opts;
+void vla_residual_default_opts(vla_residual_opts* opts);
+
+/*
+ * vla_residual_norm -- what stands between a block and the next one:
+ *
+ *     s = x + scale * act(gate) * post_weight * N(y);   h = weight * N(s);   N(v) = v / sqrt(mean v^2 + eps)
+ *
+ * with the mean over a group of columns of y, and over the row of s.
+ *
+ *   x                   [B, T, n] stream_dtype: the residual stream, or NULL (zero)
+ *   y                   [B, T, n] io_dtype: the block's output, or NULL: h = weight * N(x) alone (then s, gate, post_weight and scale are NULL)
+ *   gate                [B, T, n] io_dtype or NULL (no gate);  scale [n] or NULL (ones);  post_weight [n] or NULL: y without a norm
+ *   s                   [B, T, n] stream_dtype, written; may be x itself (the same strides)
+ *   weight, h           [n], [B, T, n] io_dtype, written; both NULL: no second norm
+ *
+ * Float32 arithmetic; h comes from s before its rounding.  n <= 8192.
+ */
+int vla_residual_norm(const void* x, const void* y, const void* gate, const void* post_weight, const void* scale, const void* weight, void* s,
+                      void* h, int B, int T, int n, int io_dtype, const vla_residual_opts* opts, void* stream);
+/* Its gradients, given those of s (of x, where y is NULL) and h (NULL: zero); each NULL if not wanted.  Those of the weights are summed over the rows
+ * in float32 in a fixed order and need the workspace. */
+size_t vla_residual_norm_workspace_bytes(int n);
+int vla_residual_norm_backward(const void* x, const void* y, const void* gate, const void* post_weight, const void* scale, const void* weight,
+                               const void* ds, const void* dh, void* dx, void* dy, void* dgate, void* dpost_weight, void* dscale, void* dweight,
+                               int B, int T, int n, int io_dtype, const vla_residual_opts* opts, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,5 +1,6 @@
 """MI355X-native Variational Linear Attention forward, and the gated delta rule and the norm of queries and keys with the
-position rotation next to it (thin binding over libvla.so)."""
+position rotation, the selective state space scan with its short causal convolution, and the norms around a block next to it
+(thin binding over libvla.so)."""
 from .binding import (  # noqa: F401
     VLA_BF16,
     VLA_F32,
@@ -21,6 +22,7 @@ from .binding import (  # noqa: F401
     vla_forward_static_raw,
     vla_forward_workspace_bytes,
 )
+from .causal_conv import causal_conv, causal_conv_backward, causal_conv_step  # noqa: F401
 from .gated_delta import (  # noqa: F401
     gated_delta,
     gated_delta_backward,
@@ -28,3 +30,10 @@ from .gated_delta import (  # noqa: F401
     gated_delta_forward,
 )
 from .qk_norm import qk_norm_rope, qk_norm_rope_backward  # noqa: F401
+from .residual_norm import residual_norm, residual_norm_backward  # noqa: F401
+from .selective_scan import (  # noqa: F401
+    selective_scan,
+    selective_scan_backward,
+    selective_scan_forward,
+    selective_scan_step,
+)

@@ -18,7 +18,11 @@ EXPORTS = ("vla_default_opts", "vla_forward_workspace_bytes", "vla_forward", "vl
            "vla_decode_step", "vla_status_string", "vla_version", "vla_resolve_mode", "vla_delta_default_opts",
            "vla_delta_workspace_bytes", "vla_delta_saved_bytes", "vla_delta_forward", "vla_delta_decode_step",
            "vla_delta_backward", "vla_norm_default_opts", "vla_qk_norm_rope", "vla_qk_norm_rope_workspace_bytes",
-           "vla_qk_norm_rope_backward")
+           "vla_qk_norm_rope_backward", "vla_conv_default_opts", "vla_causal_conv", "vla_causal_conv_step",
+           "vla_causal_conv_workspace_bytes", "vla_causal_conv_backward", "vla_scan_default_opts",
+           "vla_selective_scan_workspace_bytes", "vla_selective_scan_saved_bytes", "vla_selective_scan", "vla_selective_scan_step",
+           "vla_selective_scan_backward", "vla_residual_default_opts", "vla_residual_norm", "vla_residual_norm_workspace_bytes",
+           "vla_residual_norm_backward")
 
 
 class VlaError(RuntimeError):
@@ -49,6 +53,22 @@ class VlaNormOpts(ctypes.Structure):
     _fields_ = ([("eps", ctypes.c_float)]
                 + [(n, ctypes.c_int) for n in ("l2", "interleaved", "rot", "places", "offset", "weight_dtype")]
                 + [("positions", ctypes.c_void_p)] + [(n, VlaStrides) for n in ("q", "k", "q_out", "k_out", "dq", "dk")])
+
+
+class VlaConvOpts(ctypes.Structure):
+    _fields_ = ([("silu", ctypes.c_int), ("weight_dtype", ctypes.c_int), ("lengths", ctypes.c_void_p)]
+                + [(n, VlaStrides) for n in ("x", "y", "dx")])
+
+
+class VlaScanOpts(ctypes.Structure):
+    _fields_ = ([("softplus", ctypes.c_int), ("groups", ctypes.c_int), ("lengths", ctypes.c_void_p)]
+                + [(n, VlaStrides) for n in ("u", "delta", "z", "y", "B", "C", "du", "ddelta", "dz")]
+                + [("saved", ctypes.c_void_p), ("saved_bytes", ctypes.c_size_t), ("segments", ctypes.c_int)])
+
+
+class VlaResidualOpts(ctypes.Structure):
+    _fields_ = ([("eps", ctypes.c_float)] + [(n, ctypes.c_int) for n in ("group", "activation", "stream_dtype", "weight_dtype")]
+                + [(n, VlaStrides) for n in ("x", "y", "gate", "s", "h", "dx", "dy", "dgate")])
 
 
 _lib = None
@@ -95,6 +115,7 @@ def load_library():
     lib.vla_resolve_mode.argtypes = [I] * 6 + [OP]
     lib.vla_resolve_mode.restype = I
     DP, NP = ctypes.POINTER(VlaDeltaOpts), ctypes.POINTER(VlaNormOpts)
+    CP, SP, RP = ctypes.POINTER(VlaConvOpts), ctypes.POINTER(VlaScanOpts), ctypes.POINTER(VlaResidualOpts)
     Z = ctypes.c_size_t
     for name, args, result in (
             ("vla_delta_default_opts", [DP], None),
@@ -106,7 +127,22 @@ def load_library():
             ("vla_norm_default_opts", [NP], None),
             ("vla_qk_norm_rope", [P] * 8 + [I] * 6 + [NP, P], I),
             ("vla_qk_norm_rope_workspace_bytes", [I], Z),
-            ("vla_qk_norm_rope_backward", [P] * 12 + [I] * 6 + [NP, P, Z, P], I)):
+            ("vla_qk_norm_rope_backward", [P] * 12 + [I] * 6 + [NP, P, Z, P], I),
+            ("vla_conv_default_opts", [CP], None),
+            ("vla_causal_conv", [P] * 6 + [I] * 5 + [CP, P], I),
+            ("vla_causal_conv_step", [P] * 5 + [I] * 4 + [CP, P], I),
+            ("vla_causal_conv_workspace_bytes", [I] * 5, Z),
+            ("vla_causal_conv_backward", [P] * 10 + [I] * 5 + [CP, P, Z, P], I),
+            ("vla_scan_default_opts", [SP], None),
+            ("vla_selective_scan_workspace_bytes", [I] * 5 + [SP, I], Z),
+            ("vla_selective_scan_saved_bytes", [I] * 5 + [SP], Z),
+            ("vla_selective_scan", [P] * 11 + [I] * 5 + [SP, P, Z, P], I),
+            ("vla_selective_scan_step", [P] * 10 + [I] * 4 + [SP, P], I),
+            ("vla_selective_scan_backward", [P] * 19 + [I] * 5 + [SP, P, Z, P], I),
+            ("vla_residual_default_opts", [RP], None),
+            ("vla_residual_norm", [P] * 8 + [I] * 4 + [RP, P], I),
+            ("vla_residual_norm_workspace_bytes", [I], Z),
+            ("vla_residual_norm_backward", [P] * 14 + [I] * 4 + [RP, P, Z, P], I)):
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = result
     defaults = VlaOpts()

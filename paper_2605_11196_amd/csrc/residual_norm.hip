@@ -1,0 +1,295 @@
+// The norms around a block with its gate and its residual: what follows a block and what precedes the next one, in one pass over a row.
+//
+//   t = N(y) w1 act(gate) k,  N(y) = y r1, r1 = 1 / sqrt(mean y^2 + eps) over each group of columns;  s = x + t;
+//   h = s r2 w2, r2 = 1 / sqrt(mean s^2 + eps) over the row;  any of x, w1 (with N), gate, k, w2 (with h) may be missing
+//   backward: d = ds + r2 (dh w2 - s r2^2 mean(dh w2 s)) = dx;  c = d k act w1;  dy = r1 (c - N(y) mean(c N(y)));
+//   dgate = d k N(y) w1 act'(gate);  dw1 = sum d k act N(y), dk = sum d act w1 N(y), dw2 = sum dh s r2 over the rows
+//
+// Bound by memory: every operand is read once and every result written once (the backward pass forms t, s and the two norms again from x,
+// y and gate, which it has to read anyway; s is float32 in both).  A row lies on L lanes, from 8 to 1024, with eight neighbouring columns each; a workgroup
+// goes through rows with the weights, and in the backward pass their gradients, on registers.  Sums go through DPP and lane swaps, and over the waves
+// of a row through LDS.
+#include "mixer_util.h"
+
+namespace vla {
+namespace {
+
+constexpr int kColumns = 8;   // of a lane, together
+
+struct Eight {
+  float v[kColumns];
+  __device__ __forceinline__ float& operator[](int i) { return v[i]; }
+  __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+};
+template <typename IO>
+__device__ __forceinline__ Eight load8(const IO* p) {
+  Eight e;
+  constexpr int V = kPiece<IO>;
+#pragma unroll
+  for (int i = 0; i < kColumns; i += V) {
+    const Piece<IO> x = load_piece(p + i);
+#pragma unroll
+    for (int j = 0; j < V; ++j) e[i + j] = x[j];
+  }
+  return e;
+}
+__device__ __forceinline__ Eight weight8(const void* w, int bf16, int c) {
+  return bf16 ? load8(static_cast<const uint16_t*>(w) + c) : load8(static_cast<const float*>(w) + c);
+}
+template <typename IO> __device__ __forceinline__ void store8(IO* p, const Eight& e) { store_piece(p, e.v); }
+
+// Where a lane is in its workgroup, and the sums over its row and over its group of columns.
+struct RowLanes {
+  int L, lane, row, rows, pieces, each;   // lanes of a row, this one's place, its row among the workgroup's; eights of a row and of a group
+  float* whole;                           // LDS: [4][2][16]
+  float* parts;                           // LDS: [2][threads]
+  bool here, split;                       // columns of the row; whether the sums over groups go through LDS
+
+  __device__ __forceinline__ RowLanes(const ResidualArgs& a, int lanes, float* lds) {
+    L = lanes;
+    lane = threadIdx.x % L;
+    row = threadIdx.x / L;
+    rows = blockDim.x / L;
+    pieces = a.n / kColumns;
+    each = a.group / kColumns;
+    whole = lds;
+    parts = lds + 4 * 2 * 16;
+    here = lane < pieces;
+    split = each != pieces && ((each & (each - 1)) != 0 || each > 64);
+  }
+  // a, b summed over the row, in every lane of it.  `at`: a place in LDS; between two visits of one place lies the barrier of another
+  __device__ __forceinline__ void row_sums(float& a, float& b, int at) const {
+    a = group_sum(a, L < 64 ? L : 64);
+    b = group_sum(b, L < 64 ? L : 64);
+    if (L <= 64) return;
+    const int waves = L / 64, wave = threadIdx.x / 64;
+    float* slot = whole + at * 2 * 16;
+    if ((threadIdx.x & 63) == 0) {
+      slot[wave] = a;
+      slot[16 + wave] = b;
+    }
+    __syncthreads();
+    const int first = wave / waves * waves;
+    a = b = 0.0f;
+    for (int w = first; w < first + waves; ++w) {
+      a += slot[w];
+      b += slot[16 + w];
+    }
+  }
+  // a summed over the lane's group
+  __device__ __forceinline__ float group_total(float a, int at) const {
+    if (each == pieces) {
+      float none = 0.0f;
+      row_sums(a, none, at);
+      return a;
+    }
+    if (!split) return group_sum(a, each);
+    float* slot = parts + (at & 1) * blockDim.x + row * L;
+    slot[lane] = a;
+    __syncthreads();
+    const int first = lane / each * each;
+    float sum = 0.0f;
+    for (int i = 0; i < each && first + i < L; ++i) sum += slot[first + i];
+    return sum;
+  }
+};
+
+// act(g), and with slope also its derivative
+__device__ __forceinline__ float activation(int act, float g) {
+  const float s = sigmoid(g);
+  return act == 0 ? g * s : s;
+}
+__device__ __forceinline__ float slope(int act, float g) {
+  const float s = sigmoid(g);
+  return act == 0 ? s * fmaf(g, 1.0f - s, 1.0f) : s * (1.0f - s);
+}
+
+template <typename T>
+__device__ __forceinline__ Eight row8(const void* p, Row2 step, long long b, long long t, int c) {
+  return load8(static_cast<const T*>(p) + b * step.b + t * step.t + c);
+}
+template <typename T>
+__device__ __forceinline__ void row8_store(void* p, Row2 step, long long b, long long t, int c, const Eight& e) {
+  store8(static_cast<T*>(p) + b * step.b + t * step.t + c, e);
+}
+
+template <typename IO, typename ST>
+__global__ void __launch_bounds__(1024) residual_kernel(ResidualArgs a, int L) {
+  extern __shared__ float lds[];
+  const RowLanes r(a, L, lds);
+  const long long total = static_cast<long long>(a.B) * a.T;
+  const int c = r.here ? kColumns * r.lane : 0;
+  Eight w1{}, k{}, w2{};
+  if (a.post_weight != nullptr) w1 = weight8(a.post_weight, a.w_bf16, c);
+  if (a.scale != nullptr) k = weight8(a.scale, a.w_bf16, c);
+  if (a.weight != nullptr) w2 = weight8(a.weight, a.w_bf16, c);
+  int turn = 0;
+  for (long long first = static_cast<long long>(blockIdx.x) * r.rows; first < total; first += static_cast<long long>(gridDim.x) * r.rows) {
+    const long long n = first + r.row;
+    const bool live = n < total && r.here;
+    const long long b = n < total ? n / a.T : 0, t = n < total ? n % a.T : 0;
+    Eight s{}, x{}, g{};
+    if (live) {
+      if (a.y != nullptr) s = row8<IO>(a.y, a.ys, b, t, c);
+      if (a.x != nullptr) x = row8<ST>(a.x, a.xs, b, t, c);
+      if (a.gate != nullptr) g = row8<IO>(a.gate, a.gs, b, t, c);
+    }
+    if (a.post_weight != nullptr) {
+      float sq = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kColumns; ++i) sq = fmaf(s[i], s[i], sq);
+      const float r1 = rsqrtf(fmaf(r.group_total(sq, turn), 1.0f / a.group, a.eps));
+#pragma unroll
+      for (int i = 0; i < kColumns; ++i) s[i] *= r1 * w1[i];
+    }
+    float sum = 0.0f, none = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kColumns; ++i) {
+      if (a.gate != nullptr) s[i] *= activation(a.act, g[i]);
+      if (a.scale != nullptr) s[i] *= k[i];
+      s[i] += x[i];
+      sum = fmaf(s[i], s[i], sum);
+    }
+    if (live && a.s != nullptr) row8_store<ST>(a.s, a.ss, b, t, c, s);
+    if (a.weight != nullptr) {
+      r.row_sums(sum, none, 2 + turn);
+      const float r2 = rsqrtf(fmaf(sum, 1.0f / a.n, a.eps));
+#pragma unroll
+      for (int i = 0; i < kColumns; ++i) s[i] *= r2 * w2[i];
+      if (live) row8_store<IO>(a.h, a.hs, b, t, c, s);
+    }
+    turn ^= 1;
+  }
+}
+
+template <typename IO, typename ST>
+__global__ void __launch_bounds__(1024) residual_backward_kernel(ResidualArgs a, int L) {
+  extern __shared__ float lds[];
+  const RowLanes r(a, L, lds);
+  const long long total = static_cast<long long>(a.B) * a.T;
+  const float inv_n = 1.0f / a.n, inv_group = 1.0f / a.group;
+  const int c = r.here ? kColumns * r.lane : 0;
+  Eight w1{{1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f}}, k = w1, w2{}, dw1{}, dk{}, dw2{};
+  if (a.post_weight != nullptr) w1 = weight8(a.post_weight, a.w_bf16, c);
+  if (a.scale != nullptr) k = weight8(a.scale, a.w_bf16, c);
+  if (a.weight != nullptr) w2 = weight8(a.weight, a.w_bf16, c);
+  int turn = 0;
+  for (long long first = static_cast<long long>(blockIdx.x) * r.rows; first < total; first += static_cast<long long>(gridDim.x) * r.rows) {
+    const long long n = first + r.row;
+    const bool live = n < total && r.here;
+    const long long b = n < total ? n / a.T : 0, t = n < total ? n % a.T : 0;
+    Eight unit{}, s{}, g{}, d{}, dh{};
+    if (live) {
+      if (a.y != nullptr) unit = row8<IO>(a.y, a.ys, b, t, c);
+      if (a.x != nullptr) s = row8<ST>(a.x, a.xs, b, t, c);
+      if (a.gate != nullptr) g = row8<IO>(a.gate, a.gs, b, t, c);
+      if (a.ds != nullptr) d = row8<ST>(a.ds, a.ss, b, t, c);
+      if (a.dh != nullptr) dh = row8<IO>(a.dh, a.hs, b, t, c);
+    }
+    float r1 = 1.0f;
+    if (a.post_weight != nullptr) {
+      float sq = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kColumns; ++i) sq = fmaf(unit[i], unit[i], sq);
+      r1 = rsqrtf(fmaf(r.group_total(sq, 0), inv_group, a.eps));      // the third sum's barrier lies before the next row's
+#pragma unroll
+      for (int i = 0; i < kColumns; ++i) unit[i] *= r1;
+    }
+    if (a.dh != nullptr) {
+      float sq = 0.0f, along = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kColumns; ++i) {
+        float y = unit[i] * w1[i] * k[i];
+        if (a.gate != nullptr) y *= activation(a.act, g[i]);
+        s[i] += y;
+        sq = fmaf(s[i], s[i], sq);
+        along = fmaf(dh[i] * w2[i], s[i], along);
+      }
+      r.row_sums(sq, along, 2 + turn);
+      const float r2 = rsqrtf(fmaf(sq, inv_n, a.eps)), f = along * r2 * r2 * inv_n;
+#pragma unroll
+      for (int i = 0; i < kColumns; ++i) {
+        d[i] = fmaf(r2, fmaf(dh[i], w2[i], -s[i] * f), d[i]);
+        dw2[i] = fmaf(dh[i], s[i] * r2, dw2[i]);
+      }
+    }
+    turn ^= 1;
+    if (live && a.dx != nullptr) row8_store<ST>(a.dx, a.dxs, b, t, c, d);
+    if (a.y == nullptr) continue;
+    // d becomes the gradient of N(y)
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kColumns; ++i) {
+      const float act = a.gate != nullptr ? activation(a.act, g[i]) : 1.0f;
+      const float da = d[i] * act, du = d[i] * unit[i];
+      dk[i] = fmaf(da * w1[i], unit[i], dk[i]);
+      dw1[i] = fmaf(da * k[i], unit[i], dw1[i]);
+      if (a.gate != nullptr) g[i] = du * w1[i] * k[i] * slope(a.act, g[i]);
+      d[i] = da * k[i] * w1[i];
+      m = fmaf(d[i], unit[i], m);
+    }
+    if (live && a.dgate != nullptr) row8_store<IO>(a.dgate, a.dgs, b, t, c, g);
+    const float f = a.post_weight != nullptr ? r.group_total(m, 1) * inv_group : 0.0f;
+#pragma unroll
+    for (int i = 0; i < kColumns; ++i) d[i] = r1 * fmaf(-unit[i], f, d[i]);
+    if (live && a.dy != nullptr) row8_store<IO>(a.dy, a.dys, b, t, c, d);
+  }
+  if (a.sum_part == nullptr) return;
+  // the rows of a workgroup, one after the other
+  float* part = a.sum_part + static_cast<size_t>(blockIdx.x) * 3 * a.n + c;
+  for (int row = 0; row < r.rows; ++row) {
+    if (r.row == row && r.here) {
+      const Eight* all[3] = {&dw2, &dw1, &dk};
+#pragma unroll
+      for (int j = 0; j < 3; ++j) {
+        float* at = part + static_cast<size_t>(j) * a.n;
+        Eight e = *all[j];
+        if (row > 0) {
+          const Eight before = load8(at);
+#pragma unroll
+          for (int i = 0; i < kColumns; ++i) e[i] += before[i];
+        }
+        store8(at, e);
+      }
+    }
+    if (r.rows > 1) __syncthreads();
+  }
+}
+
+// Lanes of a row, and threads of a workgroup.
+int row_width(int n) {
+  int L = 8;
+  while (L * kColumns < n) L *= 2;
+  return L;
+}
+
+template <typename IO, typename ST>
+hipError_t launch(const ResidualArgs& a, bool backward, int* parts, hipStream_t stream) {
+  int L = row_width(a.n);
+  const int threads = L > 256 ? L : 256;
+  const long long rows = static_cast<long long>(a.B) * a.T, groups = (rows + threads / L - 1) / (threads / L);
+  const int most = backward ? kResidualPartials : 2048 * 256 / threads;
+  const int grid = static_cast<int>(groups < most ? groups : most);
+  if (parts != nullptr) *parts = grid;
+  if (grid == 0) return hipSuccess;
+  const void* kernel = backward ? reinterpret_cast<const void*>(&residual_backward_kernel<IO, ST>) : reinterpret_cast<const void*>(&residual_kernel<IO, ST>);
+  ResidualArgs args = a;
+  void* params[] = {&args, &L};
+  return hipLaunchKernel(kernel, dim3(grid), dim3(threads), params, (4 * 2 * 16 + 2 * threads) * sizeof(float), stream);
+}
+hipError_t launch_types(const ResidualArgs& a, int io_dtype, int stream_dtype, bool backward, int* parts, hipStream_t stream) {
+  if (io_dtype == 0) return launch<float, float>(a, backward, parts, stream);
+  if (stream_dtype == 0) return launch<uint16_t, float>(a, backward, parts, stream);
+  return launch<uint16_t, uint16_t>(a, backward, parts, stream);
+}
+
+}  // namespace
+
+hipError_t launch_residual_norm(const ResidualArgs& a, int io_dtype, int stream_dtype, hipStream_t stream) {
+  return launch_types(a, io_dtype, stream_dtype, false, nullptr, stream);
+}
+hipError_t launch_residual_norm_backward(const ResidualArgs& a, int io_dtype, int stream_dtype, int* parts, hipStream_t stream) {
+  return launch_types(a, io_dtype, stream_dtype, true, parts, stream);
+}
+
+}  // namespace vla

@@ -42,7 +42,7 @@ void* scratch_of_current_device() {
   return g_scratch_ptr[dev];
 }
 
-constexpr int kVersion = 700;  // 0.7.0
+constexpr int kVersion = 800;  // 0.8.0
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
