@@ -46,7 +46,6 @@ struct Place {
     b = here ? static_cast<int>(rest / a.runs) : 0;
   }
 };
-__device__ __forceinline__ int length_of(const int* lengths, int b, int T) { return lengths == nullptr ? T : min(max(lengths[b], 0), T); }
 
 // Row t of a sequence: of x, of the state before it (t < 0, at least 1 - W), zero where there is none.
 template <typename IO, int W>

@@ -27,6 +27,10 @@ bool rows2(const vla_strides& s, int B, int T, int n, int dtype, bool written, v
   *out = vla::Row2{r.b, r.t};
   return true;
 }
+// the scan's kernels address the rows of a block with 31-bit byte offsets
+bool rows_near(const vla::Row2& r, int n, int dtype) {
+  return r.t < 0x7fffffffLL / (2 * vla::kScanBlock * static_cast<long long>(size_of(dtype))) && n <= 0x7fffffffLL / (2 * static_cast<long long>(size_of(dtype)));
+}
 size_t reach2(const vla::Row2& r, int B, int T, int n, int dtype) { return reach(vla::Rows{r.b, 0, r.t}, B, 1, T, n, size_of(dtype)); }
 bool all_aligned(const void* const* p, int n) {
   for (int i = 0; i < n; ++i) {
@@ -90,7 +94,7 @@ vla_scan_opts scan_opts(const vla_scan_opts* o) {
   if (o != nullptr) r = *o;
   return r;
 }
-int tiles_of(int n, int groups, int tile = vla::kScanTile) { return (n / groups + tile - 1) / tile; }
+int tiles_of(int n, int groups, int tile) { return (n / groups + tile - 1) / tile; }
 int blocks_of(int T) { return (T + vla::kScanBlock - 1) / vla::kScanBlock; }
 
 int check_scan(int B, int T, int n, int N, int io_dtype, const vla_scan_opts& o) {
@@ -99,53 +103,50 @@ int check_scan(int B, int T, int n, int N, int io_dtype, const vla_scan_opts& o)
   if (N <= 0 || o.groups <= 0 || n % o.groups != 0 || o.segments < 0) return VLA_ERR_INVALID_ARG;
   if (st != VLA_OK) return st;
   if (!vla::scan_state_size(N) || n / o.groups % 8 != 0) return VLA_ERR_UNSUPPORTED;
-  if (!fits_launch(static_cast<long long>(B) * o.groups * tiles_of(n, o.groups, 64), 16 * N)) return VLA_ERR_UNSUPPORTED;
+  if (!fits_launch(static_cast<long long>(B) * o.groups * tiles_of(n, o.groups, vla::selective_tile(N)), 512)) return VLA_ERR_UNSUPPORTED;
   if (!fits_launch(static_cast<long long>(B) * n, N) || static_cast<long long>(B) * n * N > kMostItems - 256) return VLA_ERR_UNSUPPORTED;
   return VLA_OK;
 }
 
 // Time segments.  In segments the tokens are gone through twice (the second time without the read-out).
-struct ScanSegments {
-  int n, blocks;             // of each
+struct ScanPlan {
+  int n, tokens;             // segments, tokens of each: whole blocks
   size_t h_bytes, dt_bytes;  // of the states and the sums of steps
 };
-ScanSegments scan_segments(int B, int T, int n, int N, int groups, int requested) {
-  const int blocks = blocks_of(T);
-  const long long workgroups = static_cast<long long>(B) * groups * tiles_of(n, groups), waves = workgroups * (N / 8);
+ScanPlan scan_plan(int B, int T, int n, int N, int groups, int requested) {
+  ScanPlan p{1, T, 0, 0};
+  const int blocks = blocks_of(T), threads = 256;
+  const long long workgroups = static_cast<long long>(B) * groups * tiles_of(n, groups, vla::selective_tile(N)), waves = workgroups * (threads / 64);
   long long s = requested;
   if (requested == 0) {
     s = 1;
-    if (waves < 1024) s = (2048 + waves - 1) / waves;
+    if (waves < 1900) s = (8192 + waves - 1) / waves;
     if (s > blocks / 4) s = blocks / 4;
   }
   if (s > blocks) s = blocks;
   if (s > 1024) s = 1024;
-  if (s > 1 && !fits_launch(2 * workgroups * s, 16 * N)) s = 1;
-  if (s < 1) s = 1;
-  ScanSegments r{1, blocks, 0, 0};
-  if (s == 1) return r;
-  r.blocks = static_cast<int>((blocks + s - 1) / s);
-  r.n = (blocks + r.blocks - 1) / r.blocks;
-  r.h_bytes = padded(static_cast<size_t>(B) * r.n * n * N * 4);
-  r.dt_bytes = padded(static_cast<size_t>(B) * r.n * n * 4);
-  return r;
+  if (s > 1 && !fits_launch(workgroups * s, threads)) s = 1;
+  if (s <= 1) return p;
+  p.tokens = vla::kScanBlock * static_cast<int>((blocks + s - 1) / s);
+  p.n = (T + p.tokens - 1) / p.tokens;
+  p.h_bytes = padded(static_cast<size_t>(B) * p.n * n * N * 4);
+  p.dt_bytes = padded(static_cast<size_t>(B) * p.n * n * 4);
+  return p;
 }
 
-size_t scan_saved(int B, int T, int n, int N, int groups) {
-  return static_cast<size_t>(B) * blocks_of(T) * groups * tiles_of(n, groups) * vla::kScanTile * N * 4;
-}
+size_t scan_saved(int B, int T, int n, int N) { return static_cast<size_t>(B) * blocks_of(T) * n * N * 4; }
 struct ScanBackwardParts {
-  ScanSegments seg;
+  ScanPlan seg;
   size_t dA, dD, dbias, dBC, seg_h, seg_dt, bytes;   // offsets
 };
 ScanBackwardParts scan_backward_parts(int B, int T, int n, int N, int groups, int requested) {
   ScanBackwardParts p{};
-  p.seg = scan_segments(B, T, n, N, groups, requested);
+  p.seg = scan_plan(B, T, n, N, groups, requested);
   const size_t rows = static_cast<size_t>(B) * p.seg.n;
   p.dD = p.dA + padded(rows * n * N * 4);
   p.dbias = p.dD + padded(rows * n * 4);
   p.dBC = p.dbias + padded(rows * n * 4);
-  p.seg_h = p.dBC + padded(static_cast<size_t>(groups) * tiles_of(n, groups, vla::scan_backward_tile(N)) * B * T * 2 * N * 4);
+  p.seg_h = p.dBC + padded(static_cast<size_t>(groups) * tiles_of(n, groups, vla::selective_tile(N)) * B * T * 2 * N * 4);
   p.seg_dt = p.seg_h + p.seg.h_bytes;
   p.bytes = p.seg_dt + p.seg.dt_bytes;
   return p;
@@ -174,16 +175,19 @@ int scan_args(const void* u, const void* delta, const float* A, const void* Bm, 
       !state_rows(op.C, B, T, op.groups, N, io_dtype, &rc)) {
     return VLA_ERR_INVALID_ARG;
   }
+  for (const vla::Row2* r : {&a->us, &a->ds, &a->zs}) {
+    if (!rows_near(*r, n, io_dtype)) return VLA_ERR_UNSUPPORTED;
+  }
   a->B_b = rb.b; a->B_g = rb.h; a->B_t = rb.t;
   a->C_b = rc.b; a->C_g = rc.h; a->C_t = rc.t;
   a->u = u; a->delta = delta; a->A = A; a->Bm = Bm; a->Cm = Cm; a->D = D; a->z = z; a->bias = bias;
   a->lengths = op.lengths;
   a->nb = B; a->T = T; a->n = n; a->G = op.groups;
   a->softplus = op.softplus != 0;
-  a->tiles = tiles_of(n, op.groups);
+  a->tiles = tiles_of(n, op.groups, vla::selective_tile(N));
   a->blocks = blocks_of(T);
   a->n_seg = 1;
-  a->seg_blocks = a->blocks;
+  a->seg_tokens = vla::kScanBlock * blocks_of(T);
   return VLA_OK;
 }
 // what all calls of the scan read
@@ -344,13 +348,13 @@ size_t vla_selective_scan_workspace_bytes(int B, int T, int n, int N, int io_dty
   const vla_scan_opts op = scan_opts(opts);
   if (check_scan(B, T, n, N, io_dtype, op) != VLA_OK) return 0;
   if (backward) return scan_backward_parts(B, T, n, N, op.groups, op.segments).bytes;
-  const ScanSegments s = scan_segments(B, T, n, N, op.groups, op.segments);
+  const ScanPlan s = scan_plan(B, T, n, N, op.groups, op.segments);
   return s.h_bytes + s.dt_bytes;
 }
 
 size_t vla_selective_scan_saved_bytes(int B, int T, int n, int N, int io_dtype, const vla_scan_opts* opts) {
   const vla_scan_opts op = scan_opts(opts);
-  return check_scan(B, T, n, N, io_dtype, op) == VLA_OK ? scan_saved(B, T, n, N, op.groups) : 0;
+  return check_scan(B, T, n, N, io_dtype, op) == VLA_OK ? scan_saved(B, T, n, N) : 0;
 }
 
 int vla_selective_scan(const void* u, const void* delta, const float* A, const void* Bm, const void* Cm, const float* D, const void* z,
@@ -363,8 +367,9 @@ int vla_selective_scan(const void* u, const void* delta, const float* A, const v
   const void* ptrs[] = {h0, y, h_T, workspace, op.saved};
   if ((T > 0 && y == nullptr) || !all_aligned(ptrs, 5)) return VLA_ERR_INVALID_ARG;
   if (!rows2(op.y, B, T, n, io_dtype, true, &a.ys)) return VLA_ERR_INVALID_ARG;
-  const size_t states = static_cast<size_t>(B) * n * N * 4, saved = scan_saved(B, T, n, N, op.groups);
-  const ScanSegments seg = scan_segments(B, T, n, N, op.groups, op.segments);
+  if (!rows_near(a.ys, n, io_dtype)) return VLA_ERR_UNSUPPORTED;
+  const size_t states = static_cast<size_t>(B) * n * N * 4, saved = scan_saved(B, T, n, N);
+  const ScanPlan seg = scan_plan(B, T, n, N, op.groups, op.segments);
   const size_t need = seg.h_bytes + seg.dt_bytes;
   const bool cut = seg.n > 1 && workspace != nullptr && workspace_bytes >= need;
   Range r[kScanReads + 5];
@@ -383,7 +388,7 @@ int vla_selective_scan(const void* u, const void* delta, const float* A, const v
   hipError_t err = hipSuccess;
   if (cut) {
     a.n_seg = seg.n;
-    a.seg_blocks = seg.blocks;
+    a.seg_tokens = seg.tokens;
     a.seg_h = static_cast<float*>(workspace);
     a.seg_dt = reinterpret_cast<float*>(static_cast<char*>(workspace) + seg.h_bytes);
     err = vla::launch_selective_scan(a, N, io_dtype, true, s);
@@ -428,8 +433,9 @@ int vla_selective_scan_backward(const void* u, const void* delta, const float* A
       !rows2(op.ddelta, B, T, n, io_dtype, true, &a.dds) || !rows2(op.dz, B, T, n, io_dtype, true, &a.dzs)) {
     return VLA_ERR_INVALID_ARG;
   }
+  if (!rows_near(a.ys, n, io_dtype)) return VLA_ERR_UNSUPPORTED;
   const ScanBackwardParts parts = scan_backward_parts(B, T, n, N, op.groups, op.segments);
-  const size_t states = static_cast<size_t>(B) * n * N * 4, saved = scan_saved(B, T, n, N, op.groups);
+  const size_t states = static_cast<size_t>(B) * n * N * 4, saved = scan_saved(B, T, n, N);
   const size_t of_rows = static_cast<size_t>(B) * T * op.groups * N * size_of(io_dtype);
   Range r[kScanReads + 13];
   scan_reads(a, N, io_dtype, r);
@@ -452,12 +458,11 @@ int vla_selective_scan_backward(const void* u, const void* delta, const float* A
   if (static_cast<long long>(B) * T * op.groups > (kMostItems - 256) / (N / 4)) return VLA_ERR_UNSUPPORTED;
   char* ws = static_cast<char*>(workspace);
   const auto at = [&](size_t offset) { return reinterpret_cast<float*>(ws + offset); };
-  a.tiles = tiles_of(n, op.groups, vla::scan_backward_tile(N));
   a.dy = dy; a.dh_T = dh_T; a.du = du; a.ddelta = ddelta; a.dz = dz; a.dh0 = dh0; a.dB = dBm; a.dC = dCm;
   a.kept = static_cast<float*>(op.saved);
   a.dA_part = at(parts.dA); a.dD_part = at(parts.dD); a.dbias_part = at(parts.dbias); a.dBC_part = at(parts.dBC);
   a.n_seg = parts.seg.n;
-  a.seg_blocks = parts.seg.blocks;
+  if (a.n_seg > 1) a.seg_tokens = parts.seg.tokens;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t err = hipSuccess;
   if (a.n_seg > 1) {

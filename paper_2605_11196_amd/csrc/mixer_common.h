@@ -51,9 +51,8 @@ hipError_t launch_causal_conv(const ConvArgs& a, int width, int io_dtype, hipStr
 hipError_t launch_causal_conv_step(const ConvArgs& a, int width, int io_dtype, hipStream_t stream);
 hipError_t launch_causal_conv_backward(const ConvArgs& a, int width, int io_dtype, hipStream_t stream);
 
-constexpr int kScanTile = 128;   // channels of a workgroup: a pair for each lane
-inline int scan_backward_tile(int N) { return N == 64 ? 64 : 128; }   // of the backward pass
-constexpr int kScanBlock = 8;    // tokens that a workgroup goes through at once, and between two states that are kept
+constexpr int kScanBlock = 8;    // tokens between two states that are kept
+int selective_tile(int N);       // channels of a workgroup
 struct ScanArgs {
   const void* u;
   const void* delta;
@@ -70,12 +69,12 @@ struct ScanArgs {
   Row2 us, ds, zs, ys;    // (backward: dy has ys)
   long long B_b, B_g, B_t, C_b, C_g, C_t;   // element strides of B and C [B, T, G, N]
   int nb, T, n, G, softplus;
-  int tiles;              // workgroups of a group's channels (of kScanTile; backward: of scan_backward_tile())
-  // what is kept for the backward pass: the state before every block, as the lanes hold it, or nullptr
-  float* kept;            // [B][blocks][G * tiles][waves][4][64] float4
+  int tiles;              // workgroups of a group's channels
+  // what is kept for the backward pass: the state before every 8th token, or nullptr
+  float* kept;            // [B][blocks][n][N]
   int blocks;
-  // time segments of seg_blocks blocks each
-  int n_seg, seg_blocks;
+  // time segments
+  int n_seg, seg_tokens;
   float* seg_h;           // [B][n_seg][n][N]: the maps' own ends, then the states that the segments start from
   float* seg_dt;          // [B][n_seg][n]: sums of the steps
   // backward

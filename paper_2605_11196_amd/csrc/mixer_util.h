@@ -17,15 +17,6 @@ __device__ __forceinline__ f2 load2(const uint16_t* p) { return widen(*reinterpr
 __device__ __forceinline__ void store2(float* p, f2 x) { *reinterpret_cast<f2*>(p) = x; }
 __device__ __forceinline__ void store2(uint16_t* p, f2 x) { *reinterpret_cast<uint32_t*>(p) = pack_rne(x[0], x[1]); }
 
-// A pair as it lies in memory, for loads that are under way while other work goes on.
-template <typename IO> struct PairOf;
-template <> struct PairOf<float> { typedef f2 type; };
-template <> struct PairOf<uint16_t> { typedef uint32_t type; };
-template <typename IO> using Pair = typename PairOf<IO>::type;
-template <typename IO> __device__ __forceinline__ Pair<IO> raw2(const IO* p) { return *reinterpret_cast<const Pair<IO>*>(p); }
-__device__ __forceinline__ f2 wide2(f2 x) { return x; }
-__device__ __forceinline__ f2 wide2(uint32_t x) { return widen(x); }
-
 // 16 bytes as they lie in memory, and their values
 template <typename IO> struct Piece;
 template <> struct Piece<float> {
@@ -49,17 +40,18 @@ template <int V> __device__ __forceinline__ void store_piece(uint16_t* p, const 
   for (int i = 0; i < V; i += 4) *reinterpret_cast<u2*>(p + i) = u2{pack_rne(x[i], x[i + 1]), pack_rne(x[i + 2], x[i + 3])};
 }
 
+// Tokens of a sequence.
+__device__ __forceinline__ int length_of(const int* lengths, int b, int T) { return lengths == nullptr ? T : min(max(lengths[b], 0), T); }
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
 
-// log(1 + exp(x)) = max(x, 0) + log1p(w), w = exp(-|x|), and its derivative.  With u = 1 + w rounded, log1p(w) is log(u) w / (u - 1): the
-// quotient makes up for what the sum has lost of a small w (W. Kahan).
+// log(1 + exp(x)) = max(x, 0) + log1p(w), w = exp(-|x|).  With u = 1 + w rounded and c = w - (u - 1), which is exact, log1p(w) = log(u) + log(1 + c / u);
+// c is at most half a step of u, so that c in the place of the second term is off by c w or less: 2^-24 of the result.
 __device__ __forceinline__ float softplus(float x) {
-  const float w = __builtin_amdgcn_exp2f(-kLog2e * fabsf(x));
-  const float u = 1.0f + w, d = u - 1.0f;
-  const float l = __builtin_amdgcn_logf(u) * kLn2 * (w * __builtin_amdgcn_rcpf(d));
-  return fmaxf(x, 0.0f) + (d == 0.0f ? w : l);
+  const float w = __builtin_amdgcn_exp2f(-kLog2e * fabsf(x)), u = 1.0f + w, c = w - (u - 1.0f);
+  return fmaxf(x, 0.0f) + fmaf(__builtin_amdgcn_logf(u), kLn2, c);
 }
 
 __device__ __forceinline__ float swap32_sum(float x) {

@@ -7,12 +7,12 @@ _CONTIGUOUS = VlaStrides(0, 0, 0)
 
 def _laid_rows(x):
     """x [B,T,n] (or [B,n]) and its strides for the C call, or a contiguous copy where it is not laid out as the kernels take it: the last
-    dimension together, the others in steps of 16 bytes that are not all zero, 16-byte alignment."""
+    dimension together, the others in steps of 16 bytes that are not all zero, tokens not too far apart, 16-byte alignment."""
     aligned = not x.data_ptr() & 15
     if x.is_contiguous():
         return (x if aligned else x.clone()), _CONTIGUOUS
     size, step = x.element_size(), [s if n > 1 else 0 for s, n in zip(x.stride(), x.shape[:-1])]
-    if aligned and (x.stride(-1) == 1 or x.shape[-1] == 1) and not any(s * size & 15 for s in step) and any(step):
+    if aligned and x.stride(-1) == 1 and not any(s * size & 15 for s in step) and any(step) and step[-1] * size < 2 ** 26:
         return x, VlaStrides(step[0], 0, step[1] if len(step) > 1 else 0)
     return x.contiguous(), _CONTIGUOUS
 
