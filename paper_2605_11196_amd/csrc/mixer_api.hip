@@ -433,7 +433,9 @@ int vla_selective_scan_backward(const void* u, const void* delta, const float* A
       !rows2(op.ddelta, B, T, n, io_dtype, true, &a.dds) || !rows2(op.dz, B, T, n, io_dtype, true, &a.dzs)) {
     return VLA_ERR_INVALID_ARG;
   }
-  if (!rows_near(a.ys, n, io_dtype)) return VLA_ERR_UNSUPPORTED;
+  for (const vla::Row2* r : {&a.ys, &a.dus, &a.dds, &a.dzs}) {
+    if (!rows_near(*r, n, io_dtype)) return VLA_ERR_UNSUPPORTED;
+  }
   const ScanBackwardParts parts = scan_backward_parts(B, T, n, N, op.groups, op.segments);
   const size_t states = static_cast<size_t>(B) * n * N * 4, saved = scan_saved(B, T, n, N);
   const size_t of_rows = static_cast<size_t>(B) * T * op.groups * N * size_of(io_dtype);

@@ -59,30 +59,32 @@ __device__ __forceinline__ void wave_sums(const float (&p)[8], float* row, int s
 }
 
 template <int N, typename IO, bool MAP>
-__global__ void __launch_bounds__(64 * scan_waves(N)) backward_kernel(ScanArgs a) {
+__global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_waves_per_eu(2))) backward_kernel(ScanArgs a) {
   typedef ScanPlace<N> P;
-  constexpr int LN = P::LN, OWN = P::OWN, W = scan_waves(N);
-  __shared__ f4 steps[W][TB][P::CW];                     // dt, dt u, e
+  constexpr int LN = P::LN, OWN = P::OWN, TURNS = kTurns<LN>, W = scan_waves(N);
+  __shared__ f4 steps[W][TB][P::CW];                     // dt, dt u, e; then the sums over the states: y, p, sum g a h A
   __shared__ __align__(16) float staged[W][TB][2 * N];   // B, C
   __shared__ __align__(16) float sums[2][MAP ? 1 : W][TB][2 * N];
   const P w(a);
   const size_t state = (static_cast<size_t>(w.b) * a.n + w.c) * N + 4 * w.q, of_seg = (static_cast<size_t>(w.b) * a.n_seg + w.seg) * a.n + w.c;
   const bool gated = a.z != nullptr;
   const ScanRows<N, IO> u(w, a.u, a.us), delta(w, a.delta, a.ds), z(w, gated ? a.z : a.u, gated ? a.zs : a.us), dy(w, a.dy, a.ys);
+  const ScanRows<N, IO> du_(w, MAP ? a.u : a.du, MAP ? a.us : a.dus), ddelta_(w, MAP ? a.u : a.ddelta, MAP ? a.us : a.dds),
+      dz_(w, MAP || !gated ? a.u : a.dz, MAP || !gated ? a.us : a.dzs);
   ScanStage<N, IO> rows(w, a);
   float* const mine = staged[w.wave][0];
   f4* const step = steps[w.wave][0];
-  const int in_wave = w.lane / LN;
 
   const f4 A2 = *reinterpret_cast<const f4*>(a.A + static_cast<size_t>(w.c) * N + 4 * w.q) * kLog2e;
   f4 g = {0.0f, 0.0f, 0.0f, 0.0f}, dA = g;
   if (!MAP && a.n_seg > 1) g = *reinterpret_cast<const f4*>(a.seg_h + of_seg * N + 4 * w.q);
   if (!MAP && a.n_seg == 1 && a.dh_T != nullptr) g = *reinterpret_cast<const f4*>(a.dh_T + state);
-  const float bias = a.bias != nullptr ? a.bias[w.c] : 0.0f, D = a.D != nullptr ? a.D[w.c] : 0.0f;
-  float sum_dt = 0.0f, dD = 0.0f, dbias = 0.0f;
+  const f2 bias = pair_of(a.bias, w.c2), D = pair_of(a.D, w.c2);
+  float sum_dt = 0.0f;
+  f2 dD = {0.0f, 0.0f}, dbias = dD;
 
   // what a block reads is on its way while the one behind it is worked on
-  IO next_u[OWN], next_delta[OWN], next_z[OWN], next_dy[OWN];
+  Pair<IO> next_u[OWN] = {}, next_delta[OWN] = {}, next_z[OWN] = {}, next_dy[OWN] = {};
   f4 next_h = {};
   const auto fetch = [&](int t0) {
     u.load(w, a.T, t0, next_u);
@@ -96,18 +98,22 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) backward_kernel(ScanArgs a
   if (last >= w.first) fetch(last);
   int turn = 0;
   for (int t0 = last; t0 >= w.first; t0 -= TB) {
-    float x[OWN], raw[OWN], v[OWN], d[OWN], dt_[OWN], e_[OWN];
+    f2 x[OWN], raw[OWN], v[OWN], sig[OWN], d[OWN], dt_[OWN], e_[OWN];
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
-      const bool in = t0 + w.own(k) < w.length && w.here;
-      x[k] = wide1(next_u[k]);
-      raw[k] = wide1(next_delta[k]) + bias;
-      v[k] = wide1(next_z[k]);
-      d[k] = wide1(next_dy[k]);
-      const float dt = a.softplus ? softplus(raw[k]) : raw[k], e = gated ? d[k] * v[k] * sigmoid(v[k]) : d[k];
-      dt_[k] = in ? dt : 0.0f;
-      e_[k] = in ? e : 0.0f;
-      if (w.owner) step[w.own(k) * P::CW + in_wave] = f4{dt_[k], in ? dt * x[k] : 0.0f, e_[k], 0.0f};
+      const bool in = t0 + w.own(k) < w.length && w.here2;
+      x[k] = wide2(next_u[k]);
+      raw[k] = wide2(next_delta[k]) + bias;
+      v[k] = wide2(next_z[k]);
+      d[k] = wide2(next_dy[k]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        sig[k][j] = sigmoid(v[k][j]);
+        const float dt = a.softplus ? softplus(raw[k][j]) : raw[k][j], e = gated ? d[k][j] * v[k][j] * sig[k][j] : d[k][j];
+        dt_[k][j] = in ? dt : 0.0f;
+        e_[k][j] = in ? e : 0.0f;
+        if (w.lane < TB * P::PAIRS) steps[w.wave][w.own(k)][2 * w.pair + j] = f4{dt_[k][j], in ? dt * x[k][j] : 0.0f, e_[k][j], 0.0f};
+      }
     }
     rows.put(mine, t0, w.length);
     f4 h = next_h;
@@ -116,7 +122,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) backward_kernel(ScanArgs a
     if constexpr (MAP) {
 #pragma unroll
       for (int t = TB - 1; t >= 0; --t) {
-        const f4 s = step[t * P::CW + in_wave];
+        const f4 s = step[t * P::CW + w.in_wave];
         const f4 C = *reinterpret_cast<const f4*>(mine + t * 2 * N + N + 4 * w.q);
 #pragma unroll
         for (int i = 0; i < 4; ++i) g[i] = fmaf(s[2], C[i], g[i]) * __builtin_amdgcn_exp2f(s[0] * A2[i]);
@@ -126,11 +132,11 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) backward_kernel(ScanArgs a
     } else {
       float* const own_sums = sums[turn][w.wave][0];
       f4 decay[TB], decayed[TB];   // a, a h_{t-1}
-      float p[8], y[OWN], through[OWN], rate[OWN];
+      float p[2][8], some[2][4], y[TURNS] = {}, through[TURNS] = {}, rate[TURNS] = {};
       // the operands of a token are on their way from LDS while the one before it is worked on; more of them would not fit
       f4 s_[2], B_[2], C_[2];
       const auto operands = [&](int t) {
-        s_[t % 2] = step[t * P::CW + in_wave];
+        s_[t % 2] = step[t * P::CW + w.in_wave];
         B_[t % 2] = *reinterpret_cast<const f4*>(mine + t * 2 * N + 4 * w.q);
         C_[t % 2] = *reinterpret_cast<const f4*>(mine + t * 2 * N + N + 4 * w.q);
       };
@@ -146,14 +152,14 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) backward_kernel(ScanArgs a
           decayed[t][i] = decay[t][i] * h[i];
           h[i] = fmaf(s[1], B[i], decayed[t][i]);
           read = i == 0 ? C[0] * h[0] : fmaf(C[i], h[i], read);
-          p[t % 2 * 4 + i] = s[2] * h[i];
+          p[t / 2 % 2][t % 2 * 4 + i] = s[2] * h[i];
         }
-        const int k = LN >= TB ? 0 : t / LN;       // the lane whose token it is keeps it
-        read = channel_sum<LN>(read);
-        y[k] = t % LN == 0 || w.q == t % LN ? read : y[k];
-        if (t % 2) wave_sums<LN>(p, own_sums + (t - 1) * 2 * N + N, 2 * N, w.lane);
-        __builtin_amdgcn_sched_barrier(0);
+        keep_sum<LN>(read, some[0], y, t, t % LN == LN - 1, w.q);
+        // the sums of the pair of tokens before lie between the work on this one
+        if (t % 2 == 0 && t > 0) wave_sums<LN>(p[(t / 2 - 1) % 2], own_sums + (t - 2) * 2 * N + N, 2 * N, w.lane);
+        if (t % 2) __builtin_amdgcn_sched_barrier(0);
       }
+      wave_sums<LN>(p[1], own_sums + (TB - 2) * 2 * N + N, 2 * N, w.lane);
 #pragma unroll
       for (int t = TB - 1; t >= 0; --t) {
         if (t > 0) operands(t - 1);
@@ -163,37 +169,43 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) backward_kernel(ScanArgs a
         for (int i = 0; i < 4; ++i) {
           g[i] = fmaf(s[2], C[i], g[i]);
           sum_p = i == 0 ? g[0] * B[0] : fmaf(g[i], B[i], sum_p);
-          p[t % 2 * 4 + i] = g[i] * s[1];
+          p[t / 2 % 2][t % 2 * 4 + i] = g[i] * s[1];
           const float m = g[i] * decayed[t][i];
           sum_r = i == 0 ? m * A2[0] : fmaf(m, A2[i], sum_r);
           dA[i] = fmaf(m, s[0], dA[i]);
           g[i] *= decay[t][i];
         }
-        const int k = LN >= TB ? 0 : t / LN;
-        const bool keep = t % LN == (LN >= TB ? TB : LN) - 1 || w.q == t % LN;
-        sum_p = channel_sum<LN>(sum_p);
-        sum_r = channel_sum<LN>(sum_r);
-        through[k] = keep ? sum_p : through[k];
-        rate[k] = keep ? sum_r : rate[k];
-        if (t % 2 == 0) wave_sums<LN>(p, own_sums + t * 2 * N, 2 * N, w.lane);
-        __builtin_amdgcn_sched_barrier(0);
+        keep_sum<LN>(sum_p, some[0], through, t, t % LN == 0, w.q);
+        keep_sum<LN>(sum_r, some[1], rate, t, t % LN == 0, w.q);
+        if (t % 2 && t < TB - 1) wave_sums<LN>(p[(t / 2 + 1) % 2], own_sums + (t + 1) * 2 * N, 2 * N, w.lane);
+        if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+      }
+      wave_sums<LN>(p[0], own_sums, 2 * N, w.lane);
+      wave_fence();
+#pragma unroll
+      for (int k = 0; k < TURNS; ++k) {
+        if (LN <= TB || w.q < TB) step[(LN * k + w.q) * P::CW + w.in_wave] = f4{y[k], through[k], rate[k], 0.0f};
       }
       wave_fence();
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
         const int t = t0 + w.own(k);
         const bool in = t < w.length;
-        const float inner = fmaf(D, x[k], y[k]), sig = sigmoid(v[k]), slope = a.softplus ? sigmoid(raw[k]) : 1.0f;
-        const float du = fmaf(D, e_[k], dt_[k] * through[k]), ddelta = fmaf(x[k], through[k], kLn2 * rate[k]) * slope;
-        const float dz = d[k] * inner * sig * fmaf(v[k], 1.0f - sig, 1.0f);
-        const bool count = in && w.owner;
-        dD += count ? e_[k] * x[k] : 0.0f;
-        dbias += count ? ddelta : 0.0f;
-        if (w.here && w.owner && t < w.last) {
-          const size_t row = static_cast<size_t>(t);
-          ScanRows<N, IO>::put(static_cast<IO*>(a.du) + w.b * a.dus.b + row * a.dus.t + w.c, in ? du : 0.0f);
-          ScanRows<N, IO>::put(static_cast<IO*>(a.ddelta) + w.b * a.dds.b + row * a.dds.t + w.c, in ? ddelta : 0.0f);
-          if (gated) ScanRows<N, IO>::put(static_cast<IO*>(a.dz) + w.b * a.dzs.b + row * a.dzs.t + w.c, in ? dz : 0.0f);
+        f2 du, ddelta, dz;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const f4 sum = step[w.own(k) * P::CW + 2 * w.pair + j];
+          const float inner = fmaf(D[j], x[k][j], sum[0]), slope = a.softplus ? sigmoid(raw[k][j]) : 1.0f;
+          du[j] = in ? fmaf(D[j], e_[k][j], dt_[k][j] * sum[1]) : 0.0f;
+          ddelta[j] = in ? fmaf(x[k][j], sum[1], kLn2 * sum[2]) * slope : 0.0f;
+          dz[j] = in ? d[k][j] * inner * sig[k][j] * fmaf(v[k][j], 1.0f - sig[k][j], 1.0f) : 0.0f;
+          dD[j] += in ? e_[k][j] * x[k][j] : 0.0f;
+          dbias[j] += ddelta[j];
+        }
+        if (w.here2 && t < w.last) {
+          du_.store(t0, k, du);
+          ddelta_.store(t0, k, ddelta);
+          if (gated) dz_.store(t0, k, dz);
         }
       }
       // dB and dC of the workgroup's channels: the waves in their order
@@ -217,22 +229,36 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) backward_kernel(ScanArgs a
     for (int t0 = gone; t0 < w.last; t0 += TB) {
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
-        const size_t row = t0 + w.own(k);
-        if (w.here && w.owner && t0 + w.own(k) < w.last) {
-          ScanRows<N, IO>::put(static_cast<IO*>(a.du) + w.b * a.dus.b + row * a.dus.t + w.c, 0.0f);
-          ScanRows<N, IO>::put(static_cast<IO*>(a.ddelta) + w.b * a.dds.b + row * a.dds.t + w.c, 0.0f);
-          if (gated) ScanRows<N, IO>::put(static_cast<IO*>(a.dz) + w.b * a.dzs.b + row * a.dzs.t + w.c, 0.0f);
+        if (w.here2 && t0 + w.own(k) < w.last) {
+          const f2 zero = {0.0f, 0.0f};
+          du_.store(t0, k, zero);
+          ddelta_.store(t0, k, zero);
+          if (gated) dz_.store(t0, k, zero);
         }
       }
     }
-    dD = channel_sum<LN>(dD);
-    dbias = channel_sum<LN>(dbias);
-    if (!w.here) return;
-    *reinterpret_cast<f4*>(a.dA_part + of_seg * N + 4 * w.q) = dA;
-    if (w.seg == 0 && a.dh0 != nullptr) *reinterpret_cast<f4*>(a.dh0 + state) = g;
-    if (w.q == 0) {
-      a.dD_part[of_seg] = dD;
-      a.dbias_part[of_seg] = dbias;
+    if (w.here) {
+      *reinterpret_cast<f4*>(a.dA_part + of_seg * N + 4 * w.q) = dA;
+      if (w.seg == 0 && a.dh0 != nullptr) *reinterpret_cast<f4*>(a.dh0 + state) = g;
+    }
+    // the lanes of a pair of channels: every PAIRS-th one
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float* const all = sums[0][w.wave][0];      // room for two numbers a lane: 16 N
+      __syncthreads();
+      all[w.lane] = w.here2 ? dD[j] : 0.0f;
+      all[64 + w.lane] = w.here2 ? dbias[j] : 0.0f;
+      wave_fence();
+      if (w.lane < P::PAIRS && w.here2) {
+        float total_D = 0.0f, total_bias = 0.0f;
+        for (int l = w.lane; l < 64 && l < TB * P::PAIRS; l += P::PAIRS) {
+          total_D += all[l];
+          total_bias += all[64 + l];
+        }
+        const size_t at = (static_cast<size_t>(w.b) * a.n_seg + w.seg) * a.n + w.c2 + j;
+        a.dD_part[at] = total_D;
+        a.dbias_part[at] = total_bias;
+      }
     }
   }
 }

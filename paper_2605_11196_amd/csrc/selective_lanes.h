@@ -3,8 +3,9 @@
 //
 // N / 4 neighbouring lanes hold a channel, four states (16 bytes of A, of a state, of B and C) each; a wave 256 / N channels. So sums over states stay
 // in a row of lanes (DPP), states and A go to and from memory as they lie there, and the waves of a sequence need no barrier.  The tokens go by in
-// blocks of eight.  What depends on the token and the channel alone (the step, the gate) is formed once, by the lane whose place
-// among the channel's is the token's, and passed to the others through LDS, as B and C are, which a wave stages for itself.
+// blocks of eight.  What depends on the token and the channel alone (the step, the gate, the output) is formed once, for a token and a pair of channels a
+// lane, so that a block's rows take one load of 4 (float32: 8) bytes a lane each, and passed on through LDS, as B and C are, which a wave stages
+// for itself.
 #pragma once
 
 #include "mixer_util.h"
@@ -17,14 +18,17 @@ constexpr int TB = kScanBlock;
 constexpr int scan_waves(int N) { return 4; }
 constexpr int scan_tile(int N) { return scan_waves(N) * 256 / N; }   // channels of a workgroup
 
-// A thread's place: sequence, time segment, channel, states.
+// A thread's place: sequence, time segment, channel, states; and the tokens and pairs of channels that it loads and stores.
 template <int N>
 struct ScanPlace {
-  static constexpr int LN = N / 4, CW = 64 / LN, OWN = LN >= TB ? 1 : TB / LN;   // lanes of a channel, channels of a wave, tokens of a lane
-  int b, seg, tile, group, lane, wave, q;
+  static constexpr int LN = N / 4, CW = 64 / LN;          // lanes of a channel, channels of a wave
+  static constexpr int PAIRS = CW / 2, OWN = TB * PAIRS >= 64 ? TB * PAIRS / 64 : 1;   // pairs of a wave's channels, tokens of a lane
+  int b, seg, tile, group, lane, wave, q, in_wave;
   unsigned c;              // channel
   bool here;               // it is one of the group's (otherwise c is another one's, and nothing is stored)
-  bool owner;              // the lane has tokens
+  unsigned c2;             // first channel of the pair
+  int pair;
+  bool here2;              // the pair is the group's, and the lane has tokens
   int length, first, last, live;   // tokens of the sequence, of the segment, and where its sequence ends in it
   __device__ __forceinline__ explicit ScanPlace(const ScanArgs& a) {
     const unsigned tiles = a.G * a.tiles;
@@ -36,20 +40,31 @@ struct ScanPlace {
     lane = threadIdx.x % 64;
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     q = lane % LN;
-    const int of_group = a.n / a.G, at = tile % a.tiles * scan_tile(N) + wave * CW + lane / LN;
+    in_wave = lane / LN;
+    pair = lane % PAIRS;
+    const int of_group = a.n / a.G, from = tile % a.tiles * scan_tile(N) + wave * CW, at = from + in_wave, at2 = from + 2 * pair;
     here = at < of_group;
     c = group * of_group + (here ? at : of_group - 1);
-    owner = LN <= TB || q < TB;
+    here2 = at2 < of_group && lane < TB * PAIRS;
+    c2 = group * of_group + (at2 < of_group ? at2 : of_group - 2);
     length = a.lengths == nullptr ? a.T : min(max(a.lengths[b], 0), a.T);
     first = seg * a.seg_tokens;
     last = min(first + a.seg_tokens, a.T);
     live = min(last, length);
   }
   // token of the block that is this lane's k-th own one
-  __device__ __forceinline__ int own(int k) const { return LN > TB ? min(q, TB - 1) : q + LN * k; }
+  __device__ __forceinline__ int own(int k) const { return min(lane / PAIRS, TB - 1) + 64 / PAIRS * k; }
 };
 
-// A [B, T, n] tensor seen from a lane: its own tokens of a block, from a base that goes along with the block.
+// Two neighbouring values as they lie in memory
+template <typename IO> struct PairOf;
+template <> struct PairOf<float> { typedef f2 type; };
+template <> struct PairOf<uint16_t> { typedef uint32_t type; };
+template <typename IO> using Pair = typename PairOf<IO>::type;
+__device__ __forceinline__ f2 wide2(f2 x) { return x; }
+__device__ __forceinline__ f2 wide2(uint32_t x) { return widen(x); }
+
+// A [B, T, n] tensor seen from a lane: its own tokens' pairs of a block, from a base that goes along with the block.
 template <int N, typename IO>
 struct ScanRows {
   static constexpr int OWN = ScanPlace<N>::OWN;
@@ -60,27 +75,23 @@ struct ScanRows {
     base = const_cast<char*>(static_cast<const char*>(p)) + w.b * r.b * static_cast<long long>(sizeof(IO));
     step = r.t * static_cast<long long>(sizeof(IO));
 #pragma unroll
-    for (int k = 0; k < OWN; ++k) at[k] = w.own(k) * static_cast<unsigned>(step) + w.c * static_cast<unsigned>(sizeof(IO));
+    for (int k = 0; k < OWN; ++k) at[k] = w.own(k) * static_cast<unsigned>(step) + w.c2 * static_cast<unsigned>(sizeof(IO));
   }
   // the rows of block t0 (past the end of memory the last one)
-  __device__ __forceinline__ void load(const ScanPlace<N>& w, int T, int t0, IO (&v)[OWN]) const {
+  __device__ __forceinline__ void load(const ScanPlace<N>& w, int T, int t0, Pair<IO> (&v)[OWN]) const {
     const char* from = base + t0 * step;
     if (t0 + TB <= T) {
 #pragma unroll
-      for (int k = 0; k < OWN; ++k) v[k] = *reinterpret_cast<const IO*>(from + at[k]);
+      for (int k = 0; k < OWN; ++k) v[k] = *reinterpret_cast<const Pair<IO>*>(from + at[k]);
     } else {
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
-        v[k] = *reinterpret_cast<const IO*>(from + (min(w.own(k), T - 1 - t0) * static_cast<unsigned>(step) + w.c * static_cast<unsigned>(sizeof(IO))));
+        v[k] = *reinterpret_cast<const Pair<IO>*>(from + (min(w.own(k), T - 1 - t0) * static_cast<unsigned>(step) + w.c2 * static_cast<unsigned>(sizeof(IO))));
       }
     }
   }
-  __device__ __forceinline__ void store(int t0, int k, float x) const { put(reinterpret_cast<IO*>(base + t0 * step + at[k]), x); }
-  static __device__ __forceinline__ void put(float* p, float x) { *p = x; }
-  static __device__ __forceinline__ void put(uint16_t* p, float x) { *p = static_cast<uint16_t>(pack_rne(x, x)); }
+  __device__ __forceinline__ void store(int t0, int k, f2 x) const { store2(reinterpret_cast<IO*>(base + t0 * step + at[k]), x); }
 };
-__device__ __forceinline__ float wide1(float x) { return x; }
-__device__ __forceinline__ float wide1(uint16_t x) { return bf16_to_f32(x); }
 
 // B and C of a block: a wave's lanes load N / 4 neighbouring values each and put them into LDS as float32, [token][B | C].
 template <int N, typename IO>
@@ -133,6 +144,7 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
+__device__ __forceinline__ f2 pair_of(const float* p, unsigned c) { return p != nullptr ? f2{p[c], p[c + 1]} : f2{0.0f, 0.0f}; }
 // Sum over a channel's lanes, in every one of them.
 template <int LN> __device__ __forceinline__ float channel_sum(float x) {
   if constexpr (LN >= 2) x = dpp_sum<0xB1>(x);
@@ -140,6 +152,31 @@ template <int LN> __device__ __forceinline__ float channel_sum(float x) {
   if constexpr (LN >= 8) x = dpp_sum<0x141>(x);
   if constexpr (LN >= 16) x = dpp_sum<0x140>(x);
   return x;
+}
+
+// The lanes' sums of a number for each token of a block.  Of every LN tokens lane q gets that of token q (LN > 8: of 8), own[k] that of token LN k + q.
+template <int LN> constexpr int kTurns = LN >= TB ? 1 : TB / LN;
+template <int LN>
+__device__ __forceinline__ void keep_sum(float x, float (&some)[4], float (&own)[kTurns<LN>], int t, bool last, int q) {
+  if constexpr (LN <= 4) {
+    some[t % LN] = x;
+    if (!last) return;
+    const bool odd = q & 1, high = q & 2;
+    float r[2];
+#pragma unroll
+    for (int h = 0; h < LN / 2; ++h) {
+      const float keep = odd ? some[2 * h + 1] : some[2 * h], send = odd ? some[2 * h] : some[2 * h + 1];
+      r[h] = keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(send), 0xB1, 0xf, 0xf, true));
+    }
+    if constexpr (LN == 4) {
+      const float keep = high ? r[1] : r[0], send = high ? r[0] : r[1];
+      r[0] = keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(send), 0x4E, 0xf, 0xf, true));
+    }
+    own[t / LN] = r[0];
+  } else {
+    const float sum = channel_sum<LN>(x);
+    own[0] = q == t ? sum : own[0];
+  }
 }
 
 }  // namespace vla

@@ -15,79 +15,103 @@ namespace {
 template <int N, typename IO, bool MAP>
 __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
   typedef ScanPlace<N> P;
-  constexpr int LN = P::LN, OWN = P::OWN;
-  __shared__ f2 steps[scan_waves(N)][TB][P::CW];                     // dt, dt u
-  __shared__ __align__(16) float staged[scan_waves(N)][TB][2 * N];   // B, C
+  constexpr int LN = P::LN, OWN = P::OWN, TURNS = kTurns<LN>;
+  __shared__ f2 steps[scan_waves(N)][2][TB][P::CW];                     // dt, dt u
+  __shared__ __align__(16) float staged[scan_waves(N)][2][TB][2 * N];   // B, C
+  __shared__ __align__(8) float outs[MAP ? 1 : scan_waves(N)][TB][P::CW];            // sums of the read-out
   const P w(a);
   const size_t state = (static_cast<size_t>(w.b) * a.n + w.c) * N + 4 * w.q, of_seg = (static_cast<size_t>(w.b) * a.n_seg + w.seg) * a.n + w.c;
   const bool gated = !MAP && a.z != nullptr;
   const ScanRows<N, IO> u(w, a.u, a.us), delta(w, a.delta, a.ds), z(w, gated ? a.z : a.u, gated ? a.zs : a.us), out(w, MAP ? a.u : a.y, MAP ? a.us : a.ys);
   ScanStage<N, IO> rows(w, a);
-  float* const mine = staged[w.wave][0];
-  f2* const step = steps[w.wave][0];
-  const int in_wave = w.lane / LN;
 
   const f4 A2 = *reinterpret_cast<const f4*>(a.A + static_cast<size_t>(w.c) * N + 4 * w.q) * kLog2e;
   f4 h = {0.0f, 0.0f, 0.0f, 0.0f};
   if (!MAP && a.n_seg > 1) h = *reinterpret_cast<const f4*>(a.seg_h + of_seg * N + 4 * w.q);
   if (!MAP && a.n_seg == 1 && a.h0 != nullptr) h = *reinterpret_cast<const f4*>(a.h0 + state);
-  const float bias = a.bias != nullptr ? a.bias[w.c] : 0.0f, D = a.D != nullptr ? a.D[w.c] : 0.0f;
+  const f2 bias = pair_of(a.bias, w.c2), D = pair_of(a.D, w.c2);
   float sum_dt = 0.0f;
 
-  // what a block reads is on its way while the one before it is worked on
-  IO next_u[OWN], next_delta[OWN], next_z[OWN];
+  // What a block reads is on its way while the one before the one before it is worked on, and its steps are formed while the one before it
+  // is: neither the loads' latency nor that of the transcendental instructions stands between the states' tokens.
+  Pair<IO> next_u[OWN] = {}, next_delta[OWN] = {}, next_z[OWN] = {};
+  f2 x[OWN], v[OWN], now_x[OWN], now_v[OWN];
   const auto fetch = [&](int t0) {
     u.load(w, a.T, t0, next_u);
     delta.load(w, a.T, t0, next_delta);
     if (gated) z.load(w, a.T, t0, next_z);
     rows.load(a.T, t0);
   };
-  if (w.first < w.live) fetch(w.first);
+  const auto form = [&](int t0, int buffer) {
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) {
+      const bool in = t0 + w.own(k) < w.length;
+      x[k] = wide2(next_u[k]);
+      v[k] = wide2(next_z[k]);
+      const f2 raw = wide2(next_delta[k]) + bias;
+      const float d0 = a.softplus ? softplus(raw[0]) : raw[0], d1 = a.softplus ? softplus(raw[1]) : raw[1];
+      *reinterpret_cast<f4*>(&steps[w.wave][buffer][w.own(k)][2 * w.pair]) =
+          f4{in ? d0 : 0.0f, in ? d0 * x[k][0] : 0.0f, in ? d1 : 0.0f, in ? d1 * x[k][1] : 0.0f};
+    }
+    rows.put(staged[w.wave][buffer][0], t0, w.length);
+  };
+  if (w.first < w.live) {
+    fetch(w.first);
+    form(w.first, 0);
+    if (w.first + TB < w.live) fetch(w.first + TB);
+  }
+  int now = 0;
   for (int t0 = w.first; t0 < w.live; t0 += TB) {
     if (!MAP && a.kept != nullptr && w.here) {
       *reinterpret_cast<f4*>(a.kept + ((static_cast<size_t>(w.b) * a.blocks + t0 / TB) * a.n + w.c) * N + 4 * w.q) = h;
     }
-    float x[OWN], v[OWN];
+    wave_fence();
+    const f2* const step = steps[w.wave][now][0];
+    const float* const mine = staged[w.wave][now][0];
+    f2 s_[2];
+    f4 B_[2], C_[2] = {};
+    const auto operands = [&](int t) {
+      s_[t % 2] = step[t * P::CW + w.in_wave];
+      B_[t % 2] = *reinterpret_cast<const f4*>(mine + t * 2 * N + 4 * w.q);
+      if (!MAP) C_[t % 2] = *reinterpret_cast<const f4*>(mine + t * 2 * N + N + 4 * w.q);
+    };
+    operands(0);
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
-      const bool in = t0 + w.own(k) < w.length;
-      x[k] = wide1(next_u[k]);
-      v[k] = wide1(next_z[k]);
-      const float raw = wide1(next_delta[k]) + bias, dt = a.softplus ? softplus(raw) : raw;
-      if (w.owner) step[w.own(k) * P::CW + in_wave] = f2{in ? dt : 0.0f, in ? dt * x[k] : 0.0f};
+      now_x[k] = x[k];
+      now_v[k] = v[k];
     }
-    rows.put(mine, t0, w.length);
-    if (t0 + TB < w.live) fetch(t0 + TB);
-    wave_fence();
-    float y[OWN];
+    now ^= 1;
+    form(t0 + TB, now);
+    if (t0 + 2 * TB < w.live) fetch(t0 + 2 * TB);
+    float some[4], y[TURNS] = {};
 #pragma unroll
     for (int t = 0; t < TB; ++t) {
-      const f2 s = step[t * P::CW + in_wave];
-      const f4 B = *reinterpret_cast<const f4*>(mine + t * 2 * N + 4 * w.q);
-      f4 C = {};
-      if (!MAP) C = *reinterpret_cast<const f4*>(mine + t * 2 * N + N + 4 * w.q);
+      if (t + 1 < TB) operands(t + 1);
+      const f2 s = s_[t % 2];
+      const f4 B = B_[t % 2], C = C_[t % 2];
       float read = 0.0f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         h[i] = fmaf(__builtin_amdgcn_exp2f(s[0] * A2[i]), h[i], s[1] * B[i]);
         if (!MAP) read = i == 0 ? C[0] * h[0] : fmaf(C[i], h[i], read);
       }
-      if (MAP) {
-        sum_dt += s[0];
-      } else {
-        read = channel_sum<LN>(read);
-        const int k = LN >= TB ? 0 : t / LN;       // the lane whose token it is keeps it
-        y[k] = t % LN == 0 || w.q == t % LN ? read : y[k];
-      }
+      if (MAP) sum_dt += s[0];
+      else keep_sum<LN>(read, some, y, t, t % LN == LN - 1, w.q);
+    }
+    if (MAP) continue;
+#pragma unroll
+    for (int k = 0; k < TURNS; ++k) {
+      if (LN <= TB || w.q < TB) outs[w.wave][LN * k + w.q][w.in_wave] = y[k];
     }
     wave_fence();
-    if (MAP) continue;
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
       const int t = t0 + w.own(k);
-      float r = fmaf(D, x[k], y[k]);
-      if (gated) r *= v[k] * sigmoid(v[k]);
-      if (w.here && w.owner && t < w.last) out.store(t0, k, t < w.length ? r : 0.0f);
+      f2 r = *reinterpret_cast<const f2*>(&outs[w.wave][w.own(k)][2 * w.pair]) + D * now_x[k];
+      if (gated) r *= f2{now_v[k][0] * sigmoid(now_v[k][0]), now_v[k][1] * sigmoid(now_v[k][1])};
+      if (t >= w.length) r = f2{0.0f, 0.0f};
+      if (w.here2 && t < w.last) out.store(t0, k, r);
     }
   }
   if (!MAP) {
@@ -95,7 +119,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
     for (int t0 = gone; t0 < w.last; t0 += TB) {
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
-        if (w.here && w.owner && t0 + w.own(k) < w.last) out.store(t0, k, 0.0f);
+        if (w.here2 && t0 + w.own(k) < w.last) out.store(t0, k, f2{0.0f, 0.0f});
       }
     }
   }
