@@ -1,10 +1,11 @@
 """The short causal convolution of channels on torch tensors (vla_causal_conv of include/vla.h)."""
 import ctypes
+import functools
 
 from . import binding
 from .binding import VLA_BF16, VlaConvOpts, VlaError
-from .rows import (_all_aligned, _check_lengths, _check_rows, _check_vector, _fits, _io, _kind, _laid_rows, _no_tangents, _p, _plan, _plans, _record,
-                   _together, _wants_gradients)
+from .rows import (_all_aligned, _check_lengths, _check_rows, _check_vector, _fits, _io, _kind, _laid_rows, _like, _no_tangents, _p, _plan, _plans,
+                   _record, _together, _wants_gradients)
 
 _ACTIVATIONS = {"silu": 1, None: 0}
 
@@ -59,11 +60,17 @@ def _inputs(torch, key, x, weight, bias, state, lengths, activation):
     return kept, op
 
 
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(B, T, n, width, io):
+    """vla_causal_conv_workspace_bytes, which depends on nothing else."""
+    return binding.load_library().vla_causal_conv_workspace_bytes(B, T, n, width, io)
+
+
 def _forward(torch, kept, op, handle, outside):
     x, weight, bias, state, _ = kept
     B, T, n = x.shape
     width = weight.shape[1]
-    y = torch.empty((B, T, n), dtype=x.dtype, device=x.device)
+    y = _like(torch, x)
     state_T = torch.empty((B, width - 1, n), dtype=x.dtype, device=x.device)
     _record(outside, y, state_T)
     rc = binding.load_library().vla_causal_conv(x.data_ptr(), weight.data_ptr(), _p(bias), _p(state), y.data_ptr(), state_T.data_ptr(), B, T, n, width,
@@ -90,7 +97,7 @@ def causal_conv_step(x, weight, state, bias=None, *, activation="silu", stream=N
         (x, weight, bias, moved, _), op = _inputs(torch, key, x, weight, bias, state, None, activation)
         if moved is not state:
             raise ValueError("state must be 16-byte aligned: it is updated in place")
-        y = torch.empty((B, n), dtype=x.dtype, device=x.device)
+        y = _like(torch, x)
         _record(outside, y)
         rc = binding.load_library().vla_causal_conv_step(x.data_ptr(), weight.data_ptr(), _p(bias), state.data_ptr(), y.data_ptr(), B, n,
                                                          weight.shape[1], _io(torch, x), ctypes.byref(op), handle)
@@ -116,11 +123,11 @@ def _gradients(torch, x, weight, bias, state, dy, dstate_T, lengths, activation,
         lib, io = binding.load_library(), _io(torch, x)
         dy, op.y = _laid_rows(dy)
         dstate_T = None if dstate_T is None else _together(dstate_T)
-        dx = torch.empty((B, T, n), dtype=x.dtype, device=x.device)
+        dx = _like(torch, x)
         dweight = torch.empty_like(weight) if wanted[0] else None
         dbias = torch.empty_like(bias) if wanted[1] and bias is not None else None
         dstate = torch.empty_like(state) if wanted[2] and state is not None else None
-        need = lib.vla_causal_conv_workspace_bytes(B, T, n, width, io) if dweight is not None or dbias is not None else 0
+        need = _workspace_bytes(B, T, n, width, io) if dweight is not None or dbias is not None else 0
         ws = torch.empty((need,), dtype=torch.uint8, device=x.device) if need else None
         _record(outside, dx, dweight, dbias, dstate)
         rc = lib.vla_causal_conv_backward(x.data_ptr(), weight.data_ptr(), _p(bias), _p(state), dy.data_ptr(), _p(dstate_T), dx.data_ptr(),

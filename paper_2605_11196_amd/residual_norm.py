@@ -3,8 +3,8 @@ import ctypes
 
 from . import binding
 from .binding import VLA_BF16, VLA_F32, VlaError, VlaResidualOpts
-from .rows import (_all_aligned, _check_rows, _check_vector, _fits, _io, _kind, _laid_rows, _no_tangents, _p, _plan, _plans, _record, _together,
-                   _wants_gradients)
+from .rows import (_all_aligned, _check_rows, _check_vector, _fits, _io, _kind, _laid_rows, _like, _no_tangents, _p, _plan, _plans, _record,
+                   _together, _wants_gradients)
 
 _ACTIVATIONS = {"silu": 0, "sigmoid": 1}
 
@@ -71,8 +71,8 @@ def _forward(torch, kept, op, handle, outside):
     x, y, weight, post_weight, gate, scale = kept
     row = x if y is None else y
     B, T, n = row.shape
-    s = None if y is None else torch.empty((B, T, n), dtype=y.dtype if x is None else x.dtype, device=y.device)
-    h = None if weight is None else torch.empty((B, T, n), dtype=row.dtype, device=row.device)
+    s = None if y is None else _like(torch, y if x is None else x)
+    h = None if weight is None else _like(torch, row)
     _record(outside, s, h)
     rc = binding.load_library().vla_residual_norm(_p(x), _p(y), _p(gate), _p(post_weight), _p(scale), _p(weight), _p(s), _p(h), B, T, n,
                                                   _io(torch, row), ctypes.byref(op), handle)
@@ -100,7 +100,7 @@ def _gradients(torch, x, y, weight, post_weight, gate, scale, how, ds, dh, wante
             ds, op.s = _laid_rows(ds)
         if dh is not None:
             dh, op.h = _laid_rows(dh)
-        rows = [None if t is None or not w else torch.empty((B, T, n), dtype=t.dtype, device=t.device) for t, w in zip((x, y, gate), wanted[:2] + wanted[4:5])]
+        rows = [None if t is None or not w else _like(torch, t) for t, w in zip((x, y, gate), wanted[:2] + wanted[4:5])]
         sums = [None if t is None or not w else torch.empty_like(t) for t, w in zip((post_weight, scale, weight), (wanted[3], wanted[5], wanted[2]))]
         need = lib.vla_residual_norm_workspace_bytes(n) if any(t is not None for t in sums) else 0
         ws = torch.empty((need,), dtype=torch.uint8, device=row.device) if need else None

@@ -4,8 +4,8 @@ import functools
 
 from . import binding
 from .binding import VlaError, VlaScanOpts
-from .rows import (_all_aligned, _check_lengths, _check_rows, _check_vector, _fits, _io, _kind, _laid_groups, _laid_rows, _no_tangents, _p, _plan, _plans,
-                   _record, _together, _wants_gradients)
+from .rows import (_all_aligned, _check_lengths, _check_rows, _check_vector, _fits, _io, _kind, _laid_groups, _laid_rows, _like, _no_tangents, _p,
+                   _plan, _plans, _record, _together, _wants_gradients)
 
 
 def _grouped(x, dims):
@@ -93,7 +93,7 @@ def _forward(torch, kept, op, h0, save, handle, outside):
     N, dev, io = A.shape[1], u.device, _io(torch, u)
     lib = binding.load_library()
     h0 = _aligned(h0)
-    y = torch.empty((B, T, n), dtype=u.dtype, device=dev)
+    y = _like(torch, u)
     h_T = torch.empty((B, n, N), dtype=torch.float32, device=dev)
     saved = None
     if save:
@@ -152,7 +152,7 @@ def selective_scan_step(u, delta, A, B, C, h, D=None, z=None, *, delta_bias=None
         kept, op = _inputs(key, u, delta, A, B, C, D, z, delta_bias, None, softplus)
         u, delta, A, B, C, D, z, delta_bias, _ = kept
         batch, n = u.shape
-        y = torch.empty((batch, n), dtype=u.dtype, device=u.device)
+        y = _like(torch, u)
         _record(outside, y)
         rc = binding.load_library().vla_selective_scan_step(u.data_ptr(), delta.data_ptr(), A.data_ptr(), B.data_ptr(), C.data_ptr(), _p(D), _p(z),
                                                             _p(delta_bias), h.data_ptr(), y.data_ptr(), batch, n, A.shape[1], _io(torch, u),
@@ -181,12 +181,12 @@ def _gradients(torch, u, delta, A, Bm, Cm, D, z, delta_bias, saved, dy, dh_T, le
         lib = binding.load_library()
         (dy, op.y), dh_T, saved = _laid_rows(dy), _aligned(dh_T), _together(saved)
         op.saved, op.saved_bytes = saved.data_ptr(), saved.numel()
-        du, ddelta = (torch.empty((B, T, n), dtype=u.dtype, device=dev) for _ in range(2))
-        dz = torch.empty((B, T, n), dtype=u.dtype, device=dev) if z is not None else None
-        dB, dC = (torch.empty((B, T, G, N), dtype=u.dtype, device=dev) for _ in range(2))
-        dA = torch.empty((n, N), dtype=torch.float32, device=dev)
-        dD = torch.empty((n,), dtype=torch.float32, device=dev) if wanted[0] and D is not None else None
-        dbias = torch.empty((n,), dtype=torch.float32, device=dev) if wanted[1] and delta_bias is not None else None
+        du, ddelta = _like(torch, u), _like(torch, u)
+        dz = _like(torch, u) if z is not None else None
+        dB, dC = _like(torch, Bm), _like(torch, Cm)
+        dA = _like(torch, A)
+        dD = _like(torch, D) if wanted[0] and D is not None else None
+        dbias = _like(torch, delta_bias) if wanted[1] and delta_bias is not None else None
         dh0 = torch.empty((B, n, N), dtype=torch.float32, device=dev) if wanted[2] else None
         need = _workspace_bytes(B, T, n, N, io, G, segments, 1)
         ws = torch.empty((max(need, 16),), dtype=torch.uint8, device=dev)
