@@ -5,12 +5,15 @@
 //
 // Bound by memory: x is read and y written once (backward: x and dy read, dx written).  A thread holds 16 bytes of channels and goes
 // along a run of tokens with the window on registers, eight rows' loads under way at once; the W - 1 rows before a run are read again.
+// The taps of a thread's channels lie together and are loaded as fours: one by one they are 40 loads that all wait for the same unit (16384 rows
+// of 2048 in bf16: 43 -> 25.5 us, one token of 64 sequences, 4096 channels: 7.6 -> 3.5).  8 x 8192 rows of 4096: 207 us forward, 5.2 TB/s; 365
+// backward, 4.4 TB/s.
 #include "mixer_util.h"
 
 namespace vla {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kStepThreads = 64;
 constexpr int kAhead = 8;   // rows whose loads are under way at once
 
 template <typename IO>
@@ -18,17 +21,31 @@ struct Weights {
   static constexpr int V = kPiece<IO>;
   float w[kConvWidth][V], bias[V];
 
+  // the taps of V channels lie together
   template <int W> __device__ __forceinline__ void load(const ConvArgs& a, int c) {
+    float taps[V * W];
+    load_fours<V * W>(a, a.weight, static_cast<size_t>(c) * W, taps);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        const size_t at = static_cast<size_t>(c + i) * W + j;
-        w[j][i] = a.w_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.weight)[at]) : static_cast<const float*>(a.weight)[at];
+      for (int j = 0; j < W; ++j) w[j][i] = taps[i * W + j];
+      bias[i] = 0.0f;
+    }
+    if (a.bias != nullptr) load_fours<V>(a, a.bias, c, bias);
+  }
+  template <int COUNT> static __device__ __forceinline__ void load_fours(const ConvArgs& a, const void* p, size_t at, float* out) {
+    if (a.w_bf16) {
+#pragma unroll
+      for (int i = 0; i < COUNT; i += 4) {
+        const ushort4 x = *reinterpret_cast<const ushort4*>(static_cast<const uint16_t*>(p) + at + i);
+        out[i] = bf16_to_f32(x.x), out[i + 1] = bf16_to_f32(x.y), out[i + 2] = bf16_to_f32(x.z), out[i + 3] = bf16_to_f32(x.w);
       }
-      bias[i] = a.bias == nullptr ? 0.0f
-                : a.w_bf16        ? bf16_to_f32(static_cast<const uint16_t*>(a.bias)[c + i])
-                                  : static_cast<const float*>(a.bias)[c + i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < COUNT; i += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + at + i);
+        out[i] = x.x, out[i + 1] = x.y, out[i + 2] = x.z, out[i + 3] = x.w;
+      }
     }
   }
 };
@@ -197,9 +214,9 @@ __global__ void __launch_bounds__(kThreads) conv_backward_kernel(ConvArgs a) {
 
 // One token: the window moves on in place.
 template <int W, typename IO>
-__global__ void __launch_bounds__(kThreads) conv_step_kernel(ConvArgs a) {
+__global__ void __launch_bounds__(kStepThreads) conv_step_kernel(ConvArgs a) {
   constexpr int V = kPiece<IO>;
-  const Place p(a, V, static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x);
+  const Place p(a, V, static_cast<long long>(blockIdx.x) * kStepThreads + threadIdx.x);
   if (!p.here) return;
   IO* state = static_cast<IO*>(a.state_T) + static_cast<size_t>(p.b) * (W - 1) * a.n + p.c;
   Piece<IO> window[W];
@@ -229,7 +246,8 @@ hipError_t launch(const ConvArgs& a, int what, hipStream_t stream) {
                                    : reinterpret_cast<const void*>(&conv_backward_kernel<W, IO>);
   ConvArgs args = a;
   void* params[] = {&args};
-  return hipLaunchKernel(kernel, dim3(static_cast<unsigned>((items + kThreads - 1) / kThreads)), dim3(kThreads), params, 0, stream);
+  const int threads = what == 1 ? kStepThreads : kThreads;
+  return hipLaunchKernel(kernel, dim3(static_cast<unsigned>((items + threads - 1) / threads)), dim3(threads), params, 0, stream);
 }
 template <typename IO>
 hipError_t launch_width(const ConvArgs& a, int width, int what, hipStream_t stream) {

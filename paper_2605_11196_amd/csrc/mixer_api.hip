@@ -47,18 +47,18 @@ bool any_null(const void* const* p, int n) {
 
 // ---- short causal convolution
 
-// Tokens of a thread's run: long enough that the rows before it, read again, and its part of the weights' gradient weigh little, as
-// many runs as fill the card.
-int conv_run(int B, int T, int n, int io_dtype, int least) {
+// Tokens of a thread's run: 16, so that short and narrow calls fill the card (the backward pass of 3 x 1537 rows of 1664 in float32: runs of
+// 64 take 38 us, of 32 25, of 16 18), and longer ones as long as there are enough threads, so that the rows before a run, read again, and
+// its part of the weights' gradient weigh little.
+int conv_run(int B, int T, int n, int io_dtype) {
   const long long threads = static_cast<long long>(B) * (n / (16 / size_of(io_dtype)));
-  long long run = least;
+  long long run = 16;
   while (run < 256 && threads * (T / (2 * run)) >= 256 * 1024) run *= 2;
   return static_cast<int>(run < T ? run : T > 0 ? T : 1);
 }
 int runs_of(int T, int run) { return T > 0 ? (T + run - 1) / run : 1; }
-constexpr int kForwardRun = 16, kBackwardRun = 64;
 size_t conv_parts_bytes(int B, int T, int n, int width, int io_dtype) {
-  return static_cast<size_t>(B) * runs_of(T, conv_run(B, T, n, io_dtype, kBackwardRun)) * (width + 1) * n * 4;
+  return static_cast<size_t>(B) * runs_of(T, conv_run(B, T, n, io_dtype)) * (width + 1) * n * 4;
 }
 
 int conv_args(const void* x, const void* weight, const void* bias, const void* state, int B, int T, int n, int width, int io_dtype,
@@ -275,7 +275,7 @@ int vla_causal_conv(const void* x, const void* weight, const void* bias, const v
   if (!disjoint(r, 7, state, state_T)) return VLA_ERR_INVALID_ARG;
   a.y = y;
   a.state_T = state_T;
-  a.run = conv_run(B, T, n, io_dtype, kForwardRun);
+  a.run = conv_run(B, T, n, io_dtype);
   a.runs = runs_of(T, a.run);
   if (!conv_fits(a, io_dtype)) return VLA_ERR_UNSUPPORTED;
   return launched(vla::launch_causal_conv(a, width, io_dtype, static_cast<hipStream_t>(stream)));
@@ -322,7 +322,7 @@ int vla_causal_conv_backward(const void* x, const void* weight, const void* bias
   if (!disjoint(r, 12, nullptr, nullptr)) return VLA_ERR_INVALID_ARG;
   a.dy = dy; a.dstate_T = dstate_T; a.dx = dx; a.dstate = dstate;
   a.sum_part = sums ? static_cast<float*>(workspace) : nullptr;
-  a.run = conv_run(B, T, n, io_dtype, kBackwardRun);
+  a.run = conv_run(B, T, n, io_dtype);
   a.runs = runs_of(T, a.run);
   if (!conv_fits(a, io_dtype)) return VLA_ERR_UNSUPPORTED;
   const hipStream_t s = static_cast<hipStream_t>(stream);
