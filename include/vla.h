@@ -354,7 +354,8 @@ int vla_qk_norm_rope_backward(const void* q, const void* k, const void* q_weight
  *
  * Tensors [B, T, n]: n channels of T tokens, the rows that a projection gives (the heads of the recurrences above side by side).  Their strides are
  * a vla_strides whose h is 0; the rules above hold for them (16-byte pieces, written rows apart, all zero: contiguous; read rows may repeat).  n is a multiple
- * of 8.  `lengths` as in vla_delta_opts: what lies past the end of a sequence is not read, its outputs and gradients are 0.
+ * of 8.  `lengths` as in vla_delta_opts: what lies past the end of a sequence may hold anything (NaN too) and has no effect; outputs and gradients there
+ * are 0.
  */
 
 typedef struct vla_conv_opts {

@@ -82,7 +82,7 @@ int conv_args(const void* x, const void* weight, const void* bias, const void* s
   return VLA_OK;
 }
 bool conv_fits(const vla::ConvArgs& a, int io_dtype) {
-  return fits_launch(static_cast<long long>(a.B) * a.runs, a.n / (16 / static_cast<int>(size_of(io_dtype)))) &&
+  return static_cast<long long>(a.B) * a.runs <= 0x7fffffff && fits_launch(static_cast<long long>(a.B) * a.runs, a.n / (16 / static_cast<int>(size_of(io_dtype)))) &&
          static_cast<long long>(a.B) * a.runs * (a.n / (16 / static_cast<int>(size_of(io_dtype)))) < kMostItems - 256;
 }
 
@@ -102,7 +102,7 @@ int check_scan(int B, int T, int n, int N, int io_dtype, const vla_scan_opts& o)
   if (st == VLA_ERR_INVALID_ARG) return st;
   if (N <= 0 || o.groups <= 0 || n % o.groups != 0 || o.segments < 0) return VLA_ERR_INVALID_ARG;
   if (st != VLA_OK) return st;
-  if (!vla::scan_state_size(N) || n / o.groups % 8 != 0) return VLA_ERR_UNSUPPORTED;
+  if (!vla::scan_state_size(N) || n / o.groups % 8 != 0 || static_cast<long long>(n) * N > 0x7fffff00) return VLA_ERR_UNSUPPORTED;
   if (!fits_launch(static_cast<long long>(B) * o.groups * tiles_of(n, o.groups, vla::selective_tile(N)), 512)) return VLA_ERR_UNSUPPORTED;
   if (!fits_launch(static_cast<long long>(B) * n, N) || static_cast<long long>(B) * n * N > kMostItems - 256) return VLA_ERR_UNSUPPORTED;
   return VLA_OK;

@@ -28,7 +28,6 @@ struct ColumnSums {
 hipError_t launch_column_sums(const ColumnSums& s, hipStream_t stream);
 
 constexpr int kConvWidth = 4;        // taps at most
-constexpr int kConvPartials = 1024;  // rows of sum_part at most
 struct ConvArgs {
   const void* x;
   const void* weight;    // [n][width]
@@ -46,7 +45,6 @@ struct ConvArgs {
   int B, T, n, w_bf16, silu;
   int run, runs;         // tokens of a run, runs of a sequence
 };
-int conv_backward_run(int B, int T);
 hipError_t launch_causal_conv(const ConvArgs& a, int width, int io_dtype, hipStream_t stream);
 hipError_t launch_causal_conv_step(const ConvArgs& a, int width, int io_dtype, hipStream_t stream);
 hipError_t launch_causal_conv_backward(const ConvArgs& a, int width, int io_dtype, hipStream_t stream);
