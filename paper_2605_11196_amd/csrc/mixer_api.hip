@@ -108,7 +108,10 @@ int check_scan(int B, int T, int n, int N, int io_dtype, const vla_scan_opts& o)
   return VLA_OK;
 }
 
-// Time segments.  In segments the tokens are gone through twice (the second time without the read-out).
+// Time segments.  In segments the tokens are gone through twice (the second time without the read-out), which pays while sequences and channels
+// leave SIMDs idle: with fewer than 1400 waves on the card's 1024.  8 x 2048 tokens, 16 states, bfloat16, forward that saves and backward
+// together, whole and in segments: 1024 channels (512 waves) 887 us and 414, 2048 (1024) 923 and 819, 2560 (1280) 1189 and 1066, 3584 (1792) 1207 and 1436.
+// As many segments as give 8 waves a SIMD (2048 channels of one sequence of 16384: 16 segments 882 us, 64 838), of four blocks at least.
 struct ScanPlan {
   int n, tokens;             // segments, tokens of each: whole blocks
   size_t h_bytes, dt_bytes;  // of the states and the sums of steps
@@ -120,7 +123,7 @@ ScanPlan scan_plan(int B, int T, int n, int N, int groups, int requested) {
   long long s = requested;
   if (requested == 0) {
     s = 1;
-    if (waves < 1900) s = (8192 + waves - 1) / waves;
+    if (waves < 1400) s = (8192 + waves - 1) / waves;
     if (s > blocks / 4) s = blocks / 4;
   }
   if (s > blocks) s = blocks;

@@ -12,8 +12,6 @@ typedef float f2 __attribute__((ext_vector_type(2)));
 template <typename IO> constexpr int kPiece = 16 / sizeof(IO);
 
 __device__ __forceinline__ f2 widen(uint32_t b) { return f2{__uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)}; }
-__device__ __forceinline__ void store2(float* p, f2 x) { *reinterpret_cast<f2*>(p) = x; }
-__device__ __forceinline__ void store2(uint16_t* p, f2 x) { *reinterpret_cast<uint32_t*>(p) = pack_rne(x[0], x[1]); }
 
 // 16 bytes as they lie in memory, and their values
 template <typename IO> struct Piece;

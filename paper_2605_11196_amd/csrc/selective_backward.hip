@@ -96,6 +96,31 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
   };
   const int last = w.live > w.first ? w.first + (w.live - 1 - w.first) / TB * TB : w.first - TB;   // block
   if (last >= w.first) fetch(last);
+  // With many states a block's results are stored a block later, as in the forward pass (training steps of 8 x 2048 tokens: backward pass of 2048
+  // channels of 32 states 1025 -> 1000 us, of 1024 of 64 1140 -> 1078); with few of them the instructions between two blocks weigh more (4096 of
+  // 16: 910 us and 950).
+  constexpr bool LATER = N >= 32;
+  constexpr int PARTS = (TB * 2 * N + 64 * W - 1) / (64 * W);
+  Pair<IO> done_du[OWN] = {}, done_ddelta[OWN] = {}, done_dz[OWN] = {};
+  float done_BC[PARTS] = {};
+  const auto put = [&](int t0) {
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) {
+      if (w.here2 && t0 + w.own(k) < w.last) {
+        du_.store(t0, k, done_du[k]);
+        ddelta_.store(t0, k, done_ddelta[k]);
+        if (gated) dz_.store(t0, k, done_dz[k]);
+      }
+    }
+  };
+  const auto put_BC = [&](int t0) {
+    float* to = a.dBC_part + ((static_cast<size_t>(w.tile) * a.nb + w.b) * a.T + t0) * 2 * N;
+#pragma unroll
+    for (int j = 0; j < PARTS; ++j) {
+      const int i = threadIdx.x + j * 64 * W;
+      if (i < TB * 2 * N && t0 + i / (2 * N) < w.length) to[i] = done_BC[j];
+    }
+  };
   int turn = 0;
   for (int t0 = last; t0 >= w.first; t0 -= TB) {
     f2 x[OWN], raw[OWN], v[OWN], sig[OWN], d[OWN], dt_[OWN], e_[OWN];
@@ -117,6 +142,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
     }
     rows.put(mine, t0, w.length);
     f4 h = next_h;
+    if (!MAP && LATER && t0 < last) put(t0 + TB), put_BC(t0 + TB);
     if (t0 - TB >= w.first) fetch(t0 - TB);
     wave_fence();
     if constexpr (MAP) {
@@ -202,21 +228,24 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
           dD[j] += in ? e_[k][j] * x[k][j] : 0.0f;
           dbias[j] += ddelta[j];
         }
-        if (w.here2 && t < w.last) {
-          du_.store(t0, k, du);
-          ddelta_.store(t0, k, ddelta);
-          if (gated) dz_.store(t0, k, dz);
-        }
+        done_du[k] = narrow2<IO>(du);
+        done_ddelta[k] = narrow2<IO>(ddelta);
+        done_dz[k] = narrow2<IO>(dz);
       }
+      if (!LATER) put(t0);
       // dB and dC of the workgroup's channels: the waves in their order
       __syncthreads();
-      for (int i = threadIdx.x; i < TB * 2 * N; i += 64 * W) {
-        const int t = t0 + i / (2 * N);
-        float sum = 0.0f;
 #pragma unroll
-        for (int o = 0; o < W; ++o) sum += sums[turn][o][i / (2 * N)][i % (2 * N)];
-        if (t < w.length) a.dBC_part[((static_cast<size_t>(w.tile) * a.nb + w.b) * a.T + t) * 2 * N + i % (2 * N)] = sum;
+      for (int j = 0; j < PARTS; ++j) {
+        const int i = threadIdx.x + j * 64 * W;
+        float sum = 0.0f;
+        if (TB * 2 * N >= 64 * W || i < TB * 2 * N) {
+#pragma unroll
+          for (int o = 0; o < W; ++o) sum += sums[turn][o][i / (2 * N)][i % (2 * N)];
+        }
+        done_BC[j] = sum;
       }
+      if (!LATER) put_BC(t0);
       turn ^= 1;
     }
   }
@@ -225,12 +254,13 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
     *reinterpret_cast<f4*>(a.seg_h + of_seg * N + 4 * w.q) = g;
     if (w.q == 0) a.seg_dt[of_seg] = sum_dt;
   } else {
+    if (LATER && last >= w.first) put(w.first), put_BC(w.first);
     const int gone = w.live > w.first ? last + TB : w.first;
     for (int t0 = gone; t0 < w.last; t0 += TB) {
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
         if (w.here2 && t0 + w.own(k) < w.last) {
-          const f2 zero = {0.0f, 0.0f};
+          const Pair<IO> zero = {};
           du_.store(t0, k, zero);
           ddelta_.store(t0, k, zero);
           if (gated) dz_.store(t0, k, zero);

@@ -63,6 +63,10 @@ template <> struct PairOf<uint16_t> { typedef uint32_t type; };
 template <typename IO> using Pair = typename PairOf<IO>::type;
 __device__ __forceinline__ f2 wide2(f2 x) { return x; }
 __device__ __forceinline__ f2 wide2(uint32_t x) { return widen(x); }
+template <typename IO> __device__ __forceinline__ Pair<IO> narrow2(f2 x) {
+  if constexpr (sizeof(IO) == 2) return pack_rne(x[0], x[1]);
+  else return x;
+}
 
 // A [B, T, n] tensor seen from a lane: its own tokens' pairs of a block, from a base that goes along with the block.
 template <int N, typename IO>
@@ -90,7 +94,7 @@ struct ScanRows {
       }
     }
   }
-  __device__ __forceinline__ void store(int t0, int k, f2 x) const { store2(reinterpret_cast<IO*>(base + t0 * step + at[k]), x); }
+  __device__ __forceinline__ void store(int t0, int k, Pair<IO> x) const { *reinterpret_cast<Pair<IO>*>(base + t0 * step + at[k]) = x; }
 };
 
 // B and C of a block: a wave's lanes load N / 4 neighbouring values each and put them into LDS as float32, [token][B | C].

@@ -33,7 +33,9 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
   float sum_dt = 0.0f;
 
   // What a block reads is on its way while the one before the one before it is worked on, and its steps are formed while the one before it
-  // is: neither the loads' latency nor that of the transcendental instructions stands between the states' tokens.
+  // is: neither the loads' latency nor that of the transcendental instructions stands between the states' tokens.  Loads and stores are counted
+  // together and in order, so that a wait for loads is one for the stores before it: a block's results are stored a block later, between the
+  // wait for one block's rows and the loads of the next one's.
   Pair<IO> next_u[OWN] = {}, next_delta[OWN] = {}, next_z[OWN] = {};
   f2 x[OWN], v[OWN], now_x[OWN], now_v[OWN];
   const auto fetch = [&](int t0) {
@@ -60,11 +62,17 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
     form(w.first, 0);
     if (w.first + TB < w.live) fetch(w.first + TB);
   }
+  Pair<IO> done[OWN] = {};
+  const auto put = [&](int t0) {
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) {
+      if (w.here2 && t0 + w.own(k) < w.last) out.store(t0, k, done[k]);
+    }
+  };
+  const size_t kept_step = static_cast<size_t>(a.n) * N;
+  float* kept = a.kept + (static_cast<size_t>(w.b) * a.blocks + w.first / TB) * kept_step + static_cast<size_t>(w.c) * N + 4 * w.q;
   int now = 0;
   for (int t0 = w.first; t0 < w.live; t0 += TB) {
-    if (!MAP && a.kept != nullptr && w.here) {
-      *reinterpret_cast<f4*>(a.kept + ((static_cast<size_t>(w.b) * a.blocks + t0 / TB) * a.n + w.c) * N + 4 * w.q) = h;
-    }
     wave_fence();
     const f2* const step = steps[w.wave][now][0];
     const float* const mine = staged[w.wave][now][0];
@@ -83,6 +91,11 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
     }
     now ^= 1;
     form(t0 + TB, now);
+    if (!MAP && a.kept != nullptr) {
+      if (w.here) *reinterpret_cast<f4*>(kept) = h;
+      kept += kept_step;
+    }
+    if (!MAP && t0 > w.first) put(t0 - TB);
     if (t0 + 2 * TB < w.live) fetch(t0 + 2 * TB);
     float some[4], y[TURNS] = {};
 #pragma unroll
@@ -111,15 +124,16 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
       f2 r = *reinterpret_cast<const f2*>(&outs[w.wave][w.own(k)][2 * w.pair]) + D * now_x[k];
       if (gated) r *= f2{now_v[k][0] * sigmoid(now_v[k][0]), now_v[k][1] * sigmoid(now_v[k][1])};
       if (t >= w.length) r = f2{0.0f, 0.0f};
-      if (w.here2 && t < w.last) out.store(t0, k, r);
+      done[k] = narrow2<IO>(r);
     }
   }
   if (!MAP) {
     const int gone = w.live > w.first ? w.first + (w.live - w.first + TB - 1) / TB * TB : w.first;
+    if (gone > w.first) put(gone - TB);
     for (int t0 = gone; t0 < w.last; t0 += TB) {
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
-        if (w.here2 && t0 + w.own(k) < w.last) out.store(t0, k, f2{0.0f, 0.0f});
+        if (w.here2 && t0 + w.own(k) < w.last) out.store(t0, k, Pair<IO>{});
       }
     }
   }
