@@ -66,6 +66,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
   __shared__ __align__(16) float staged[W][TB][2 * N];   // B, C
   __shared__ __align__(16) float sums[2][MAP ? 1 : W][TB][2 * N];
   const P w(a);
+  if (MAP && w.seg == 0) return;      // nothing ends at its start
   const size_t state = (static_cast<size_t>(w.b) * a.n + w.c) * N + 4 * w.q, of_seg = (static_cast<size_t>(w.b) * a.n_seg + w.seg) * a.n + w.c;
   const bool gated = a.z != nullptr;
   const ScanRows<N, IO> u(w, a.u, a.us), delta(w, a.delta, a.ds), z(w, gated ? a.z : a.u, gated ? a.zs : a.us), dy(w, a.dy, a.ys);

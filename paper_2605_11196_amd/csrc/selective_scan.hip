@@ -20,6 +20,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
   __shared__ __align__(16) float staged[scan_waves(N)][2][TB][2 * N];   // B, C
   __shared__ __align__(8) float outs[MAP ? 1 : scan_waves(N)][TB][P::CW];            // sums of the read-out
   const P w(a);
+  if (MAP && w.seg == a.n_seg - 1) return;      // nothing starts from its end
   const size_t state = (static_cast<size_t>(w.b) * a.n + w.c) * N + 4 * w.q, of_seg = (static_cast<size_t>(w.b) * a.n_seg + w.seg) * a.n + w.c;
   const bool gated = !MAP && a.z != nullptr;
   const ScanRows<N, IO> u(w, a.u, a.us), delta(w, a.delta, a.ds), z(w, gated ? a.z : a.u, gated ? a.zs : a.us), out(w, MAP ? a.u : a.y, MAP ? a.us : a.ys);
@@ -146,7 +147,8 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
   }
 }
 
-// The states that the segments start from, in the place of their maps' ends; backward: the gradients behind them, from the last one on.
+// The states that the segments start from, in the place of their maps' ends; backward: the gradients behind them, from the last one on.  (The segment
+// that comes last has no map: what is read for it goes nowhere.)
 constexpr int kCombine = 256;
 template <bool BACK>
 __global__ void __launch_bounds__(kCombine) combine_kernel(ScanArgs a, int N) {
@@ -172,7 +174,8 @@ __global__ void __launch_bounds__(kCombine) combine_kernel(ScanArgs a, int N) {
       const int s = s0 + k, seg = BACK ? a.n_seg - 1 - s : s;
       if (s >= a.n_seg) break;
       ends[seg * each] = h;
-      h = fmaf(__builtin_amdgcn_exp2f(decay[k] * A2), h, end[k]);
+      // nothing of nothing is left, also where A > 0 has made the factor infinite
+      h = h == 0.0f ? end[k] : fmaf(__builtin_amdgcn_exp2f(decay[k] * A2), h, end[k]);
     }
   }
 }

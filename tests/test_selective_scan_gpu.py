@@ -250,3 +250,22 @@ def test_infinities_stay_in_their_channel():
     keep[[3, 7]] = False
     assert torch.equal(y[0][:, keep], want[0][0][:, keep]) and torch.equal(h[0][keep], want[1][0][keep]) and torch.equal(y[1], want[0][1])
     assert torch.isnan(y[0, 5:, 3]).all() and torch.equal(y[0, :5, 3], want[0][0, :5, 3]) and not torch.isfinite(y[0, :, 7]).any()
+
+
+def test_growing_states_that_are_zero_stay_zero():
+    """A > 0 and steps whose product over a segment overflows: an empty state has nothing to grow, in segments as in one piece, and the gradients have
+    nothing to go back to."""
+    B, T, n, N = 1, 40, 64, 16
+    s = make(B, T, n, N, "f32", D=False, gate=False, bias=False, carried=False, seed=8)
+    args = dict(s, A=torch.ones(n, N).cuda(), delta=torch.full((B, T, n), 30.0).cuda(), u=torch.zeros(B, T, n).cuda())
+    args["u"][:, -1] = s["u"][:, -1]
+    y, h, saved = vla.selective_scan_forward(*(args[k] for k in ("u", "delta", "A", "B", "C")), softplus=False, save_for_backward=True, segments=1)
+    assert torch.isfinite(y).all() and torch.isfinite(h).all() and (y[:, :-1] == 0).all() and (h != 0).all()
+    cut = vla.selective_scan_forward(*(args[k] for k in ("u", "delta", "A", "B", "C")), softplus=False, segments=5)
+    assert torch.equal(cut[0], y) and torch.equal(cut[1], h)
+    dy = torch.zeros(B, T, n).cuda()
+    dy[:, 0] = 1.0
+    whole, pieces = (vla.selective_scan_backward(*(args[k] for k in ("u", "delta", "A", "B", "C")), None, None, saved, dy, softplus=False, segments=k)
+                     for k in (1, 5))
+    for name, a, b in zip(("du", "ddelta", "dA", "dB", "dC"), whole, pieces):
+        assert torch.isfinite(a).all() and torch.equal(a, b), name
