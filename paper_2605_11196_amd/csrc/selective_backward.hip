@@ -72,7 +72,6 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
   const ScanRows<N, IO> u(w, a.u, a.us), delta(w, a.delta, a.ds), z(w, gated ? a.z : a.u, gated ? a.zs : a.us), dy(w, a.dy, a.ys);
   const ScanRows<N, IO> du_(w, MAP ? a.u : a.du, MAP ? a.us : a.dus), ddelta_(w, MAP ? a.u : a.ddelta, MAP ? a.us : a.dds),
       dz_(w, MAP || !gated ? a.u : a.dz, MAP || !gated ? a.us : a.dzs);
-  ScanStage<N, IO> rows(w, a);
   float* const mine = staged[w.wave][0];
   f4* const step = steps[w.wave][0];
 
@@ -84,6 +83,8 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
   float sum_dt = 0.0f;
   f2 dD = {0.0f, 0.0f}, dbias = dD;
 
+  const int last = w.live > w.first ? w.first + (w.live - 1 - w.first) / TB * TB : w.first - TB;   // block
+  ScanStage<N, IO> rows(w, a, last);
   // what a block reads is on its way while the one behind it is worked on
   Pair<IO> next_u[OWN] = {}, next_delta[OWN] = {}, next_z[OWN] = {}, next_dy[OWN] = {};
   f4 next_h = {};
@@ -92,10 +93,9 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
     delta.load(w, a.T, t0, next_delta);
     dy.load(w, a.T, t0, next_dy);
     if (gated) z.load(w, a.T, t0, next_z);
-    rows.load(a.T, t0);
+    rows.template load<true>(a.T, t0);
     if (!MAP) next_h = *reinterpret_cast<const f4*>(a.kept + ((static_cast<size_t>(w.b) * a.blocks + t0 / TB) * a.n + w.c) * N + 4 * w.q);
   };
-  const int last = w.live > w.first ? w.first + (w.live - 1 - w.first) / TB * TB : w.first - TB;   // block
   if (last >= w.first) fetch(last);
   // With many states a block's results are stored a block later, as in the forward pass (training steps of 8 x 2048 tokens: backward pass of 2048
   // channels of 32 states 1025 -> 1000 us, of 1024 of 64 1140 -> 1078); with few of them the instructions between two blocks weigh more (4096 of

@@ -63,6 +63,8 @@ template <> struct PairOf<uint16_t> { typedef uint32_t type; };
 template <typename IO> using Pair = typename PairOf<IO>::type;
 __device__ __forceinline__ f2 wide2(f2 x) { return x; }
 __device__ __forceinline__ f2 wide2(uint32_t x) { return widen(x); }
+__device__ __forceinline__ f2 or_zero(bool in, f2 x) { return f2{in ? x[0] : 0.0f, in ? x[1] : 0.0f}; }
+__device__ __forceinline__ uint32_t or_zero(bool in, uint32_t x) { return in ? x : 0u; }
 template <typename IO> __device__ __forceinline__ Pair<IO> narrow2(f2 x) {
   if constexpr (sizeof(IO) == 2) return pack_rne(x[0], x[1]);
   else return x;
@@ -101,20 +103,26 @@ struct ScanRows {
 template <int N, typename IO>
 struct ScanStage {
   static constexpr int V = N / 4, WORDS = V * sizeof(IO) / 4;
-  const char* from;        // of the sequence, this lane's piece of a row
-  long long step;
+  const char* row;         // this lane's piece of its token's row
+  long long step;          // bytes from token to token
   int t, at;               // token of the block, float of the row
   uint32_t raw[WORDS];
-  __device__ __forceinline__ ScanStage(const ScanPlace<N>& w, const ScanArgs& a) {
+  // row: of the block at t0
+  __device__ __forceinline__ ScanStage(const ScanPlace<N>& w, const ScanArgs& a, int t0) {
     t = w.lane / 8;
     at = w.lane % 8 * V;
     const bool is_c = at >= N;
     step = (is_c ? a.C_t : a.B_t) * static_cast<long long>(sizeof(IO));
-    from = is_c ? static_cast<const char*>(a.Cm) + (w.b * a.C_b + w.group * a.C_g + (at - N)) * static_cast<long long>(sizeof(IO))
-                : static_cast<const char*>(a.Bm) + (w.b * a.B_b + w.group * a.B_g + at) * static_cast<long long>(sizeof(IO));
+    row = (is_c ? static_cast<const char*>(a.Cm) + (w.b * a.C_b + w.group * a.C_g + (at - N)) * static_cast<long long>(sizeof(IO))
+                : static_cast<const char*>(a.Bm) + (w.b * a.B_b + w.group * a.B_g + at) * static_cast<long long>(sizeof(IO))) + (t0 + t) * step;
   }
+  // the rows of block t0 (past the end of memory the last one), to which `row` points; `row` goes on to the next block (BACK: to the one before)
+  template <bool BACK>
   __device__ __forceinline__ void load(int T, int t0) {
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(from + min(t0 + t, T - 1) * step);
+    const char* from = row;
+    if (t0 + TB > T) from -= max(t0 + t - (T - 1), 0) * step;
+    row = BACK ? row - TB * step : row + TB * step;
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(from);
     if constexpr (WORDS == 1) {
       raw[0] = *p;
     } else if constexpr (WORDS == 2) {
@@ -133,12 +141,15 @@ struct ScanStage {
   // rows: the wave's own [TB][2 N]; tokens past the end of the sequence give zeros
   __device__ __forceinline__ void put(float* rows, int t0, int length) const {
     const bool in = t0 + t < length;
+    uint32_t kept[WORDS];
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) kept[i] = in ? raw[i] : 0u;
 #pragma unroll
     for (int i = 0; i < V; i += 2) {
       f2 x;
-      if constexpr (sizeof(IO) == 2) x = widen(raw[i / 2]);
-      else x = f2{__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])};
-      *reinterpret_cast<f2*>(rows + t * 2 * N + at + i) = f2{in ? x[0] : 0.0f, in ? x[1] : 0.0f};
+      if constexpr (sizeof(IO) == 2) x = widen(kept[i / 2]);
+      else x = f2{__uint_as_float(kept[i]), __uint_as_float(kept[i + 1])};
+      *reinterpret_cast<f2*>(rows + t * 2 * N + at + i) = x;
     }
   }
 };

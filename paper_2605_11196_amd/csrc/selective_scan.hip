@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
   const size_t state = (static_cast<size_t>(w.b) * a.n + w.c) * N + 4 * w.q, of_seg = (static_cast<size_t>(w.b) * a.n_seg + w.seg) * a.n + w.c;
   const bool gated = !MAP && a.z != nullptr;
   const ScanRows<N, IO> u(w, a.u, a.us), delta(w, a.delta, a.ds), z(w, gated ? a.z : a.u, gated ? a.zs : a.us), out(w, MAP ? a.u : a.y, MAP ? a.us : a.ys);
-  ScanStage<N, IO> rows(w, a);
+  ScanStage<N, IO> rows(w, a, w.first);
 
   const f4 A2 = *reinterpret_cast<const f4*>(a.A + static_cast<size_t>(w.c) * N + 4 * w.q) * kLog2e;
   f4 h = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -43,18 +43,18 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
     u.load(w, a.T, t0, next_u);
     delta.load(w, a.T, t0, next_delta);
     if (gated) z.load(w, a.T, t0, next_z);
-    rows.load(a.T, t0);
+    rows.template load<false>(a.T, t0);
   };
   const auto form = [&](int t0, int buffer) {
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
       const bool in = t0 + w.own(k) < w.length;
-      x[k] = wide2(next_u[k]);
+      x[k] = wide2(or_zero(in, next_u[k]));
       v[k] = wide2(next_z[k]);
       const f2 raw = wide2(next_delta[k]) + bias;
       const float d0 = a.softplus ? softplus(raw[0]) : raw[0], d1 = a.softplus ? softplus(raw[1]) : raw[1];
       *reinterpret_cast<f4*>(&steps[w.wave][buffer][w.own(k)][2 * w.pair]) =
-          f4{in ? d0 : 0.0f, in ? d0 * x[k][0] : 0.0f, in ? d1 : 0.0f, in ? d1 * x[k][1] : 0.0f};
+          f4{in ? d0 : 0.0f, (in ? d0 : 0.0f) * x[k][0], in ? d1 : 0.0f, (in ? d1 : 0.0f) * x[k][1]};
     }
     rows.put(staged[w.wave][buffer][0], t0, w.length);
   };
@@ -124,8 +124,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
       const int t = t0 + w.own(k);
       f2 r = *reinterpret_cast<const f2*>(&outs[w.wave][w.own(k)][2 * w.pair]) + D * now_x[k];
       if (gated) r *= f2{now_v[k][0] * sigmoid(now_v[k][0]), now_v[k][1] * sigmoid(now_v[k][1])};
-      if (t >= w.length) r = f2{0.0f, 0.0f};
-      done[k] = narrow2<IO>(r);
+      done[k] = or_zero(t < w.length, narrow2<IO>(r));
     }
   }
   if (!MAP) {
