@@ -71,9 +71,6 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
   if (MAP && w.seg == 0) return;      // nothing ends at its start
   const size_t state = (static_cast<size_t>(w.b) * a.n + w.c) * N + 4 * w.q, of_seg = (static_cast<size_t>(w.b) * a.n_seg + w.seg) * a.n + w.c;
   const bool gated = a.z != nullptr;
-  const ScanRows<N, IO> u(w, a.u, a.us), delta(w, a.delta, a.ds), z(w, gated ? a.z : a.u, gated ? a.zs : a.us), dy(w, a.dy, a.ys);
-  const ScanRows<N, IO> du_(w, MAP ? a.u : a.du, MAP ? a.us : a.dus), ddelta_(w, MAP ? a.u : a.ddelta, MAP ? a.us : a.dds),
-      dz_(w, MAP || !gated ? a.u : a.dz, MAP || !gated ? a.us : a.dzs);
   float* const mine = staged[w.wave][0];
   f4* const step = steps[w.wave][0];
 
@@ -87,15 +84,19 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
 
   const int last = w.live > w.first ? w.first + (w.live - 1 - w.first) / TB * TB : w.first - TB;   // block
   ScanStage<N, IO> rows(w, a, last);
+  const ScanRows<N, IO> u(w, a.u, a.us), delta(w, a.delta, a.ds), z(w, gated ? a.z : a.u, gated ? a.zs : a.us), dy(w, a.dy, a.ys);
+  const ScanRows<N, IO> du_(w, MAP ? a.u : a.du, MAP ? a.us : a.dus), ddelta_(w, MAP ? a.u : a.ddelta, MAP ? a.us : a.dds),
+      dz_(w, MAP || !gated ? a.u : a.dz, MAP || !gated ? a.us : a.dzs);
   // what a block reads is on its way while the one behind it is worked on
   Pair<IO> next_u[OWN] = {}, next_delta[OWN] = {}, next_z[OWN] = {}, next_dy[OWN] = {};
   f4 next_h = {};
-  const auto fetch = [&](int t0) {
-    u.load(w, a.T, t0, next_u);
-    delta.load(w, a.T, t0, next_delta);
-    dy.load(w, a.T, t0, next_dy);
-    if (gated) z.load(w, a.T, t0, next_z);
-    rows.template load<true>(a.T, t0);
+  const auto fetch = [&](int t0) {      // the blocks one after the other
+    u.load(next_u, w, a.T, t0);
+    delta.load(next_delta, w, a.T, t0);
+    dy.load(next_dy, w, a.T, t0);
+    if (gated) z.load(next_z, w, a.T, t0);
+    rows.load(a.T - t0);
+    rows.template go<true>();
     if (!MAP) next_h = *reinterpret_cast<const f4*>(a.kept + ((static_cast<size_t>(w.b) * a.blocks + t0 / TB) * a.n + w.c) * N + 4 * w.q);
   };
   if (last >= w.first) fetch(last);
@@ -110,9 +111,9 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
       if (w.here2 && t0 + w.own(k) < w.last) {
-        du_.store(t0, k, done_du[k]);
-        ddelta_.store(t0, k, done_ddelta[k]);
-        if (gated) dz_.store(t0, k, done_dz[k]);
+        du_.store(du_.row(t0), k, done_du[k]);
+        ddelta_.store(ddelta_.row(t0), k, done_ddelta[k]);
+        if (gated) dz_.store(dz_.row(t0), k, done_dz[k]);
       }
     }
   };
@@ -264,9 +265,9 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
       for (int k = 0; k < OWN; ++k) {
         if (w.here2 && t0 + w.own(k) < w.last) {
           const Pair<IO> zero = {};
-          du_.store(t0, k, zero);
-          ddelta_.store(t0, k, zero);
-          if (gated) dz_.store(t0, k, zero);
+          du_.store(du_.row(t0), k, zero);
+          ddelta_.store(ddelta_.row(t0), k, zero);
+          if (gated) dz_.store(dz_.row(t0), k, zero);
         }
       }
     }

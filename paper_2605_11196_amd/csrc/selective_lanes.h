@@ -70,25 +70,34 @@ template <typename IO> __device__ __forceinline__ Pair<IO> narrow2(f2 x) {
   else return x;
 }
 
-// A [B, T, n] tensor seen from a lane: its own tokens' pairs of a block, from a base that goes along with the block.
+// A [B, T, n] tensor seen from a lane: its own tokens' pairs of a block, from the block's first token on (`row`).
 template <int N, typename IO>
 struct ScanRows {
   static constexpr int OWN = ScanPlace<N>::OWN;
   char* base;              // of the sequence
   long long step;          // bytes from token to token
-  unsigned at[OWN];        // bytes from the block's first token
+  unsigned at[OWN];        // bytes from a block's first token
   __device__ __forceinline__ ScanRows(const ScanPlace<N>& w, const void* p, Row2 r) {
     base = const_cast<char*>(static_cast<const char*>(p)) + w.b * r.b * static_cast<long long>(sizeof(IO));
     step = r.t * static_cast<long long>(sizeof(IO));
 #pragma unroll
     for (int k = 0; k < OWN; ++k) at[k] = w.own(k) * static_cast<unsigned>(step) + w.c2 * static_cast<unsigned>(sizeof(IO));
   }
-  // the rows of block t0 (past the end of memory the last one)
-  __device__ __forceinline__ void load(const ScanPlace<N>& w, int T, int t0, Pair<IO> (&v)[OWN]) const {
-    const char* from = base + t0 * step;
-    if (t0 + TB <= T) {
+  __device__ __forceinline__ char* row(int t0) const { return base + t0 * step; }
+  __device__ __forceinline__ void load(const char* row, Pair<IO> (&v)[OWN]) const {
 #pragma unroll
-      for (int k = 0; k < OWN; ++k) v[k] = *reinterpret_cast<const Pair<IO>*>(from + at[k]);
+    for (int k = 0; k < OWN; ++k) v[k] = *reinterpret_cast<const Pair<IO>*>(row + at[k]);
+  }
+  // of a block with `tokens` of them, the rest of its rows being the last one
+  __device__ __forceinline__ void load(const char* row, Pair<IO> (&v)[OWN], const ScanPlace<N>& w, int tokens) const {
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) v[k] = *reinterpret_cast<const Pair<IO>*>(row + (at[k] - max(w.own(k) - (tokens - 1), 0) * static_cast<unsigned>(step)));
+  }
+  // either, with the choice between their addresses: fewer registers than two ways
+  __device__ __forceinline__ void load(Pair<IO> (&v)[OWN], const ScanPlace<N>& w, int T, int t0) const {
+    const char* from = row(t0);
+    if (t0 + TB <= T) {
+      load(from, v);
     } else {
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
@@ -96,7 +105,7 @@ struct ScanRows {
       }
     }
   }
-  __device__ __forceinline__ void store(int t0, int k, Pair<IO> x) const { *reinterpret_cast<Pair<IO>*>(base + t0 * step + at[k]) = x; }
+  __device__ __forceinline__ void store(char* row, int k, Pair<IO> x) const { *reinterpret_cast<Pair<IO>*>(row + at[k]) = x; }
 };
 
 // B and C of a block: a wave's lanes load N / 4 neighbouring values each and put them into LDS as float32, [token][B | C].
@@ -116,13 +125,10 @@ struct ScanStage {
     row = (is_c ? static_cast<const char*>(a.Cm) + (w.b * a.C_b + w.group * a.C_g + (at - N)) * static_cast<long long>(sizeof(IO))
                 : static_cast<const char*>(a.Bm) + (w.b * a.B_b + w.group * a.B_g + at) * static_cast<long long>(sizeof(IO))) + (t0 + t) * step;
   }
-  // the rows of block t0 (past the end of memory the last one), to which `row` points; `row` goes on to the next block (BACK: to the one before)
-  template <bool BACK>
-  __device__ __forceinline__ void load(int T, int t0) {
-    const char* from = row;
-    if (t0 + TB > T) from -= max(t0 + t - (T - 1), 0) * step;
-    row = BACK ? row - TB * step : row + TB * step;
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(from);
+  template <bool BACK> __device__ __forceinline__ void go() { row = BACK ? row - TB * step : row + TB * step; }
+  // of a block with `tokens` of them (TB: all), the rest of its rows being the last one
+  __device__ __forceinline__ void load(int tokens) {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(tokens < TB ? row - max(t - (tokens - 1), 0) * step : row);
     if constexpr (WORDS == 1) {
       raw[0] = *p;
     } else if constexpr (WORDS == 2) {

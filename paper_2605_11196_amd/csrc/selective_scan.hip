@@ -26,6 +26,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
   const size_t state = (static_cast<size_t>(w.b) * a.n + w.c) * N + 4 * w.q, of_seg = (static_cast<size_t>(w.b) * a.n_seg + w.seg) * a.n + w.c;
   const bool gated = !MAP && a.z != nullptr;
   const ScanRows<N, IO> u(w, a.u, a.us), delta(w, a.delta, a.ds), z(w, gated ? a.z : a.u, gated ? a.zs : a.us), out(w, MAP ? a.u : a.y, MAP ? a.us : a.ys);
+  char *next_row_u = u.row(w.first), *next_row_delta = delta.row(w.first), *next_row_z = z.row(w.first), *row_out = out.row(w.first);
   ScanStage<N, IO> rows(w, a, w.first);
 
   const f4 A2 = *reinterpret_cast<const f4*>(a.A + static_cast<size_t>(w.c) * N + 4 * w.q) * kLog2e;
@@ -41,22 +42,40 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
   // wait for one block's rows and the loads of the next one's.
   Pair<IO> next_u[OWN] = {}, next_delta[OWN] = {}, next_z[OWN] = {};
   f2 x[OWN], v[OWN], now_x[OWN], now_v[OWN];
-  const auto fetch = [&](int t0) {
-    u.load(w, a.T, t0, next_u);
-    delta.load(w, a.T, t0, next_delta);
-    if (gated) z.load(w, a.T, t0, next_z);
-    rows.template load<false>(a.T, t0);
+  const auto fetch = [&](int t0) {      // the blocks one after the other
+    if (t0 + TB <= a.T) {
+      u.load(next_row_u, next_u);
+      delta.load(next_row_delta, next_delta);
+      if (gated) z.load(next_row_z, next_z);
+      rows.load(TB);
+    } else {
+      const int tokens = a.T - t0;
+      u.load(next_row_u, next_u, w, tokens);
+      delta.load(next_row_delta, next_delta, w, tokens);
+      if (gated) z.load(next_row_z, next_z, w, tokens);
+      rows.load(tokens);
+      asm volatile("" ::: "memory");      // two ways with loads of their own, and no choice of addresses for one
+    }
+    next_row_u += TB * u.step;
+    next_row_delta += TB * delta.step;
+    next_row_z += TB * z.step;
+    rows.template go<false>();
   };
   const auto form = [&](int t0, int buffer) {
+    f2 dt[OWN];
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) dt[k] = wide2(next_delta[k]) + bias;
+    if (a.softplus) {
+#pragma unroll
+      for (int k = 0; k < OWN; ++k) dt[k] = f2{softplus(dt[k][0]), softplus(dt[k][1])};
+    }
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
       const bool in = t0 + w.own(k) < w.length;
       x[k] = wide2(or_zero(in, next_u[k]));
       v[k] = wide2(next_z[k]);
-      const f2 raw = wide2(next_delta[k]) + bias;
-      const float d0 = a.softplus ? softplus(raw[0]) : raw[0], d1 = a.softplus ? softplus(raw[1]) : raw[1];
-      *reinterpret_cast<f4*>(&steps[w.wave][buffer][w.own(k)][2 * w.pair]) =
-          f4{in ? d0 : 0.0f, (in ? d0 : 0.0f) * x[k][0], in ? d1 : 0.0f, (in ? d1 : 0.0f) * x[k][1]};
+      const f2 d = or_zero(in, dt[k]);
+      *reinterpret_cast<f4*>(&steps[w.wave][buffer][w.own(k)][2 * w.pair]) = f4{d[0], d[0] * x[k][0], d[1], d[1] * x[k][1]};
     }
     rows.put(staged[w.wave][buffer][0], t0, w.length);
   };
@@ -69,8 +88,9 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
   const auto put = [&](int t0) {
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
-      if (w.here2 && t0 + w.own(k) < w.last) out.store(t0, k, done[k]);
+      if (w.here2 && t0 + w.own(k) < w.last) out.store(row_out, k, done[k]);
     }
+    row_out += TB * out.step;
   };
   const size_t kept_step = static_cast<size_t>(a.n) * N;
   float* kept = a.kept + (static_cast<size_t>(w.b) * a.blocks + w.first / TB) * kept_step + static_cast<size_t>(w.c) * N + 4 * w.q;
@@ -135,8 +155,9 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
     for (int t0 = gone; t0 < w.last; t0 += TB) {
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
-        if (w.here2 && t0 + w.own(k) < w.last) out.store(t0, k, Pair<IO>{});
+        if (w.here2 && t0 + w.own(k) < w.last) out.store(row_out, k, Pair<IO>{});
       }
+      row_out += TB * out.step;
     }
   }
   if (!w.here) return;
