@@ -29,10 +29,12 @@ __device__ __forceinline__ void swap16(float& a, float& b) {
   a = __uint_as_float(r[0]);
   b = __uint_as_float(r[1]);
 }
-// p[4 j + i], tokens j = 0, 1 and states i of a lane, summed over the wave's channels.  Into row[j][4 q + i] (step: floats between the two rows):
-// lane bits 5, 4 and 3 (LN = 16: 5 and 4) come to say which of the numbers a lane has.
+// p[4 j + i], tokens 2 pair + j and states i of a lane, summed over the wave's channels, into rows[token][4 q + i] (step: floats from row to row): lane
+// bits 5, 4 and 3 (LN = 16: 5 and 4) come to say which of the numbers a lane has.  LN = 4: bit 2 too, for the two pairs of four tokens, of which the
+// first one's numbers wait in `half` for the last one's.  A rotation by four lanes takes bit 3 along for one half of the lanes, which does not matter as
+// long as the sum over bit 3 is still to come.
 template <int LN>
-__device__ __forceinline__ void wave_sums(const float (&p)[8], float* row, int step, int lane) {
+__device__ __forceinline__ void wave_sums(const float (&p)[8], float (&half)[2], bool last, int pair, float* rows, int step, int lane) {
   float x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = p[i];
@@ -47,15 +49,35 @@ __device__ __forceinline__ void wave_sums(const float (&p)[8], float* row, int s
     x[i] += x[i + 2];
   }
   const int q = lane % LN;
-  float* to = row + (lane / 32) * step + 4 * q + (lane / 16 % 2) * 2;
+  const bool odd = lane & 8;
+  if constexpr (LN == 4) {
+    if (!last) {
+      half[0] = x[0];
+      half[1] = x[1];
+      return;
+    }
+    const bool second = lane & 4;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float a = pair % 2 ? half[i] : x[i], b = pair % 2 ? x[i] : half[i], keep = second ? b : a, send = second ? a : b;
+      x[i] = keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(send), 0x124, 0xf, 0xf, true));
+    }
+    const float keep = odd ? x[1] : x[0], send = odd ? x[0] : x[1];
+    const float sum = keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(send), 0x128, 0xf, 0xf, true));
+    float* to = rows + (lane / 4 % 2 * 2 + lane / 32) * step + 4 * q + lane / 16 % 2 * 2 + lane / 8 % 2;
+    to[pair / 2 * 4 * step] = sum;
+    return;
+  }
+  float* to = rows + (2 * pair + lane / 32) * step + 4 * q + (lane / 16 % 2) * 2;
   if constexpr (LN == 16) {
     *reinterpret_cast<f2*>(to) = f2{x[0], x[1]};
-  } else {
-    const bool odd = lane & 8;
+  } else if constexpr (LN != 4) {
     const float keep = odd ? x[1] : x[0], send = odd ? x[0] : x[1];
     float sum = keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(send), 0x128, 0xf, 0xf, true));
-    if constexpr (LN <= 4) sum += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(sum), 0x104, 0xf, 0xf, true));   // from four lanes on
-    if constexpr (LN <= 2) sum = dpp_sum<0x4E>(sum);
+    if constexpr (LN == 2) {
+      sum += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(sum), 0x104, 0xf, 0xf, true));   // from four lanes on
+      sum = dpp_sum<0x4E>(sum);
+    }
     if (LN == 8 || (lane & 7 & ~(LN - 1)) == 0) to[odd ? 1 : 0] = sum;
   }
 }
@@ -162,7 +184,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
     } else {
       float* const own_sums = sums[turn][w.wave][0];
       f4 decay[TB], decayed[TB];   // a, a h_{t-1}
-      float p[2][8], some[2][4], y[TURNS] = {}, through[TURNS] = {}, rate[TURNS] = {};
+      float p[2][8], half[2], some[2][4], y[TURNS] = {}, through[TURNS] = {}, rate[TURNS] = {};
       // the operands of a token are on their way from LDS while the one before it is worked on; more of them would not fit
       f4 s_[2], B_[2], C_[2];
       const auto operands = [&](int t) {
@@ -186,10 +208,10 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
         }
         keep_sum<LN>(read, some[0], y, t, t % LN == LN - 1, w.q);
         // the sums of the pair of tokens before lie between the work on this one
-        if (t % 2 == 0 && t > 0) wave_sums<LN>(p[(t / 2 - 1) % 2], own_sums + (t - 2) * 2 * N + N, 2 * N, w.lane);
+        if (t % 2 == 0 && t > 0) wave_sums<LN>(p[(t / 2 - 1) % 2], half, t / 2 % 2 == 0, t / 2 - 1, own_sums + N, 2 * N, w.lane);
         if (t % 2) __builtin_amdgcn_sched_barrier(0);
       }
-      wave_sums<LN>(p[1], own_sums + (TB - 2) * 2 * N + N, 2 * N, w.lane);
+      wave_sums<LN>(p[1], half, true, TB / 2 - 1, own_sums + N, 2 * N, w.lane);
 #pragma unroll
       for (int t = TB - 1; t >= 0; --t) {
         if (t > 0) operands(t - 1);
@@ -207,10 +229,10 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
         }
         keep_sum<LN>(sum_p, some[0], through, t, t % LN == 0, w.q);
         keep_sum<LN>(sum_r, some[1], rate, t, t % LN == 0, w.q);
-        if (t % 2 && t < TB - 1) wave_sums<LN>(p[(t / 2 + 1) % 2], own_sums + (t + 1) * 2 * N, 2 * N, w.lane);
+        if (t % 2 && t < TB - 1) wave_sums<LN>(p[(t / 2 + 1) % 2], half, t / 2 % 2 == 1, t / 2 + 1, own_sums, 2 * N, w.lane);
         if (t % 2 == 0) __builtin_amdgcn_sched_barrier(0);
       }
-      wave_sums<LN>(p[0], own_sums, 2 * N, w.lane);
+      wave_sums<LN>(p[0], half, true, 0, own_sums, 2 * N, w.lane);
       wave_fence();
 #pragma unroll
       for (int k = 0; k < TURNS; ++k) {
