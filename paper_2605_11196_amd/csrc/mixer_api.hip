@@ -494,7 +494,7 @@ void vla_residual_default_opts(vla_residual_opts* opts) {
 }
 
 size_t vla_residual_norm_workspace_bytes(int n) {
-  return n > 0 && n % 8 == 0 && n <= vla::kResidualColumns ? static_cast<size_t>(vla::kResidualPartials) * 3 * n * 4 : 0;
+  return n > 0 && n % 8 == 0 && n <= vla::kResidualColumns ? static_cast<size_t>(vla::residual_partials(n)) * 3 * n * 4 : 0;
 }
 
 int vla_residual_norm(const void* x, const void* y, const void* gate, const void* post_weight, const void* scale, const void* weight, void* s,

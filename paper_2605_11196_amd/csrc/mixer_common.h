@@ -97,7 +97,6 @@ hipError_t launch_selective_backward(const ScanArgs& a, int N, int io_dtype, boo
 hipError_t launch_selective_shared(const ScanArgs& a, int N, int io_dtype, hipStream_t stream);
 inline bool scan_state_size(int N) { return N == 8 || N == 16 || N == 32 || N == 64; }
 
-constexpr int kResidualPartials = 512;   // workgroups of the backward pass at most: rows of sum_part
 constexpr int kResidualColumns = 8192;  // columns of a row at most
 struct ResidualArgs {
   const void* x;            // the residual stream, or nullptr
@@ -119,6 +118,7 @@ struct ResidualArgs {
   int w_bf16, act;          // act 0: silu, 1: sigmoid
   float eps;
 };
+int residual_partials(int n);   // workgroups of the backward pass at most: rows of sum_part
 hipError_t launch_residual_norm(const ResidualArgs& a, int io_dtype, int stream_dtype, hipStream_t stream);
 hipError_t launch_residual_norm_backward(const ResidualArgs& a, int io_dtype, int stream_dtype, int* parts, hipStream_t stream);
 

@@ -67,7 +67,8 @@ struct RawWeight {
 };
 template <typename IO> __device__ __forceinline__ void store8(IO* p, const Eight& e) { store_piece(p, e.v); }
 
-// Where a lane is in its workgroup, and the sums over its row and over its group of columns.
+// Where a lane is in its workgroup, and the sums over its row and over its group of columns.  WHOLE: the row fills the workgroup, four waves or more.
+template <bool WHOLE>
 struct RowLanes {
   int L, lane, row, rows, pieces, each;   // lanes of a row, this one's place, its row among the workgroup's; eights of a row and of a group
   float* whole;                           // LDS: [4][2][16]
@@ -98,30 +99,30 @@ struct RowLanes {
     __syncthreads();
   }
   __device__ __forceinline__ Eight weight(int which, int c) const { return load8(weights + which * pieces * kColumns + c); }
-  // a, b summed over the row, in every lane of it.  `at`: a place in LDS; between two visits of one place lies the barrier of another
+  // a (and b) summed over the row, in every lane of it.  `at`: a place in LDS; between two visits of one place lies the barrier of another.  The sums of
+  // the waves are read by 16 lanes and added up like the lanes' own, which is sooner done than a loop over them.
+  template <bool TWO>
   __device__ __forceinline__ void row_sums(float& a, float& b, int at) const {
-    a = group_sum(a, L < 64 ? L : 64);
-    b = group_sum(b, L < 64 ? L : 64);
-    if (L <= 64) return;
-    const int waves = L / 64, wave = threadIdx.x / 64;
+    const int lanes = WHOLE || L > 64 ? 64 : L;
+    a = group_sum(a, lanes);
+    if (TWO) b = group_sum(b, lanes);
+    if (!WHOLE && L <= 64) return;
+    const int waves = L / 64, wave = threadIdx.x / 64, of = wave / waves * waves + (threadIdx.x & 15);
     float* slot = whole + at * 2 * 16;
     if ((threadIdx.x & 63) == 0) {
       slot[wave] = a;
-      slot[16 + wave] = b;
+      if (TWO) slot[16 + wave] = b;
     }
     __syncthreads();
-    const int first = wave / waves * waves;
-    a = b = 0.0f;
-    for (int w = first; w < first + waves; ++w) {
-      a += slot[w];
-      b += slot[16 + w];
-    }
+    const bool in = (threadIdx.x & 15) < waves;
+    a = group_sum(in ? slot[of] : 0.0f, 16);
+    if (TWO) b = group_sum(in ? slot[16 + of] : 0.0f, 16);
   }
   // a summed over the lane's group
   __device__ __forceinline__ float group_total(float a, int at) const {
     if (each == pieces) {
       float none = 0.0f;
-      row_sums(a, none, at);
+      row_sums<false>(a, none, at);
       return a;
     }
     if (!split) return group_sum(a, each);
@@ -157,7 +158,7 @@ __device__ __forceinline__ void row8_store(void* p, Row2 step, long long b, long
 template <typename IO, typename ST, bool WHOLE>
 __global__ void __launch_bounds__(WHOLE ? 1024 : 256) residual_kernel(ResidualArgs a, int L) {
   extern __shared__ float lds[];
-  const RowLanes r(a, L, lds);
+  const RowLanes<WHOLE> r(a, L, lds);
   const long long total = static_cast<long long>(a.B) * a.T, stride = static_cast<long long>(gridDim.x) * r.rows;
   const int c = r.here ? kColumns * r.lane : 0;
   const int row_here = WHOLE ? 0 : r.row;   // known to be the same for the whole workgroup
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(WHOLE ? 1024 : 256) residual_kernel(ResidualAr
     }
     if (live && a.s != nullptr) row8_store<ST>(a.s, a.ss, b, t, c, s);
     if (a.weight != nullptr) {
-      r.row_sums(sum, none, 2 + turn);
+      r.template row_sums<false>(sum, none, 2 + turn);
       const float r2 = rsqrtf(fmaf(sum, 1.0f / a.n, a.eps));
 #pragma unroll
       for (int i = 0; i < kColumns; ++i) s[i] *= r2 * w2[i];
@@ -213,9 +214,9 @@ __global__ void __launch_bounds__(WHOLE ? 1024 : 256) residual_kernel(ResidualAr
 }
 
 template <typename IO, typename ST, bool WHOLE>
-__global__ void __launch_bounds__(WHOLE ? 1024 : 256) residual_backward_kernel(ResidualArgs a, int L) {
+__global__ void __launch_bounds__(WHOLE ? 1024 : 512) residual_backward_kernel(ResidualArgs a, int L) {
   extern __shared__ float lds[];
-  const RowLanes r(a, L, lds);
+  const RowLanes<WHOLE> r(a, L, lds);
   const long long total = static_cast<long long>(a.B) * a.T;
   const float inv_n = 1.0f / a.n, inv_group = 1.0f / a.group;
   const int c = r.here ? kColumns * r.lane : 0;
@@ -260,7 +261,7 @@ __global__ void __launch_bounds__(WHOLE ? 1024 : 256) residual_backward_kernel(R
         sq = fmaf(s[i], s[i], sq);
         along = fmaf(dh[i] * w2[i], s[i], along);
       }
-      r.row_sums(sq, along, 2 + turn);
+      r.template row_sums<true>(sq, along, 2 + turn);
       const float r2 = rsqrtf(fmaf(sq, inv_n, a.eps)), f = along * r2 * r2 * inv_n;
 #pragma unroll
       for (int i = 0; i < kColumns; ++i) {
@@ -292,40 +293,57 @@ __global__ void __launch_bounds__(WHOLE ? 1024 : 256) residual_backward_kernel(R
     if (live && a.dy != nullptr) row8_store<IO>(a.dy, a.dys, b, t, c, d);
   }
   if (a.sum_part == nullptr) return;
-  // the rows of a workgroup, one after the other
-  float* part = a.sum_part + static_cast<size_t>(blockIdx.x) * 3 * a.n + c;
-  for (int row = 0; row < r.rows; ++row) {
-    if (r.row == row && r.here) {
-      const Eight* all[3] = {&dw2, &dw1, &dk};
+  // the rows of a workgroup, in their order
+  float* part = a.sum_part + static_cast<size_t>(blockIdx.x) * 3 * a.n;
+  const Eight* all[3] = {&dw2, &dw1, &dk};
+  if (WHOLE) {
+    if (!r.here) return;
 #pragma unroll
-      for (int j = 0; j < 3; ++j) {
-        float* at = part + static_cast<size_t>(j) * a.n;
-        Eight e = *all[j];
-        if (row > 0) {
-          const Eight before = load8(at);
+    for (int j = 0; j < 3; ++j) store8(part + static_cast<size_t>(j) * a.n + c, *all[j]);
+    return;
+  }
+  float* const rows = r.weights + 3 * a.n;      // LDS: [rows][8 L]
 #pragma unroll
-          for (int i = 0; i < kColumns; ++i) e[i] += before[i];
-        }
-        store8(at, e);
-      }
+  for (int j = 0; j < 3; ++j) {
+    __syncthreads();
+    store8(rows + kColumns * threadIdx.x, *all[j]);
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
+      float sum = 0.0f;
+      for (int row = 0; row < r.rows; ++row) sum += rows[row * kColumns * L + i];
+      part[static_cast<size_t>(j) * a.n + i] = sum;
     }
-    if (r.rows > 1) __syncthreads();
   }
 }
 
-// Lanes of a row, and threads of a workgroup.
+// Lanes of a row: a power of two up to a wave, whole waves beyond.
 int row_width(int n) {
+  const int pieces = n / kColumns;
+  if (pieces > 64) return (pieces + 63) / 64 * 64;
   int L = 8;
-  while (L * kColumns < n) L *= 2;
+  while (L < pieces) L *= 2;
   return L;
+}
+// Threads of a workgroup: whole rows, four waves or more (backward: eight, whose number of workgroups is held by what they leave of the weights'
+// gradients; 87381 rows of 1536 in bfloat16, backward: 784 us with four waves, three of them at work).
+int threads_of(int L, bool backward) {
+  const int most = backward ? 512 : 256;
+  return L < most ? most / L * L : L;
+}
+
+// As many as the card's 256 compute units hold at once, with the registers that the kernels take 24 waves each (backward: 16): a workgroup more would go
+// through its rows when all others have ended (backward pass of 52428 rows of 2560 in bfloat16 with 819 workgroups 993 us, with 768 706).
+int workgroups_of(int threads, bool backward) {
+  const int held = (backward ? 16 : 24) / (threads / 64);
+  return 256 * (held > 0 ? held : 1);
 }
 
 template <typename IO, typename ST>
 hipError_t launch(const ResidualArgs& a, bool backward, int* parts, hipStream_t stream) {
   int L = row_width(a.n);
-  const int threads = L > 256 ? L : 256;
+  const int threads = threads_of(L, backward);
   const long long rows = static_cast<long long>(a.B) * a.T, groups = (rows + threads / L - 1) / (threads / L);
-  const int most = backward ? kResidualPartials : 2048 * 256 / threads;
+  const int most = workgroups_of(threads, backward);
   const int grid = static_cast<int>(groups < most ? groups : most);
   if (parts != nullptr) *parts = grid;
   if (grid == 0) return hipSuccess;
@@ -334,7 +352,7 @@ hipError_t launch(const ResidualArgs& a, bool backward, int* parts, hipStream_t 
   const void* backward_kernel =
       whole ? reinterpret_cast<const void*>(&residual_backward_kernel<IO, ST, true>) : reinterpret_cast<const void*>(&residual_backward_kernel<IO, ST, false>);
   ResidualArgs args = a;
-  const int lds = 4 * 2 * 16 + 2 * threads + (backward ? 3 * a.n : 0);
+  const int lds = 4 * 2 * 16 + 2 * threads + (backward ? 3 * a.n + (whole ? 0 : kColumns * threads) : 0);
   void* params[] = {&args, &L};
   return hipLaunchKernel(backward ? backward_kernel : forward_kernel, dim3(grid), dim3(threads), params, lds * sizeof(float), stream);
 }
@@ -346,6 +364,7 @@ hipError_t launch_types(const ResidualArgs& a, int io_dtype, int stream_dtype, b
 
 }  // namespace
 
+int residual_partials(int n) { return workgroups_of(threads_of(row_width(n), true), true); }
 hipError_t launch_residual_norm(const ResidualArgs& a, int io_dtype, int stream_dtype, hipStream_t stream) {
   return launch_types(a, io_dtype, stream_dtype, false, nullptr, stream);
 }
