@@ -7,13 +7,14 @@
 // along a run of tokens with the window on registers, eight rows' loads under way at once; the W - 1 rows before a run are read again.
 // The taps of a thread's channels lie together and are loaded as fours: one by one they are 40 loads that all wait for the same unit (16384 rows
 // of 2048 in bf16: 43 -> 25.5 us, one token of 64 sequences, 4096 channels: 7.6 -> 3.5).  8 x 8192 rows of 4096: 207 us forward, 5.2 TB/s; 365
-// backward, 4.4 TB/s.
+// backward, 4.4 TB/s.  The weights' gradient: a sum for each run, or, where a workgroup has several runs of its channels, one of these (4 x
+// 262144 rows of 64 in bf16, backward: 219 -> 127 us, most of which were the sums' way through memory).
 #include "mixer_util.h"
 
 namespace vla {
 namespace {
 
-constexpr int kThreads = 256, kStepThreads = 64;
+constexpr int kThreads = kConvThreads, kStepThreads = 64;
 constexpr int kAhead = 8;   // rows whose loads are under way at once
 
 template <typename IO>
@@ -127,7 +128,7 @@ template <int W, typename IO>
 __global__ void __launch_bounds__(kThreads) conv_backward_kernel(ConvArgs a) {
   constexpr int V = kPiece<IO>;
   const Place p(a, V, static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x);
-  if (!p.here) return;
+  if (!p.here && !a.joined) return;
   Weights<IO> k;
   k.template load<W>(a, p.c);
   const int length = length_of(a.lengths, p.b, a.T);
@@ -138,7 +139,7 @@ __global__ void __launch_bounds__(kThreads) conv_backward_kernel(ConvArgs a) {
   IO* dstate = a.dstate == nullptr ? nullptr : static_cast<IO*>(a.dstate) + static_cast<size_t>(p.b) * (W - 1) * a.n + p.c;
   const int first = p.run * a.run, last = min(first + a.run, a.T);
   const int own = min(last, length);          // tokens whose e counts for the weights here
-  const int end = last + W - 1;               // tokens that the run's rows are read by
+  const int end = p.here ? last + W - 1 : first;   // tokens that the run's rows are read by
   float e[W][V] = {};                         // e[j] of token t - (W - 1) + j
   float dw[W][V] = {}, db[V] = {};
   Piece<IO> window[W];                        // x of the same tokens
@@ -206,6 +207,24 @@ __global__ void __launch_bounds__(kThreads) conv_backward_kernel(ConvArgs a) {
     }
   }
   if (a.sum_part == nullptr) return;
+  if (a.joined) {      // the workgroup's runs of each channel, in their order
+    __shared__ __align__(16) float of_run[kThreads * V];
+    const int pieces = a.n / V, at = static_cast<int>(static_cast<long long>(blockIdx.x) * kThreads % pieces);
+    float* part = a.sum_part + static_cast<size_t>(blockIdx.x) * (W + 1) * a.n;
+#pragma unroll
+    for (int j = 0; j <= W; ++j) {
+      __syncthreads();
+      store_piece(of_run + threadIdx.x * V, j < W ? dw[j < W ? j : 0] : db);
+      __syncthreads();
+      for (int i = threadIdx.x; i < a.n; i += kThreads) {
+        const int piece = i / V;
+        float sum = 0.0f;
+        for (int q = piece >= at ? piece - at : piece - at + pieces; q < kThreads; q += pieces) sum += of_run[q * V + i % V];
+        part[static_cast<size_t>(j) * a.n + i] = sum;
+      }
+    }
+    return;
+  }
   float* part = a.sum_part + (static_cast<size_t>(p.b) * a.runs + p.run) * (W + 1) * a.n + p.c;
 #pragma unroll
   for (int j = 0; j < W; ++j) store_piece(part + static_cast<size_t>(j) * a.n, dw[j]);

@@ -57,8 +57,14 @@ int conv_run(int B, int T, int n, int io_dtype) {
   return static_cast<int>(run < T ? run : T > 0 ? T : 1);
 }
 int runs_of(int T, int run) { return T > 0 ? (T + run - 1) / run : 1; }
+// Parts of the weights' gradient: a run each, or, with channels that a workgroup holds at least twice, a workgroup each.
+bool conv_joined(int n, int io_dtype) { return n / (16 / static_cast<int>(size_of(io_dtype))) <= vla::kConvThreads / 2; }
+long long conv_parts(int B, int runs, int n, int io_dtype) {
+  const long long all = static_cast<long long>(B) * runs, pieces = n / (16 / static_cast<int>(size_of(io_dtype)));
+  return conv_joined(n, io_dtype) ? (all * pieces + vla::kConvThreads - 1) / vla::kConvThreads : all;
+}
 size_t conv_parts_bytes(int B, int T, int n, int width, int io_dtype) {
-  return static_cast<size_t>(B) * runs_of(T, conv_run(B, T, n, io_dtype)) * (width + 1) * n * 4;
+  return static_cast<size_t>(conv_parts(B, runs_of(T, conv_run(B, T, n, io_dtype)), n, io_dtype)) * (width + 1) * n * 4;
 }
 
 int conv_args(const void* x, const void* weight, const void* bias, const void* state, int B, int T, int n, int width, int io_dtype,
@@ -329,14 +335,16 @@ int vla_causal_conv_backward(const void* x, const void* weight, const void* bias
   a.runs = runs_of(T, a.run);
   if (!conv_fits(a, io_dtype)) return VLA_ERR_UNSUPPORTED;
   const hipStream_t s = static_cast<hipStream_t>(stream);
+  a.joined = sums && conv_joined(n, io_dtype);
   const hipError_t err = vla::launch_causal_conv_backward(a, width, io_dtype, s);
   if (err != hipSuccess || !sums) return launched(err);
+  const int parts = static_cast<int>(conv_parts(B, a.runs, n, io_dtype));
   vla::ColumnSums all{};
   const size_t row = static_cast<size_t>(width + 1) * n;
   for (int j = 0; j < width && dweight != nullptr; ++j) {
-    all.job[all.n++] = {a.sum_part + static_cast<size_t>(j) * n, row, B * a.runs, n, static_cast<char*>(dweight) + j * ws, a.w_bf16, width};
+    all.job[all.n++] = {a.sum_part + static_cast<size_t>(j) * n, row, parts, n, static_cast<char*>(dweight) + j * ws, a.w_bf16, width};
   }
-  if (dbias != nullptr) all.job[all.n++] = {a.sum_part + static_cast<size_t>(width) * n, row, B * a.runs, n, dbias, a.w_bf16, 1};
+  if (dbias != nullptr) all.job[all.n++] = {a.sum_part + static_cast<size_t>(width) * n, row, parts, n, dbias, a.w_bf16, 1};
   return launched(vla::launch_column_sums(all, s));
 }
 

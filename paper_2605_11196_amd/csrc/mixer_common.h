@@ -28,6 +28,7 @@ struct ColumnSums {
 hipError_t launch_column_sums(const ColumnSums& s, hipStream_t stream);
 
 constexpr int kConvWidth = 4;        // taps at most
+constexpr int kConvThreads = 256;    // of a workgroup, 16 bytes of channels each
 struct ConvArgs {
   const void* x;
   const void* weight;    // [n][width]
@@ -40,7 +41,8 @@ struct ConvArgs {
   const void* dstate_T;  // or nullptr (zero)
   void* dx;              // strides dxs
   void* dstate;          // or nullptr
-  float* sum_part;       // [B * runs][width + 1][n]: what a run of tokens gives of the gradients of weight and bias, or nullptr
+  float* sum_part;       // [parts][width + 1][n]: what runs of tokens give of the gradients of weight and bias, or nullptr
+  int joined;            // a part for each workgroup (otherwise for each run)
   Row2 xs, ys, dxs;
   int B, T, n, w_bf16, silu;
   int run, runs;         // tokens of a run, runs of a sequence

@@ -46,6 +46,9 @@ CASES = [
     (1, 131, 64, 2, "bf16", None, False, dict(bias=False, carried=False)),
     (2, 200, 520, 3, "bf16", None, True, {}),
     (1, 300, 40, 4, "f32", "bf16", True, {}),
+    (3, 300, 72, 4, "bf16", None, True, {}),          # runs of the same channels in a workgroup, not all as often
+    (2, 500, 1024, 2, "bf16", None, True, {}),        # twice each
+    (2, 50, 1032, 3, "bf16", None, True, {}),         # and not
 ]
 
 

@@ -128,7 +128,9 @@ def test_convolution_backward_refuses(given, opts, status):
 
 def test_convolution_workspace():
     size = lib().vla_causal_conv_workspace_bytes
-    assert size(2, 24, 32, 4, 0) == 2 * 2 * 5 * 32 * 4      # two runs of 16 tokens a sequence, four taps and the bias
+    assert size(2, 24, 1024, 4, 0) == 2 * 2 * 5 * 1024 * 4      # two runs of 16 tokens a sequence, four taps and the bias
+    assert size(2, 24, 32, 4, 0) == 5 * 32 * 4                  # 8 lanes a run: the four runs lie in one workgroup
+    assert size(3, 1537, 72, 2, 1) == 11 * 3 * 72 * 4           # 97 runs of 9 lanes a sequence
     assert size(1, 0, 32, 2, 1) == 3 * 32 * 4
     assert size(0, 24, 32, 4, 0) == 0 and size(2, 24, 30, 4, 0) == 0 and size(2, 24, 32, 5, 0) == 0 and size(2, 24, 32, 4, 7) == 0
 
