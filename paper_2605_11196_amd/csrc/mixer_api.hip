@@ -278,8 +278,8 @@ int vla_causal_conv(const void* x, const void* weight, const void* bias, const v
   if (st != VLA_OK) return st;
   if ((T > 0 && y == nullptr) || !aligned16(y) || !aligned16(state_T)) return VLA_ERR_INVALID_ARG;
   if (!rows2(op.y, B, T, n, io_dtype, true, &a.ys)) return VLA_ERR_INVALID_ARG;
-  const size_t es = size_of(io_dtype), ws = size_of(op.weight_dtype), window = static_cast<size_t>(B) * (width - 1) * n * es;
-  const Range r[] = {{x, reach2(a.xs, B, T, n, io_dtype), false}, {weight, n * width * ws, false}, {bias, n * ws, false}, {state, window, false},
+  const size_t columns = n, es = size_of(io_dtype), ws = size_of(op.weight_dtype), window = static_cast<size_t>(B) * (width - 1) * n * es;
+  const Range r[] = {{x, reach2(a.xs, B, T, n, io_dtype), false}, {weight, columns * width * ws, false}, {bias, columns * ws, false}, {state, window, false},
                      {op.lengths, static_cast<size_t>(B) * 4, false}, {y, reach2(a.ys, B, T, n, io_dtype), true}, {state_T, window, true}};
   if (!disjoint(r, 7, state, state_T)) return VLA_ERR_INVALID_ARG;
   a.y = y;
@@ -298,8 +298,8 @@ int vla_causal_conv_step(const void* x, const void* weight, const void* bias, vo
   if (st != VLA_OK) return st;
   if (state == nullptr || y == nullptr || op.lengths != nullptr || !aligned16(state) || !aligned16(y)) return VLA_ERR_INVALID_ARG;
   if (!rows2(op.y, B, 1, n, io_dtype, true, &a.ys)) return VLA_ERR_INVALID_ARG;
-  const size_t es = size_of(io_dtype), ws = size_of(op.weight_dtype);
-  const Range r[] = {{x, reach2(a.xs, B, 1, n, io_dtype), false}, {weight, n * width * ws, false}, {bias, n * ws, false},
+  const size_t columns = n, es = size_of(io_dtype), ws = size_of(op.weight_dtype);
+  const Range r[] = {{x, reach2(a.xs, B, 1, n, io_dtype), false}, {weight, columns * width * ws, false}, {bias, columns * ws, false},
                      {state, static_cast<size_t>(B) * (width - 1) * n * es, true}, {y, reach2(a.ys, B, 1, n, io_dtype), true}};
   if (!disjoint(r, 5, nullptr, nullptr)) return VLA_ERR_INVALID_ARG;
   a.y = y;
@@ -321,12 +321,12 @@ int vla_causal_conv_backward(const void* x, const void* weight, const void* bias
   if (!all_aligned(ptrs, 7)) return VLA_ERR_INVALID_ARG;
   if (!rows2(op.y, B, T, n, io_dtype, false, &a.ys) || !rows2(op.dx, B, T, n, io_dtype, true, &a.dxs)) return VLA_ERR_INVALID_ARG;
   const bool sums = dweight != nullptr || dbias != nullptr;
-  const size_t need = conv_parts_bytes(B, T, n, width, io_dtype), es = size_of(io_dtype), ws = size_of(op.weight_dtype);
+  const size_t columns = n, need = conv_parts_bytes(B, T, n, width, io_dtype), es = size_of(io_dtype), ws = size_of(op.weight_dtype);
   if (sums && (workspace == nullptr || workspace_bytes < need)) return VLA_ERR_WORKSPACE;
   const size_t window = static_cast<size_t>(B) * (width - 1) * n * es;
-  const Range r[] = {{x, reach2(a.xs, B, T, n, io_dtype), false}, {weight, n * width * ws, false}, {bias, n * ws, false}, {state, window, false},
+  const Range r[] = {{x, reach2(a.xs, B, T, n, io_dtype), false}, {weight, columns * width * ws, false}, {bias, columns * ws, false}, {state, window, false},
                      {op.lengths, static_cast<size_t>(B) * 4, false}, {dy, reach2(a.ys, B, T, n, io_dtype), false}, {dstate_T, window, false},
-                     {dx, reach2(a.dxs, B, T, n, io_dtype), true}, {dweight, n * width * ws, true}, {dbias, n * ws, true}, {dstate, window, true},
+                     {dx, reach2(a.dxs, B, T, n, io_dtype), true}, {dweight, columns * width * ws, true}, {dbias, columns * ws, true}, {dstate, window, true},
                      {sums ? workspace : nullptr, need, true}};
   if (!disjoint(r, 12, nullptr, nullptr)) return VLA_ERR_INVALID_ARG;
   a.dy = dy; a.dstate_T = dstate_T; a.dx = dx; a.dstate = dstate;

@@ -75,3 +75,18 @@ def test_every_launch_holds_its_work_items(recorder, name, args):
     assert status == 0 and grids
     for x, y, z, threads, *rest in grids:
         assert rest == [1, 1] and x >= 1 and x * threads < 2 ** 32 and y <= 65535 and z == 1 and threads <= 1024, grids
+
+
+@pytest.mark.parametrize("name,place", [("vla_causal_conv", 4), ("vla_causal_conv_step", 4), ("vla_causal_conv_backward", 6)])
+@pytest.mark.parametrize("n,width", [(2 ** 29, 4), (2 ** 30, 2), (2 ** 31 - 8, 4)])
+def test_outputs_inside_the_taps_of_many_channels_are_refused(recorder, name, place, n, width):
+    """An output that starts in the second half of taps [n, width] whose number passes 31 bits."""
+    at = places(10)
+    at[place] = str(int(at[1]) + n * width // 2 * 4)      # float32
+    if name.endswith("step"):
+        args = [*at[:5], 1, n, width, 1, "0", "0"]
+    elif place == 4:
+        args = [*at[:6], 1, 1, n, width, 1, "0", "0"]
+    else:
+        args = [*at, 1, 1, n, width, 1, "0", str(100 << 41), ROOM, "0"]
+    assert launches(recorder, name, args) == ([], 1)
