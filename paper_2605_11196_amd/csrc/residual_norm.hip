@@ -158,7 +158,7 @@ __device__ __forceinline__ void row8_store(void* p, Row2 step, long long b, long
 
 template <typename IO, typename ST, bool WHOLE>
 __global__ void __launch_bounds__(WHOLE ? 1024 : 256) residual_kernel(ResidualArgs a, int L) {
-  extern __shared__ float lds[];
+  extern __shared__ __align__(16) float lds[];
   const RowLanes<WHOLE> r(a, L, lds);
   const long long total = static_cast<long long>(a.B) * a.T, stride = static_cast<long long>(gridDim.x) * r.rows;
   const int c = r.here ? kColumns * r.lane : 0;
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(WHOLE ? 1024 : 256) residual_kernel(ResidualAr
 
 template <typename IO, typename ST, bool WHOLE>
 __global__ void __launch_bounds__(WHOLE ? 1024 : 512) residual_backward_kernel(ResidualArgs a, int L) {
-  extern __shared__ float lds[];
+  extern __shared__ __align__(16) float lds[];
   const RowLanes<WHOLE> r(a, L, lds);
   const long long total = static_cast<long long>(a.B) * a.T;
   const float inv_n = 1.0f / a.n, inv_group = 1.0f / a.group;

@@ -18,7 +18,7 @@ template <int N, typename IO, bool MAP>
 __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
   typedef ScanPlace<N> P;
   constexpr int LN = P::LN, OWN = P::OWN, TURNS = kTurns<LN>;
-  __shared__ f2 steps[scan_waves(N)][2][TB][P::CW];                     // dt, dt u
+  __shared__ __align__(16) f2 steps[scan_waves(N)][2][TB][P::CW];       // dt, dt u
   __shared__ __align__(16) float staged[scan_waves(N)][2][TB][2 * N];   // B, C
   __shared__ __align__(8) float outs[MAP ? 1 : scan_waves(N)][TB][P::CW];            // sums of the read-out
   const P w(a);
