@@ -105,6 +105,9 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
   f2 dD = {0.0f, 0.0f}, dbias = dD;
 
   const int last = w.live > w.first ? w.first + (w.live - 1 - w.first) / TB * TB : w.first - TB;   // block
+  // Tokens that the last block has not: it is gone through as the eight tokens up to the sequence's end, whose first `skip` count for nothing.  (Behind the end
+  // they would meet the last state, and an infinite one times their step of 0 is no number.)
+  const int skip_last = last >= w.first ? last + TB - w.live : 0;
   ScanStage<N, IO> rows(w, a, last);
   const ScanRows<N, IO> u(w, a.u, a.us), delta(w, a.delta, a.ds), z(w, gated ? a.z : a.u, gated ? a.zs : a.us), dy(w, a.dy, a.ys);
   const ScanRows<N, IO> du_(w, MAP ? a.u : a.du, MAP ? a.us : a.dus), ddelta_(w, MAP ? a.u : a.ddelta, MAP ? a.us : a.dds),
@@ -112,16 +115,16 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
   // what a block reads is on its way while the one behind it is worked on
   Pair<IO> next_u[OWN] = {}, next_delta[OWN] = {}, next_z[OWN] = {}, next_dy[OWN] = {};
   f4 next_h = {};
-  const auto fetch = [&](int t0) {      // the blocks one after the other
-    u.load(next_u, w, a.T, t0);
-    delta.load(next_delta, w, a.T, t0);
-    dy.load(next_dy, w, a.T, t0);
-    if (gated) z.load(next_z, w, a.T, t0);
-    rows.load(a.T - t0);
+  const auto fetch = [&](int t0, int skip) {      // the blocks one after the other
+    u.load(next_u, w, t0, skip);
+    delta.load(next_delta, w, t0, skip);
+    dy.load(next_dy, w, t0, skip);
+    if (gated) z.load(next_z, w, t0, skip);
+    rows.load_behind(skip);
     rows.template go<true>();
     if (!MAP) next_h = *reinterpret_cast<const f4*>(a.kept + ((static_cast<size_t>(w.b) * a.blocks + t0 / TB) * a.n + w.c) * N + 4 * w.q);
   };
-  if (last >= w.first) fetch(last);
+  if (last >= w.first) fetch(last, skip_last);
   // With many states a block's results are stored a block later, as in the forward pass (training steps of 8 x 2048 tokens: backward pass of 2048
   // channels of 32 states 1025 -> 1000 us, of 1024 of 64 1140 -> 1078); with few of them the instructions between two blocks weigh more (4096 of
   // 16: 910 us and 950).
@@ -129,30 +132,30 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
   constexpr int PARTS = (TB * 2 * N + 64 * W - 1) / (64 * W);
   Pair<IO> done_du[OWN] = {}, done_ddelta[OWN] = {}, done_dz[OWN] = {};
   float done_BC[PARTS] = {};
-  const auto put = [&](int t0) {
+  const auto put = [&](int t0, int skip) {
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
-      if (w.here2 && t0 + w.own(k) < w.last) {
-        du_.store(du_.row(t0), k, done_du[k]);
-        ddelta_.store(ddelta_.row(t0), k, done_ddelta[k]);
-        if (gated) dz_.store(dz_.row(t0), k, done_dz[k]);
+      if (w.here2 && w.own(k) >= skip) {
+        du_.store(du_.row(t0 - skip), k, done_du[k]);
+        ddelta_.store(ddelta_.row(t0 - skip), k, done_ddelta[k]);
+        if (gated) dz_.store(dz_.row(t0 - skip), k, done_dz[k]);
       }
     }
   };
-  const auto put_BC = [&](int t0) {
-    float* to = a.dBC_part + ((static_cast<size_t>(w.tile) * a.nb + w.b) * a.T + t0) * 2 * N;
+  const auto put_BC = [&](int t0, int skip) {
+    float* to = a.dBC_part + ((static_cast<long long>(w.tile) * a.nb + w.b) * a.T + t0 - skip) * 2 * N;
 #pragma unroll
     for (int j = 0; j < PARTS; ++j) {
       const int i = threadIdx.x + j * 64 * W;
-      if (i < TB * 2 * N && t0 + i / (2 * N) < w.length) to[i] = done_BC[j];
+      if (i < TB * 2 * N && i / (2 * N) >= skip) to[i] = done_BC[j];
     }
   };
-  int turn = 0;
+  int turn = 0, skip = skip_last;
   for (int t0 = last; t0 >= w.first; t0 -= TB) {
     f2 x[OWN], raw[OWN], v[OWN], sig[OWN], d[OWN], dt_[OWN], e_[OWN];
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
-      const bool in = t0 + w.own(k) < w.length && w.here2;
+      const bool in = w.own(k) >= skip && w.here2;
       x[k] = wide2(next_u[k]);
       raw[k] = wide2(next_delta[k]) + bias;
       v[k] = wide2(next_z[k]);
@@ -166,10 +169,10 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
         if (w.lane < TB * P::PAIRS) steps[w.wave][w.own(k)][2 * w.pair + j] = f4{dt_[k][j], in ? dt * x[k][j] : 0.0f, e_[k][j], 0.0f};
       }
     }
-    rows.put(mine, t0, w.length);
+    rows.put(mine, rows.t >= skip);
     f4 h = next_h;
-    if (!MAP && LATER && t0 < last) put(t0 + TB), put_BC(t0 + TB);
-    if (t0 - TB >= w.first) fetch(t0 - TB);
+    if (!MAP && LATER && t0 < last) put(t0 + TB, t0 + TB == last ? skip_last : 0), put_BC(t0 + TB, t0 + TB == last ? skip_last : 0);
+    if (t0 - TB >= w.first) fetch(t0 - TB, 0);
     wave_fence();
     if constexpr (MAP) {
 #pragma unroll
@@ -241,8 +244,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
       wave_fence();
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
-        const int t = t0 + w.own(k);
-        const bool in = t < w.length;
+        const bool in = w.own(k) >= skip;
         f2 du, ddelta, dz;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -258,7 +260,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
         done_ddelta[k] = narrow2<IO>(ddelta);
         done_dz[k] = narrow2<IO>(dz);
       }
-      if (!LATER) put(t0);
+      if (!LATER) put(t0, skip);
       // dB and dC of the workgroup's channels: the waves in their order
       __syncthreads();
 #pragma unroll
@@ -271,18 +273,18 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
         }
         done_BC[j] = sum;
       }
-      if (!LATER) put_BC(t0);
+      if (!LATER) put_BC(t0, skip);
       turn ^= 1;
     }
+    skip = 0;
   }
   if constexpr (MAP) {
     if (!w.here) return;
     *reinterpret_cast<f4*>(a.seg_h + of_seg * N + 4 * w.q) = g;
     if (w.q == 0) a.seg_dt[of_seg] = sum_dt;
   } else {
-    if (LATER && last >= w.first) put(w.first), put_BC(w.first);
-    const int gone = w.live > w.first ? last + TB : w.first;
-    for (int t0 = gone; t0 < w.last; t0 += TB) {
+    if (LATER && last >= w.first) put(w.first, w.first == last ? skip_last : 0), put_BC(w.first, w.first == last ? skip_last : 0);
+    for (int t0 = max(w.live, w.first); t0 < w.last; t0 += TB) {
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
         if (w.here2 && t0 + w.own(k) < w.last) {

@@ -76,36 +76,35 @@ struct ScanRows {
   static constexpr int OWN = ScanPlace<N>::OWN;
   char* base;              // of the sequence
   long long step;          // bytes from token to token
-  unsigned at[OWN];        // bytes from a block's first token
+  unsigned at;             // bytes from a block's first token to the lane's own first one
   __device__ __forceinline__ ScanRows(const ScanPlace<N>& w, const void* p, Row2 r) {
     base = const_cast<char*>(static_cast<const char*>(p)) + w.b * r.b * static_cast<long long>(sizeof(IO));
     step = r.t * static_cast<long long>(sizeof(IO));
-#pragma unroll
-    for (int k = 0; k < OWN; ++k) at[k] = w.own(k) * static_cast<unsigned>(step) + w.c2 * static_cast<unsigned>(sizeof(IO));
+    at = w.own(0) * static_cast<unsigned>(step) + w.c2 * static_cast<unsigned>(sizeof(IO));
   }
   __device__ __forceinline__ char* row(int t0) const { return base + t0 * step; }
+  // where the k-th own tokens' rows begin: the same for all lanes
+  template <typename P> __device__ __forceinline__ P* own(P* row, int k) const { return row + k * (64 / ScanPlace<N>::PAIRS) * step; }
   __device__ __forceinline__ void load(const char* row, Pair<IO> (&v)[OWN]) const {
 #pragma unroll
-    for (int k = 0; k < OWN; ++k) v[k] = *reinterpret_cast<const Pair<IO>*>(row + at[k]);
+    for (int k = 0; k < OWN; ++k) v[k] = *reinterpret_cast<const Pair<IO>*>(own(row, k) + at);
   }
   // of a block with `tokens` of them, the rest of its rows being the last one
   __device__ __forceinline__ void load(const char* row, Pair<IO> (&v)[OWN], const ScanPlace<N>& w, int tokens) const {
 #pragma unroll
-    for (int k = 0; k < OWN; ++k) v[k] = *reinterpret_cast<const Pair<IO>*>(row + (at[k] - max(w.own(k) - (tokens - 1), 0) * static_cast<unsigned>(step)));
+    for (int k = 0; k < OWN; ++k) v[k] = *reinterpret_cast<const Pair<IO>*>(row + (at + k * (64 / ScanPlace<N>::PAIRS) * static_cast<unsigned>(step) - max(w.own(k) - (tokens - 1), 0) * static_cast<unsigned>(step)));
   }
-  // either, with the choice between their addresses: fewer registers than two ways
-  __device__ __forceinline__ void load(Pair<IO> (&v)[OWN], const ScanPlace<N>& w, int T, int t0) const {
-    const char* from = row(t0);
-    if (t0 + TB <= T) {
+  // of the block at t0 - skip, the `skip` tokens before t0 being the one at t0
+  __device__ __forceinline__ void load(Pair<IO> (&v)[OWN], const ScanPlace<N>& w, int t0, int skip) const {
+    const char* from = row(t0 - skip);
+    if (skip == 0) {
       load(from, v);
     } else {
 #pragma unroll
-      for (int k = 0; k < OWN; ++k) {
-        v[k] = *reinterpret_cast<const Pair<IO>*>(from + (min(w.own(k), T - 1 - t0) * static_cast<unsigned>(step) + w.c2 * static_cast<unsigned>(sizeof(IO))));
-      }
+      for (int k = 0; k < OWN; ++k) v[k] = *reinterpret_cast<const Pair<IO>*>(own(from, k) + (at + max(skip - w.own(k), 0) * static_cast<unsigned>(step)));
     }
   }
-  __device__ __forceinline__ void store(char* row, int k, Pair<IO> x) const { *reinterpret_cast<Pair<IO>*>(row + at[k]) = x; }
+  __device__ __forceinline__ void store(char* row, int k, Pair<IO> x) const { *reinterpret_cast<Pair<IO>*>(own(row, k) + at) = x; }
 };
 
 // B and C of a block: a wave's lanes load N / 4 neighbouring values each and put them into LDS as float32, [token][B | C].
@@ -127,8 +126,11 @@ struct ScanStage {
   }
   template <bool BACK> __device__ __forceinline__ void go() { row = BACK ? row - TB * step : row + TB * step; }
   // of a block with `tokens` of them (TB: all), the rest of its rows being the last one
-  __device__ __forceinline__ void load(int tokens) {
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(tokens < TB ? row - max(t - (tokens - 1), 0) * step : row);
+  __device__ __forceinline__ void load(int tokens) { load(tokens < TB ? row - max(t - (tokens - 1), 0) * step : row); }
+  // of the block `skip` tokens earlier, those that lie before the row's own block being its first one
+  __device__ __forceinline__ void load_behind(int skip) { load(skip != 0 ? row - min(skip, t) * step : row); }
+  __device__ __forceinline__ void load(const char* from) {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(from);
     if constexpr (WORDS == 1) {
       raw[0] = *p;
     } else if constexpr (WORDS == 2) {
@@ -144,9 +146,8 @@ struct ScanStage {
       }
     }
   }
-  // rows: the wave's own [TB][2 N]; tokens past the end of the sequence give zeros
-  __device__ __forceinline__ void put(float* rows, int t0, int length) const {
-    const bool in = t0 + t < length;
+  // rows: the wave's own [TB][2 N]; in: whether the token counts, otherwise zeros
+  __device__ __forceinline__ void put(float* rows, bool in) const {
     uint32_t kept[WORDS];
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) kept[i] = in ? raw[i] : 0u;

@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
       const f2 d = or_zero(in, dt[k]);
       *reinterpret_cast<f4*>(&steps[w.wave][buffer][w.own(k)][2 * w.pair]) = f4{d[0], d[0] * x[k][0], d[1], d[1] * x[k][1]};
     }
-    rows.put(staged[w.wave][buffer][0], t0, w.length);
+    rows.put(staged[w.wave][buffer][0], t0 + rows.t < w.length);
   };
   if (w.first < w.live) {
     fetch(w.first);
