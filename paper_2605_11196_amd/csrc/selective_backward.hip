@@ -249,8 +249,11 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const f4 sum = step[w.own(k) * P::CW + 2 * w.pair + j];
-          const float inner = fmaf(D[j], x[k][j], sum[0]), slope = a.softplus ? sigmoid(raw[k][j]) : 1.0f;
-          du[j] = in ? fmaf(D[j], e_[k][j], dt_[k][j] * sum[1]) : 0.0f;
+          // (without D its terms are left out: 0 times an infinite number would be none)
+          const float inner = a.D != nullptr ? fmaf(D[j], x[k][j], sum[0]) : sum[0], slope = a.softplus ? sigmoid(raw[k][j]) : 1.0f;
+          du[j] = dt_[k][j] * sum[1];
+          if (a.D != nullptr) du[j] = fmaf(D[j], e_[k][j], du[j]);
+          du[j] = in ? du[j] : 0.0f;
           ddelta[j] = in ? fmaf(x[k][j], sum[1], kLn2 * sum[2]) * slope : 0.0f;
           dz[j] = in ? d[k][j] * inner * sig[k][j] * fmaf(v[k][j], 1.0f - sig[k][j], 1.0f) : 0.0f;
           dD[j] += in ? e_[k][j] * x[k][j] : 0.0f;

@@ -144,7 +144,8 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) scan_kernel(ScanArgs a) {
 #pragma unroll
     for (int k = 0; k < OWN; ++k) {
       const int t = t0 + w.own(k);
-      f2 r = *reinterpret_cast<const f2*>(&outs[w.wave][w.own(k)][2 * w.pair]) + D * now_x[k];
+      f2 r = *reinterpret_cast<const f2*>(&outs[w.wave][w.own(k)][2 * w.pair]);
+      if (a.D != nullptr) r += D * now_x[k];      // without D nothing is added: 0 times an infinite input would be no number
       if (gated) r *= f2{now_v[k][0] * sigmoid(now_v[k][0]), now_v[k][1] * sigmoid(now_v[k][1])};
       done[k] = or_zero(t < w.length, narrow2<IO>(r));
     }

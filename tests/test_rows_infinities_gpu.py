@@ -40,3 +40,29 @@ def test_the_rates_gradient_where_the_last_state_overflows(dtype, N, T, last):
     dA = vla.selective_scan_backward(*args, None, None, saved, dy.cuda(), dh.cuda(), softplus=False, lengths=lengths.cuda())[2]
     # as for the scan's other tests: 48 roundings a token, the sums over tokens and sequences
     ref.close(dA, *both, 48 * T + 64 + 2 * T)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_an_infinite_input_without_a_skip(dtype):
+    """Without D the read-out is C . h alone, which has a sign where B and C do: over a sequence as token by token."""
+    n, N, T = 64, 16, 11
+    gen = torch.Generator().manual_seed(3)
+    u, delta = (torch.randn((1, T, n), generator=gen).to(DT[dtype]).cuda() for _ in range(2))
+    B, C = (1 + torch.rand((1, T, N), generator=gen).to(DT[dtype]).cuda() for _ in range(2))
+    A = -torch.rand((n, N), generator=gen).cuda()
+    u[0, 4, 5] = float("inf")
+    z = torch.ones_like(u)
+    y, h = vla.selective_scan(u, delta, A, B, C, None, z)
+    assert (y[0, 4:, 5] == float("inf")).all() and (h[0, 5] == float("inf")).all()
+    state = torch.zeros(1, n, N, device="cuda")
+    for t in range(T):
+        one = vla.selective_scan_step(u[:, t], delta[:, t], A, B[:, t], C[:, t], state, None, z[:, t])
+        assert torch.equal(torch.isinf(one), torch.isinf(y[:, t])) and not torch.isnan(one).any(), t
+    # the gate's gradient is the sign of dy times that, the input's dt times sum g B, which is finite
+    _, _, saved = vla.selective_scan_forward(u, delta, A, B, C, None, z, save_for_backward=True)
+    grads = vla.selective_scan_backward(u, delta, A, B, C, None, z, saved, torch.ones_like(u))
+    assert (grads[6][0, 4:, 5] == float("inf")).all() and torch.isfinite(grads[0]).all()
+    dy = torch.ones_like(u)
+    dy[0, 6, 9] = float("inf")
+    grads = vla.selective_scan_backward(u, delta, A, B, C, None, z, saved, dy)
+    assert (grads[0][0, :7, 9] == float("inf")).all() and not torch.isnan(grads[0]).any()
