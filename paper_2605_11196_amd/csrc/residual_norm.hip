@@ -288,9 +288,11 @@ __global__ void __launch_bounds__(WHOLE ? 1024 : 512) residual_backward_kernel(R
       m = fmaf(d[i], unit[i], m);
     }
     if (live && a.dgate != nullptr) row8_store<IO>(a.dgate, a.dgs, b, t, c, g);
-    const float f = a.post_weight != nullptr ? r.group_total(m, 1) * inv_group : 0.0f;
+    if (a.post_weight != nullptr) {
+      const float f = r.group_total(m, 1) * inv_group;
 #pragma unroll
-    for (int i = 0; i < kColumns; ++i) d[i] = r1 * fmaf(-unit[i], f, d[i]);
+      for (int i = 0; i < kColumns; ++i) d[i] = r1 * fmaf(-unit[i], f, d[i]);
+    }
     if (live && a.dy != nullptr) row8_store<IO>(a.dy, a.dys, b, t, c, d);
   }
   if (a.sum_part == nullptr) return;

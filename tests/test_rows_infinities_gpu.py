@@ -66,3 +66,15 @@ def test_an_infinite_input_without_a_skip(dtype):
     dy[0, 6, 9] = float("inf")
     grads = vla.selective_scan_backward(u, delta, A, B, C, None, z, saved, dy)
     assert (grads[0][0, :7, 9] == float("inf")).all() and not torch.isnan(grads[0]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [64, 1536, 4096])
+def test_an_infinite_output_of_a_block_without_its_norm(dtype, n):
+    """s = x + scale y: dy is scale ds, whatever y is."""
+    gen = torch.Generator().manual_seed(n)
+    x, y, ds = (torch.randn((1, 5, n), generator=gen).to(DT[dtype]).cuda() for _ in range(3))
+    scale = (0.5 + torch.rand(n, generator=gen)).to(DT[dtype]).cuda()
+    y[0, 2, 7], y[0, 3, 9] = float("inf"), float("nan")
+    dx, dy, *_ = vla.residual_norm_backward(x, y, None, ds, None, scale=scale)
+    assert torch.equal(dx, ds) and torch.equal(dy, (ds.float() * scale.float()).to(DT[dtype]))
