@@ -125,31 +125,9 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
     if (!MAP) next_h = *reinterpret_cast<const f4*>(a.kept + ((static_cast<size_t>(w.b) * a.blocks + t0 / TB) * a.n + w.c) * N + 4 * w.q);
   };
   if (last >= w.first) fetch(last, skip_last);
-  // With many states a block's results are stored a block later, as in the forward pass (training steps of 8 x 2048 tokens: backward pass of 2048
-  // channels of 32 states 1025 -> 1000 us, of 1024 of 64 1140 -> 1078); with few of them the instructions between two blocks weigh more (4096 of
-  // 16: 910 us and 950).
-  constexpr bool LATER = N >= 32;
+  // (Results stored a block later, as in the forward pass, gain nothing here: backward pass of 8 x 2048 tokens of 4096 channels of 16 states 879 -> 896 us, of
+  // 2048 of 32 960 -> 968, of 1024 of 64 1107 -> 1112.)
   constexpr int PARTS = (TB * 2 * N + 64 * W - 1) / (64 * W);
-  Pair<IO> done_du[OWN] = {}, done_ddelta[OWN] = {}, done_dz[OWN] = {};
-  float done_BC[PARTS] = {};
-  const auto put = [&](int t0, int skip) {
-#pragma unroll
-    for (int k = 0; k < OWN; ++k) {
-      if (w.here2 && w.own(k) >= skip) {
-        du_.store(du_.row(t0 - skip), k, done_du[k]);
-        ddelta_.store(ddelta_.row(t0 - skip), k, done_ddelta[k]);
-        if (gated) dz_.store(dz_.row(t0 - skip), k, done_dz[k]);
-      }
-    }
-  };
-  const auto put_BC = [&](int t0, int skip) {
-    float* to = a.dBC_part + ((static_cast<long long>(w.tile) * a.nb + w.b) * a.T + t0 - skip) * 2 * N;
-#pragma unroll
-    for (int j = 0; j < PARTS; ++j) {
-      const int i = threadIdx.x + j * 64 * W;
-      if (i < TB * 2 * N && i / (2 * N) >= skip) to[i] = done_BC[j];
-    }
-  };
   int turn = 0, skip = skip_last;
   for (int t0 = last; t0 >= w.first; t0 -= TB) {
     f2 x[OWN], raw[OWN], v[OWN], sig[OWN], d[OWN], dt_[OWN], e_[OWN];
@@ -171,7 +149,6 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
     }
     rows.put(mine, rows.t >= skip);
     f4 h = next_h;
-    if (!MAP && LATER && t0 < last) put(t0 + TB, t0 + TB == last ? skip_last : 0), put_BC(t0 + TB, t0 + TB == last ? skip_last : 0);
     if (t0 - TB >= w.first) fetch(t0 - TB, 0);
     wave_fence();
     if constexpr (MAP) {
@@ -259,24 +236,30 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
           dD[j] += in ? e_[k][j] * x[k][j] : 0.0f;
           dbias[j] += ddelta[j];
         }
-        done_du[k] = narrow2<IO>(du);
-        done_ddelta[k] = narrow2<IO>(ddelta);
-        done_dz[k] = narrow2<IO>(dz);
+        if (w.here2 && in) {
+          du_.store(du_.row(t0 - skip), k, narrow2<IO>(du));
+          ddelta_.store(ddelta_.row(t0 - skip), k, narrow2<IO>(ddelta));
+          if (gated) dz_.store(dz_.row(t0 - skip), k, narrow2<IO>(dz));
+        }
       }
-      if (!LATER) put(t0, skip);
       // dB and dC of the workgroup's channels: the waves in their order
       __syncthreads();
+      float of_all[PARTS];
 #pragma unroll
       for (int j = 0; j < PARTS; ++j) {
         const int i = threadIdx.x + j * 64 * W;
-        float sum = 0.0f;
+        of_all[j] = 0.0f;
         if (TB * 2 * N >= 64 * W || i < TB * 2 * N) {
 #pragma unroll
-          for (int o = 0; o < W; ++o) sum += sums[turn][o][i / (2 * N)][i % (2 * N)];
+          for (int o = 0; o < W; ++o) of_all[j] += sums[turn][o][i / (2 * N)][i % (2 * N)];
         }
-        done_BC[j] = sum;
       }
-      if (!LATER) put_BC(t0, skip);
+      float* const to = a.dBC_part + ((static_cast<long long>(w.tile) * a.nb + w.b) * a.T + t0 - skip) * 2 * N;
+#pragma unroll
+      for (int j = 0; j < PARTS; ++j) {
+        const int i = threadIdx.x + j * 64 * W;
+        if (i < TB * 2 * N && i / (2 * N) >= skip) to[i] = of_all[j];
+      }
       turn ^= 1;
     }
     skip = 0;
@@ -286,7 +269,6 @@ __global__ void __launch_bounds__(64 * scan_waves(N)) __attribute__((amdgpu_wave
     *reinterpret_cast<f4*>(a.seg_h + of_seg * N + 4 * w.q) = g;
     if (w.q == 0) a.seg_dt[of_seg] = sum_dt;
   } else {
-    if (LATER && last >= w.first) put(w.first, w.first == last ? skip_last : 0), put_BC(w.first, w.first == last ? skip_last : 0);
     for (int t0 = max(w.live, w.first); t0 < w.last; t0 += TB) {
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
