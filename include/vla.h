@@ -396,8 +396,8 @@ typedef struct vla_scan_opts {
   vla_strides u, delta, z, y; /* [contiguous] of y and of dy */
   vla_strides B, C;           /* [contiguous [B, T, groups, N]]; h: from group to group */
   vla_strides du, ddelta, dz; /* [contiguous]; the gradients of B and C are contiguous [B, T, groups, N] */
-  void* saved;                /* [NULL = not wanted] device, vla_selective_scan_saved_bytes(): the state at every 8th token, written by
-                                 vla_selective_scan, read by vla_selective_scan_backward */
+  void* saved;                /* [NULL = not wanted] device, vla_selective_scan_saved_bytes(): the state at every 8th token (N / 2 bytes for every
+                                 token and channel), written by vla_selective_scan, read by vla_selective_scan_backward */
   size_t saved_bytes;
   int segments;               /* [0 = the library chooses] time segments that long sequences of few channels are cut into (1: none).  Sizes the
                                  workspace, so pass the same value to vla_selective_scan_workspace_bytes() */

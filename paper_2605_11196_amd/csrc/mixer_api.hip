@@ -116,8 +116,11 @@ int check_scan(int B, int T, int n, int N, int io_dtype, const vla_scan_opts& o)
 
 // Time segments.  In segments the tokens are gone through twice (the second time without the read-out), which pays while sequences and channels
 // leave SIMDs idle: with fewer than 1400 waves on the card's 1024.  8 x 2048 tokens, 16 states, bfloat16, forward that saves and backward
-// together, whole and in segments: 1024 channels (512 waves) 887 us and 414, 2048 (1024) 923 and 819, 2560 (1280) 1189 and 1066, 3584 (1792) 1207 and 1436.
-// As many segments as give 8 waves a SIMD (2048 channels of one sequence of 16384: 16 segments 882 us, 64 838), of four blocks at least.
+// together, whole and in segments: 1024 channels (512 waves) 858 us and 428, 2048 (1024) 904 and 815, 2560 (1280) 1177 and 1039, 3584 (1792) 1195 and (two) 1505.
+// As many segments as give 8192 waves, of four blocks at least; the maps hold 6 to 8 of them a SIMD, the outputs 4 to 6, the gradients 2, and the others
+// come when these have ended (2048 channels of one sequence of 16384: 16 segments 864 us, 64 831; of 32768: 48 1601, 64 1582, 96 1587).
+// From 1400 waves on what does not fit at once is a round of its own, two waves a SIMD of the gradients: 4096 channels (2048 waves) take 1205 us, 4160 1750,
+// 5120 1844, 8192 2372.
 struct ScanPlan {
   int n, tokens;             // segments, tokens of each: whole blocks
   size_t h_bytes, dt_bytes;  // of the states and the sums of steps

@@ -44,7 +44,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
 
 // log(1 + exp(x)) = max(x, 0) + log1p(w), w = exp(-|x|).  With u = 1 + w rounded and c = w - (u - 1), which is exact, log1p(w) = log(u) + log(1 + c / u);
-// c is at most half a step of u, so that c in the place of the second term is off by c w or less: 2^-24 of the result.
+// c is at most half a step of u, so that c in the place of the second term is off by c w or less: 2^-24 of the result.  The exponential's argument, rounded to
+// float32, adds |x| half steps where x is negative and the result about w.
 __device__ __forceinline__ float softplus(float x) {
   const float w = __builtin_amdgcn_exp2f(-kLog2e * fabsf(x)), u = 1.0f + w, c = w - (u - 1.0f);
   return fmaxf(x, 0.0f) + fmaf(__builtin_amdgcn_logf(u), kLn2, c);

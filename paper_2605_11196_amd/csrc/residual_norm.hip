@@ -13,7 +13,9 @@
 // registers beside their gradients (683 -> 604), no workgroup waits for a place (forward 295 -> 269), and the waves' sums are added by lanes
 // and not by a loop (540 -> 465, 269 -> 264).  A row that fills its workgroup is numbered by the block alone, which takes the addresses
 // off the vector registers.  Asking for the next row ahead was tried: 139 registers in the backward pass and one workgroup, 905 us.  5.1 TB/s
-// forward and 4.6 backward, where a copy reaches 4.9.
+// forward and 4.6 backward, where a copy reaches 4.9.  That holds for the row's norm and for groups of a power of two of columns up to 512, whose sums stay in a
+// wave.  Other groups are added up from LDS by every lane for itself: 80 to 320 columns 2.9 to 5 TB/s forward and 1.7 to 3.3 backward in bfloat16, two groups of
+// 1024 columns 1.5 and 1.1, of 4096 0.4 and 0.3.
 #include "mixer_util.h"
 
 namespace vla {
@@ -68,7 +70,7 @@ struct RawWeight {
 };
 template <typename IO> __device__ __forceinline__ void store8(IO* p, const Eight& e) { store_piece(p, e.v); }
 
-// Where a lane is in its workgroup, and the sums over its row and over its group of columns.  WHOLE: the row fills the workgroup, four waves or more.
+// Where a lane is in its workgroup, and the sums over its row and over its group of columns.  WHOLE: one row fills the workgroup, of three waves or more.
 template <bool WHOLE>
 struct RowLanes {
   int L, lane, row, rows, pieces, each;   // lanes of a row, this one's place, its row among the workgroup's; eights of a row and of a group
@@ -327,15 +329,15 @@ int row_width(int n) {
   while (L < pieces) L *= 2;
   return L;
 }
-// Threads of a workgroup: whole rows, four waves or more (backward: eight, whose number of workgroups is held by what they leave of the weights'
-// gradients; 87381 rows of 1536 in bfloat16, backward: 784 us with four waves, three of them at work).
+// Threads of a workgroup: as many whole rows as four waves hold, or one row (backward: eight waves, as the number of workgroups is held by what they leave of the
+// weights' gradients; 87381 rows of 1536 in bfloat16, backward: 784 us with four waves, three of them at work).
 int threads_of(int L, bool backward) {
   const int most = backward ? 512 : 256;
   return L < most ? most / L * L : L;
 }
 
-// As many as the card's 256 compute units hold at once, with the registers that the kernels take 24 waves each (backward: 16): a workgroup more would go
-// through its rows when all others have ended (backward pass of 52428 rows of 2560 in bfloat16 with 819 workgroups 993 us, with 768 706).
+// As many as the card's 256 compute units hold at once, 24 waves each (their registers would let in 28, in workgroups of 3 to 16) and 16 in the backward pass: a
+// workgroup more would go through its rows when all others have ended (backward pass of 52428 rows of 2560 in bfloat16 with 819 workgroups 993 us, with 768 706).
 int workgroups_of(int threads, bool backward) {
   const int held = (backward ? 16 : 24) / (threads / 64);
   return 256 * (held > 0 ? held : 1);

@@ -6,7 +6,8 @@
 // Bound by vector instructions: an element of the state takes a product and an exponential, the input's product, the update and the
 // read-out, and nothing of that is a matrix product, since every element has a decay of its own.  8 x 2048 tokens, 4096 channels of 16 states,
 // bfloat16: 345 us, vector unit busy for 74 % of the cycles with 8.1 instructions an element (138 us for those five alone), two waves a SIMD, which is all that so
-// many channels give; a long sequence in segments, eight waves a SIMD: 86 %.
+// many channels give; a long sequence in segments: 86 %, with six waves a SIMD at most (80 registers; float32 and 32 states five, 64 states four; 8 states five
+// and four).
 // Few sequences of few channels are cut into time segments: a first pass gives the end of every segment from a zero start and the
 // sum of its steps (its decay is exp(A sum dt)), a second kernel the states that the segments start from.
 #include "selective_lanes.h"

@@ -155,7 +155,7 @@ def residual_norm(x, y=None, weight=None, *, post_weight=None, groups=1, gate=No
     """What stands between a block and the next one, in one pass:  s = x + scale * act(gate) * post_weight * N(y);  h = weight * N(s).
 
     x: the residual stream [B,T,n] or None (zero), y: the block's output [B,T,n] on the GPU (float32 or bfloat16, n a multiple of 8 up to
-    8192; views with a contiguous last dimension are read as they are); x may be float32 with y bfloat16, and s has x's type.  N divides by the
+    8192; views with a contiguous last dimension are read as they are); x may be float32 with y bfloat16; s has x's type and h y's (without y: x's).  N divides by the
     root of the mean square + eps, of the row, and of y over each of `groups` groups of neighbouring columns (heads).  gate [B,T,n] of y's
     type goes through activation ("silu" or "sigmoid"); post_weight, scale and weight [n] share a type.  What is None is left out: without
     post_weight y has no norm, without weight h is None, without y the call is h = weight * N(x), and s is x.  Returns

@@ -118,7 +118,7 @@ def selective_scan_forward(u, delta, A, B, C, D=None, z=None, h0=None, *, delta_
     are read as they are), B, C [B,T,N] or, for G groups of neighbouring channels, [B,T,G,N], of u's type; A [n,N] with N 8, 16, 32 or
     64, D and delta_bias [n] (or None) and h0 [B,n,N] (or None: zero) float32.  softplus False: dt = delta + delta_bias.  lengths: int32
     [B], tokens of each sequence; y is zero beyond.  Returns (y, h_T), and with save_for_backward also what
-    selective_scan_backward needs.  Workspace, outputs and work are on `stream` (default: torch's current one).
+    selective_scan_backward needs (N / 2 bytes for every token and channel).  Workspace, outputs and work are on `stream` (default: torch's current one).
     """
     import torch
 
@@ -249,7 +249,7 @@ def _autograd():
 
 def selective_scan(u, delta, A, B, C, D=None, z=None, h0=None, *, delta_bias=None, softplus=True, lengths=None, stream=None):
     """selective_scan_forward as a differentiable function: (y, h_T), with gradients for u, delta, A, B, C, D, z, delta_bias and h0 (once,
-    in reverse mode, on the current stream)."""
+    in reverse mode, on the current stream).  Until then the states at every 8th token are kept: N / 2 bytes for every token and channel."""
     import torch
 
     _no_tangents(torch, u, delta, A, B, C, D, z, h0, delta_bias)
