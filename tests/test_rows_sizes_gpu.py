@@ -51,7 +51,7 @@ def test_gradients_of_2_28_channels_taps():
 @pytest.mark.parametrize("n,rows,each,groups,stream", [
     # each: rows that a workgroup of the backward pass takes at once
     (264, 2 * 6144 + 1001, 8, 3, None),      # four rows a workgroup forward, groups whose sums go through shared memory
-    (1000, 2 * 3072 + 999, 4, 1, "f32"),     # a row on two waves, two rows a workgroup forward
+    (1000, 4 * 1536 + 999, 4, 1, "f32"),     # a row on two waves, two rows a workgroup forward
     (1536, 2 * 2048 + 1537, 2, 1, None),     # three waves, a row alone forward
     (4096, 2 * 768 + 501, 1, 64, None),      # eight waves, heads of 64 columns
     (4096, 2 * 768 + 501, 1, 1, "f32"),
